@@ -20,8 +20,9 @@
  *     Workspace, where an entry point takes one, is caller-supplied device
  *     memory; its required size comes from the matching *_workspace call.
  *     A NULL workspace (or one that is too small) selects a slower variant
- *     that needs none, so workspace only ever buys speed (the convolution,
- *     whose unfolded input lives there, is the one exception).
+ *     that needs none, so workspace only ever buys speed. The exceptions need
+ *     theirs: the convolution (its unfolded input), mt_attention_bwd and the
+ *     weight gradients of mt_qk_norm_rope_bwd.
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *     All device work is enqueued on it asynchronously; results are visible
  *     after the caller synchronises that stream.
@@ -43,7 +44,7 @@
  *     terms and ReLU layers (mt_linear_act_fwd), whose gradients turn on the
  *     sign of a sum. bf16 operands are multiplied
  *     exactly and accumulated in fp32 (v_mfma_f32_32x32x16_bf16). Every
- *     output, bias and bias gradient is fp32.
+ *     output, bias and bias gradient of a product is fp32.
  */
 #ifndef MINITENSOR_HIP_H
 #define MINITENSOR_HIP_H
@@ -57,7 +58,11 @@ extern "C" {
 
 #define MT_MAX_DIMS 8
 
-typedef enum { MT_F32 = 0, MT_BF16 = 1 } mt_dtype;
+typedef enum {
+  MT_F32 = 0,
+  MT_BF16 = 1,
+  MT_I32 = 2  /* lengths and positions, where an entry point asks for them */
+} mt_dtype;
 
 typedef enum {
   MT_OK = 0,
@@ -341,6 +346,128 @@ mt_status mt_reduce_broadcast_grad(const mt_tensor* grad_out, const mt_tensor* g
 
 mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt_tensor* grad_in,
                                              size_t* bytes);
+
+/* ------------------------------------------------------------- attention
+ * Softmax attention of HQ query heads over HK key heads (HQ a multiple of HK;
+ * query head h reads key head h / (HQ / HK)), for training and serving:
+ *   S = scale q k^T over the keys a query sees;  lse = log sum exp S
+ *   o = P v,  P = exp(S - lse)
+ * The scores are never stored.
+ *   q, o [B, TQ, HQ, D]; k, v [B, TK, HK, D], one dtype (f32 or bf16), any
+ *   strides with each vector contiguous (memory order [B, H, T, D], packed
+ *   projections and caches are views); o addresses each element once. D is 1
+ *   to 128.
+ *   lse [B, HQ, TQ] f32, contiguous, or NULL (the backward needs it).
+ *   kv_len [B] i32 or NULL (TK): key j of batch b exists for j < kv_len[b]
+ *   (clamped to 0 .. TK). Keys and values past it are never used, whatever
+ *   they hold.
+ *   q_start [B] i32 or NULL (TK - TQ, the last positions): the key position
+ *   of query 0.
+ *   scale: positive and finite, usually D^(-1/2).
+ * flags: MT_CAUSAL: query i sees key j for j <= q_start + i only.
+ * A query that sees no key gets o = 0 and lse = -inf, and its gradients are 0.
+ * A key that some queries see should hold finite values: its infinities and
+ * NaN may reach the queries near them that do not see it.
+ * fp32: products and sums in fp32. bf16: products exact, sums and softmax in
+ * fp32, P rounded to bf16 for its product with v. lse is from fp32 sums.
+ * ws: optional (mt_attention_fwd_workspace): a few queries against many keys
+ * are split along the keys, the parts joined in a fixed order.
+ */
+#define MT_CAUSAL 8u
+mt_status mt_attention_fwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
+                           const mt_tensor* kv_len, const mt_tensor* q_start, const mt_tensor* o,
+                           const mt_tensor* lse, float scale, uint32_t flags, void* ws,
+                           size_t ws_bytes, void* stream);
+mt_status mt_attention_fwd_workspace(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
+                                     const mt_tensor* kv_len, const mt_tensor* q_start,
+                                     const mt_tensor* o, const mt_tensor* lse, uint32_t flags,
+                                     size_t* bytes);
+
+/* mt_attention_bwd: the gradients from dout, P computed again from lse:
+ *   delta = sum_d dout o;  dP = dout v^T;  dS = P (dP - delta)
+ *   dq = scale dS k;  dk = scale dS^T q;  dv = P^T dout
+ *   (dk, dv summed over a key head's query heads)
+ *   o and lse as the forward wrote them; dout the shape and dtype of q; dq, dk,
+ *   dv the shape and dtype of q, k, v, NULL to skip. Outputs may be views of
+ *   one packed buffer. kv_len, q_start, scale and MT_CAUSAL as in the forward;
+ *   dk and dv of keys past kv_len are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
+ *   bf16: P and dS are rounded to bf16 for the products.
+ *   ws: REQUIRED (mt_attention_bwd_workspace): delta, and partial sums.
+ */
+mt_status mt_attention_bwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
+                           const mt_tensor* kv_len, const mt_tensor* q_start, const mt_tensor* o,
+                           const mt_tensor* lse, const mt_tensor* dout, const mt_tensor* dq,
+                           const mt_tensor* dk, const mt_tensor* dv, float scale, uint32_t flags,
+                           void* ws, size_t ws_bytes, void* stream);
+mt_status mt_attention_bwd_workspace(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
+                                     const mt_tensor* kv_len, const mt_tensor* q_start,
+                                     const mt_tensor* o, const mt_tensor* lse, const mt_tensor* dout,
+                                     const mt_tensor* dq, const mt_tensor* dk, const mt_tensor* dv,
+                                     uint32_t flags, size_t* bytes);
+
+/* ------------------------------- head norms with the rotary rotation
+ * mt_qk_norm_rope_fwd: for every head x of D values of the queries and keys
+ *   y = rotate(x (mean x^2 + eps)^(-1/2) w)
+ * where rotate turns pair i of the first R values by the angle whose cosine
+ * and sine are entry i of the token's row of cos and sin:
+ *   (a, b) -> (a cos - b sin, b cos + a sin);
+ * pairs are (i, i + R / 2), with MT_ROPE_INTERLEAVED (2 i, 2 i + 1); the other
+ * D - R values pass.
+ *   q, yq [B, T, HQ, D]; k, yk [B, T, HK, D], or both NULL. q and k share a
+ *   dtype, yq and yk one of their own (f32 or bf16). Strides as for attention;
+ *   D is 1 to 1024.
+ *   wq, wk [D] f32 or NULL (ones).
+ *   cos, sin [B, T, R / 2] f32, rows contiguous, any other strides (0: shared
+ *   by the batch, or by the tokens), or both NULL (R = 0).
+ * Arithmetic is fp32, bf16 results rounded to nearest even once.
+ */
+#define MT_ROPE_INTERLEAVED 16u
+mt_status mt_qk_norm_rope_fwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq,
+                              const mt_tensor* wk, const mt_tensor* cos, const mt_tensor* sin,
+                              const mt_tensor* yq, const mt_tensor* yk, float eps, uint32_t flags,
+                              void* stream);
+
+/* mt_qk_norm_rope_bwd: its gradients, the norms computed again from q and k.
+ * With n = x r, r = (mean x^2 + eps)^(-1/2), and g = dy rotated back:
+ *   dw = sum over tokens and heads of g n;  dx = r (g w - n mean(n g w))
+ *   dyq, dyk: yq's and yk's shapes, one dtype; dq, dk (together, or NULL):
+ *   the shape of q and k, dyq's dtype; dwq, dwk [D] f32 or NULL.
+ * flags: MT_ROPE_INTERLEAVED, MT_ACCUMULATE.
+ * ws: required for dwq and dwk (mt_qk_norm_rope_bwd_workspace): partial sums.
+ */
+mt_status mt_qk_norm_rope_bwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq,
+                              const mt_tensor* wk, const mt_tensor* cos, const mt_tensor* sin,
+                              const mt_tensor* dyq, const mt_tensor* dyk, const mt_tensor* dq,
+                              const mt_tensor* dk, const mt_tensor* dwq, const mt_tensor* dwk,
+                              float eps, uint32_t flags, void* ws, size_t ws_bytes, void* stream);
+mt_status mt_qk_norm_rope_bwd_workspace(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq,
+                                        const mt_tensor* wk, const mt_tensor* cos,
+                                        const mt_tensor* sin, const mt_tensor* dyq,
+                                        const mt_tensor* dyk, const mt_tensor* dq,
+                                        const mt_tensor* dk, const mt_tensor* dwq,
+                                        const mt_tensor* dwk, size_t* bytes);
+
+/* --------------------------------------------------------------- dropout
+ * mt_dropout_fwd: y = residual + x keep / (1 - p'), the mask never stored.
+ *   x, y [M, N] f32 or bf16 each; residual [M, N] of y's dtype, or NULL. Any
+ *   row pitch, inner dim contiguous.
+ * p' is p (0 to 1) rounded to a multiple of 2^-16; with p' = 1 nothing stays.
+ * Element i (row-major) stays where 16 bits drawn for it are not below
+ * 65536 p': of the words w0 .. w3 of Philox4x32-10 (Salmon et al., SC 2011)
+ * with key `seed` (low word first) and counter words (offset + i / 8 as 64
+ * bits, low word first, 0, 0), the low (i even) or high half of word (i % 8) / 2.
+ * A call uses the ceil(M N / 8) counters from `offset`. A dropped element
+ * counts as 0 whatever x holds.
+ */
+mt_status mt_dropout_fwd(const mt_tensor* x, const mt_tensor* residual, float p, uint64_t seed,
+                         uint64_t offset, const mt_tensor* y, void* stream);
+
+/* mt_dropout_bwd: dx = dy keep / (1 - p') with the forward's p, seed and
+ * offset (the residual's gradient is dy itself). dy, dx [M, N] f32 or bf16
+ * each. flags: MT_ACCUMULATE.
+ */
+mt_status mt_dropout_bwd(const mt_tensor* dy, float p, uint64_t seed, uint64_t offset,
+                         const mt_tensor* dx, uint32_t flags, void* stream);
 
 /* ------------------------------------------------------- workspace query
  * mt_workspace_bytes: the workspace size of one call, by operation, with the

@@ -30,8 +30,8 @@ if not os.path.exists(LIB_PATH):
 lib = ctypes.CDLL(LIB_PATH)
 
 MAX_DIMS = 8
-F32, BF16 = 0, 1
-ACCUMULATE, REDUCE_INTO, CONV_REUSE_UNFOLD = 1, 2, 4
+F32, BF16, I32 = 0, 1, 2
+ACCUMULATE, REDUCE_INTO, CONV_REUSE_UNFOLD, CAUSAL, ROPE_INTERLEAVED = 1, 2, 4, 8, 16
 STATUS = {0: "MT_OK", 1: "MT_ERR_NULL", 2: "MT_ERR_NDIM", 3: "MT_ERR_SHAPE", 4: "MT_ERR_DTYPE",
           5: "MT_ERR_LAYOUT", 6: "MT_ERR_ALIAS", 7: "MT_ERR_WORKSPACE", 8: "MT_ERR_HIP",
           9: "MT_ERR_INVALID"}
@@ -43,7 +43,9 @@ EXPORTS = ["mt_linear_fwd", "mt_linear_bwd", "mt_linear_bwd_workspace", "mt_matm
            "mt_linear_act_fwd", "mt_act_bwd", "mt_act_bwd_workspace", "mt_mse_loss",
            "mt_mse_loss_workspace", "mt_sgd_step", "mt_adam_step", "mt_rmsprop_step",
            "mt_conv2d_fwd", "mt_conv2d_fwd_workspace", "mt_conv2d_bwd", "mt_conv2d_bwd_workspace",
-           "mt_workspace_bytes", "mt_linear_bwd_noalloc"]
+           "mt_workspace_bytes", "mt_linear_bwd_noalloc", "mt_attention_fwd", "mt_attention_fwd_workspace",
+           "mt_attention_bwd", "mt_attention_bwd_workspace", "mt_qk_norm_rope_fwd", "mt_qk_norm_rope_bwd",
+           "mt_qk_norm_rope_bwd_workspace", "mt_dropout_fwd", "mt_dropout_bwd"]
 NOALLOC_SCRATCH_BYTES = 32 << 20  # MT_NOALLOC_SCRATCH_BYTES
 NUM_GEMM_CFG = 19  # tile configurations mt_debug_set("cfg", i) accepts
 ACT = {"none": 0, "relu": 1, "sigmoid": 2, "tanh": 3, "gelu": 4}
@@ -83,6 +85,16 @@ lib.mt_conv2d_fwd_workspace.argtypes = [_P, _P, _P, _P, _i32, _i32, _i32, _i32, 
 lib.mt_conv2d_bwd.argtypes = [_P, _P, _P, _P, _P, _P, _i32, _i32, _i32, _i32, _u32, _vp, _sz, _vp]
 lib.mt_conv2d_bwd_workspace.argtypes = [_P, _P, _P, _P, _P, _P, _i32, _i32, _i32, _i32,
                                         ctypes.POINTER(_sz)]
+lib.mt_attention_fwd.argtypes = [_P] * 7 + [_f, _u32, _vp, _sz, _vp]
+lib.mt_attention_fwd_workspace.argtypes = [_P] * 7 + [_u32, ctypes.POINTER(_sz)]
+lib.mt_attention_bwd.argtypes = [_P] * 11 + [_f, _u32, _vp, _sz, _vp]
+lib.mt_attention_bwd_workspace.argtypes = [_P] * 11 + [_u32, ctypes.POINTER(_sz)]
+lib.mt_qk_norm_rope_fwd.argtypes = [_P] * 8 + [_f, _u32, _vp]
+lib.mt_qk_norm_rope_bwd.argtypes = [_P] * 12 + [_f, _u32, _vp, _sz, _vp]
+lib.mt_qk_norm_rope_bwd_workspace.argtypes = [_P] * 12 + [ctypes.POINTER(_sz)]
+_u64 = ctypes.c_uint64
+lib.mt_dropout_fwd.argtypes = [_P, _P, _f, _u64, _u64, _P, _vp]
+lib.mt_dropout_bwd.argtypes = [_P, _f, _u64, _u64, _P, _u32, _vp]
 lib.mt_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.POINTER(_P), ctypes.c_int32]
 lib.mt_debug_set.argtypes = [ctypes.c_char_p, ctypes.c_int64]
 lib.mt_status_str.argtypes = [ctypes.c_int]
@@ -122,12 +134,17 @@ def raw_desc(ptr: int, dtype: int, shape, stride) -> MtTensor:
     return d
 
 
-def desc(t: torch.Tensor | None):
+def desc(t: torch.Tensor | None, index: bool = False):
+    """The descriptor of a tensor (index: one of int32 lengths or positions)."""
     if t is None:
         return None
     if not t.is_cuda:
         raise ValueError("libminitensor_hip works on device tensors (got a CPU tensor)")
-    if t.dtype == torch.float32:
+    if index:
+        if t.dtype != torch.int32:
+            raise TypeError(f"lengths and positions are int32 (got {t.dtype})")
+        dt = I32
+    elif t.dtype == torch.float32:
         dt = F32
     elif t.dtype == torch.bfloat16:
         dt = BF16
@@ -157,7 +174,7 @@ def _current_stream() -> int:
     return _raw_stream(_device())
 
 
-_m.init(lib._handle, torch.float32, torch.bfloat16, desc, _current_stream, _stream)
+_m.init(lib._handle, torch.float32, torch.bfloat16, torch.int32, desc, _current_stream, _stream)
 
 
 def linear_fwd(x, w, b, y, stream=None) -> None:
@@ -313,6 +330,80 @@ def conv2d_bwd(x, w, dy, dx=None, dw=None, db=None, stride=1, padding=0, accumul
     flags = (ACCUMULATE if accumulate else 0) | (CONV_REUSE_UNFOLD if reuse_unfold else 0)
     _check(_m.conv2d_bwd(x, w, dy, dx, dw, db, *_pair(stride), *_pair(padding), flags, workspace, stream),
            "mt_conv2d_bwd")
+
+
+def _attention_args(tensors, kv_len, q_start, rest):
+    return [_ref(desc(t)) for t in tensors] + [_ref(desc(kv_len, True)), _ref(desc(q_start, True))] + \
+        [_ref(desc(t)) for t in rest]
+
+
+def attention_fwd_workspace(q, k, v, o, lse=None, kv_len=None, q_start=None, causal=False) -> int:
+    n = _sz(0)
+    _check(lib.mt_attention_fwd_workspace(*_attention_args((q, k, v), kv_len, q_start, (o, lse)),
+                                          CAUSAL if causal else 0, ctypes.byref(n)), "mt_attention_fwd_workspace")
+    return int(n.value)
+
+
+def _scale(scale, q):
+    return float(scale) if scale is not None else max(1, q.shape[-1]) ** -0.5
+
+
+def attention_fwd(q, k, v, o, lse=None, kv_len=None, q_start=None, scale=None, causal=False, workspace=None,
+                  stream=None) -> None:
+    """o = softmax(scale q k^T) v for q, o [B, TQ, HQ, D], k, v [B, TK, HK, D] (scale: D^-0.5 if None); lse
+    [B, HQ, TQ] receives the log-sum-exp. kv_len, q_start: int32 [B], each batch element's keys and (causal) the
+    key position of its query 0, by default all and TK - TQ."""
+    _check(_m.attention_fwd(q, k, v, kv_len, q_start, o, lse, _scale(scale, q), CAUSAL if causal else 0, workspace,
+                            stream), "mt_attention_fwd")
+
+
+def attention_bwd_workspace(q, k, v, o, lse, dout, dq=None, dk=None, dv=None, kv_len=None, q_start=None,
+                            causal=False) -> int:
+    n = _sz(0)
+    _check(lib.mt_attention_bwd_workspace(*_attention_args((q, k, v), kv_len, q_start, (o, lse, dout, dq, dk, dv)),
+                                          CAUSAL if causal else 0, ctypes.byref(n)), "mt_attention_bwd_workspace")
+    return int(n.value)
+
+
+def attention_bwd(q, k, v, o, lse, dout, dq=None, dk=None, dv=None, kv_len=None, q_start=None, scale=None,
+                  causal=False, accumulate=False, workspace=None, stream=None) -> None:
+    """The gradients of attention_fwd from dout (None skips one); needs the workspace."""
+    flags = (CAUSAL if causal else 0) | (ACCUMULATE if accumulate else 0)
+    _check(_m.attention_bwd(q, k, v, kv_len, q_start, o, lse, dout, dq, dk, dv, _scale(scale, q), flags, workspace,
+                            stream), "mt_attention_bwd")
+
+
+def qk_norm_rope_fwd(q, k, wq, wk, cos, sin, yq, yk, eps=1e-6, interleaved=False, stream=None) -> None:
+    """yq, yk = rotate(norm(q) wq), rotate(norm(k) wk) head by head; q [B, T, HQ, D], k [B, T, HK, D] (or None with
+    wk and yk), cos and sin [B, T, R / 2]."""
+    _check(_m.qk_norm_rope_fwd(q, k, wq, wk, cos, sin, yq, yk, eps, ROPE_INTERLEAVED if interleaved else 0, stream),
+           "mt_qk_norm_rope_fwd")
+
+
+def qk_norm_rope_bwd_workspace(q, k, wq, wk, cos, sin, dyq, dyk, dq=None, dk=None, dwq=None, dwk=None) -> int:
+    n = _sz(0)
+    ds = [desc(t) for t in (q, k, wq, wk, cos, sin, dyq, dyk, dq, dk, dwq, dwk)]
+    _check(lib.mt_qk_norm_rope_bwd_workspace(*[_ref(d) for d in ds], ctypes.byref(n)),
+           "mt_qk_norm_rope_bwd_workspace")
+    return int(n.value)
+
+
+def qk_norm_rope_bwd(q, k, wq, wk, cos, sin, dyq, dyk, dq=None, dk=None, dwq=None, dwk=None, eps=1e-6,
+                     interleaved=False, accumulate=False, workspace=None, stream=None) -> None:
+    """The gradients of qk_norm_rope_fwd (dq and dk together; None skips); dwq and dwk need the workspace."""
+    flags = (ROPE_INTERLEAVED if interleaved else 0) | (ACCUMULATE if accumulate else 0)
+    _check(_m.qk_norm_rope_bwd(q, k, wq, wk, cos, sin, dyq, dyk, dq, dk, dwq, dwk, eps, flags, workspace, stream),
+           "mt_qk_norm_rope_bwd")
+
+
+def dropout_fwd(x, residual, p, seed, offset, y, stream=None) -> None:
+    """y = residual + dropout(x) (residual may be None); the mask is a function of seed and offset."""
+    _check(_m.dropout_fwd(x, residual, p, seed, offset, y, stream), "mt_dropout_fwd")
+
+
+def dropout_bwd(dy, p, seed, offset, dx, accumulate=False, stream=None) -> None:
+    """dx = dy with the forward's mask and scale."""
+    _check(_m.dropout_bwd(dy, p, seed, offset, dx, ACCUMULATE if accumulate else 0, stream), "mt_dropout_bwd")
 
 
 def _shape_call(fn, a, b, where):

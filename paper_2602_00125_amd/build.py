@@ -20,11 +20,12 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["gemm_f32.hip", "gemm_bf16.hip", "reduce.hip", "elementwise.hip", "conv.hip", "noalloc.hip",
-           "shape.cpp", "capi.cpp", "conv_host.cpp"]
+           "attention.hip", "dropout.hip", "head_norm.hip", "shape.cpp", "capi.cpp", "conv_host.cpp",
+           "attention_host.cpp"]
 # what is compiled: (source, extra flags); the fp32 products take most of the
 # time and compile in parts, side by side
 UNITS = ([("gemm_f32.hip", [f"-DMT_F32_PART={n}"]) for n in (3, 4, 1, 2, 6, 5)] +
-         [(s, []) for s in SOURCES if s != "gemm_f32.hip"])
+         [(s, ["-DMT_SEPARATE_UNITS"]) for s in SOURCES if s != "gemm_f32.hip"])
 COMMON = ["-std=c++17", "-O3", "-fPIC", "-Wall", "-Wno-unused-result",
           f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-I", os.path.join(HERE, "..", "include")]

@@ -1,0 +1,668 @@
+// Attention and its gradient, gfx950, one pass over the data each.
+//
+//   S = scale q k^T over the visible keys, lse = log sum exp S, P = exp(S - lse)
+//   o = P v
+//   delta = sum_d do o, dP = do v^T, dS = P (dP - delta)
+//   dq = scale dS k, dk = scale dS^T q, dv = P^T do
+//
+// The scores are never stored: the forward keeps a running maximum and sum,
+// the backward computes P anew from lse. The same scheme serves all three
+// kernels. A wave owns 32 tokens (queries; keys in the dk / dv pass), one a
+// lane of each half-wave, whose vectors sit in registers as the right operand
+// of the MFMAs. Tiles of the other tokens stream through LDS. A product
+// stream x own comes out with the wave's token in the lane and 16 of 32 stream
+// tokens in registers (f32x16), so softmax statistics are one value a lane and
+// P goes back into the next product from the registers it is in:
+//   dot:   C[r][n]  = sum_d tile[r][d] own[n][d]     (S, dP)
+//   accum: A[d][n] += sum_r tile[r][d] C[r][n]       (o, dq; dk, dv)
+// The MFMA's C holds row 8 (i / 4) + 4 h + i % 4 in register i of lane half h.
+// The rows of the left operand are handed to it in an order that makes this
+// row 16 (i / 8) + 8 h + i % 8 of the tile (tile_row): eight consecutive stream
+// tokens a half, which is what the next product's right operand wants (no
+// exchange between lanes), and eight consecutive d of a result row, written by
+// 16-byte stores.
+//
+// Sums, statistics and accumulators are fp32. With bf16 inputs P and dS are
+// rounded to bf16 (nearest even) for the second product: the matrix cores'
+// operand type, an error of 2^-8 of a term where the output is rounded to
+// bf16 as well. The row sum of P is taken before the rounding.
+//
+// Each result is summed by one block in a fixed order: no atomics. dq and
+// dk / dv take a pass each, and both compute S and dP (7 products in place of
+// 5): adding dq across the blocks of one pass would take atomics, or partial
+// sums of 4 bytes a d for every 128 keys, which cost more than the products.
+#include <hip/hip_runtime.h>
+
+#include "attention.hpp"
+#include "gemm_dma.hpp"
+
+namespace mt {
+namespace attn {
+
+using gemm::dma16;
+using gemm::dma4;
+using gemm::kOOB;
+using gemm::kRsrcWord3;
+using gemm::lds_byte_addr;
+using gemm::uniform_ptr;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kInf = __builtin_inff();
+
+// All loads and LDS accesses of this wave done, then every wave's.
+__device__ __forceinline__ void wait_all_barrier() {
+  __asm__ __volatile__("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// The stream row a lane hands to the MFMA as row lane & 31 (see the top).
+__device__ __forceinline__ int tile_row(int lane) {
+  const int m = lane & 31;
+  return 16 * (m >> 4) + 8 * ((m >> 2) & 1) + 4 * ((m >> 3) & 1) + (m & 3);
+}
+
+// Maximum / sum over the two lanes (n, n + 32) that share an own token.
+__device__ __forceinline__ u32x2 halves(float v) {
+  return __builtin_bit_cast(
+      u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false));
+}
+__device__ __forceinline__ float max_halves(float v) {
+  const u32x2 s = halves(v);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+  const u32x2 s = halves(v);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+  bf16x2 v;
+  v[0] = (__bf16)a;
+  v[1] = (__bf16)b;
+  return __builtin_bit_cast(unsigned, v);
+}
+
+__device__ __forceinline__ float ld_elem(const char* p, int64_t i, bool bf) {
+  return bf ? __uint_as_float((unsigned)((const unsigned short*)p)[i] << 16) : ((const float*)p)[i];
+}
+
+// A tile of stream tokens in LDS, rows of RB bytes in 16-byte chunks whose
+// index is XORed with a function of the row, so that both kinds of reads hit
+// distinct banks: `dot` reads one chunk of 16 rows that differ modulo 16,
+// `accum` four consecutive rows x four chunks (bf16, ds_read_b64_tr_b16) or
+// two rows 8 apart (fp32, 4-byte reads).
+template <bool BF, int DP>
+struct Tile {
+  static constexpr int ES = BF ? 2 : 4;
+  static constexpr int RB = DP <= 64 ? 64 * ES : 128 * ES;
+  static constexpr int EPC = 16 / ES;
+  static constexpr int ND = DP / 32;
+  static constexpr int NF = DP * ES / 32;  // 16-byte own fragments a lane
+  static __device__ __forceinline__ int swz(int r) {
+    if constexpr (!BF) return r & 15;
+    else if constexpr (RB == 256) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+  }
+};
+
+// What a wave multiplies tiles with: 32 own tokens, one a lane.
+template <bool BF, int DP>
+struct Own {
+  using T = Tile<BF, DP>;
+  u32x4 f[T::NF];
+  // row: the lane's token in global memory (not read unless ok)
+  template <bool VEC>
+  __device__ __forceinline__ void load(const char* row, bool ok, int D, int lane) {
+    const int h = lane >> 5;
+#pragma unroll
+    for (int s = 0; s < T::NF; ++s) {
+      const int d = (2 * s + h) * T::EPC;
+      f[s] = u32x4{0, 0, 0, 0};
+      if constexpr (VEC) {
+        if (ok && d < D) f[s] = *(const u32x4*)(row + d * T::ES);
+      } else if (ok) {
+        if constexpr (BF) {
+          u16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (d + e < D) v[e] = ((const unsigned short*)row)[d + e];
+          f[s] = __builtin_bit_cast(u32x4, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (d + e < D) f[s][e] = ((const unsigned*)row)[d + e];
+        }
+      }
+    }
+  }
+  // sum over d of the lane's part of own . other
+  __device__ __forceinline__ float dot(const Own& b) const {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < T::NF; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (BF) {
+          s = fmaf(__uint_as_float(f[i][e] << 16), __uint_as_float(b.f[i][e] << 16), s);
+          s = fmaf(__uint_as_float(f[i][e] & 0xffff0000u), __uint_as_float(b.f[i][e] & 0xffff0000u), s);
+        } else {
+          s = fmaf(__uint_as_float(f[i][e]), __uint_as_float(b.f[i][e]), s);
+        }
+      }
+    return s;
+  }
+};
+
+// C[r][n] = sum_d tile[r0 + r][d] own[n][d], r in 0..31 (r0 a multiple of 32).
+template <bool BF, int DP>
+__device__ __forceinline__ f32x16 dot(const char* S, int r0, const Own<BF, DP>& own, int lane) {
+  using T = Tile<BF, DP>;
+  const int r = tile_row(lane), h = lane >> 5;
+  const char* row = S + (r0 + r) * T::RB;
+  const int x = T::swz(r);
+  f32x16 c = {};
+#pragma unroll
+  for (int s = 0; s < T::NF; ++s) {
+    const u32x4 a = *(const u32x4*)(row + (((2 * s + h) ^ x) * 16));
+    if constexpr (BF) {
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, own.f[s]), c,
+                                                  0, 0, 0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(own.f[s][e]), c,
+                                                 0, 0, 0);
+    }
+  }
+  return c;
+}
+
+// acc[d][n] += sum_r tile[r0 + r][d] c[r][n], r in 0..31.
+template <bool BF, int DP>
+__device__ __forceinline__ void accum(const char* S, int r0, const f32x16& c, f32x16 (&acc)[DP / 32], int lane) {
+  using T = Tile<BF, DP>;
+  const int h = lane >> 5;
+  if constexpr (BF) {
+    // ds_read_b64_tr_b16: lane s of a 16-lane group addresses four columns of
+    // row s / 4; lane i receives the rows' column 4 p(i / 4) + i % 4, where
+    // p swaps the middle two of four column groups (the order of tile_row)
+    const int s = lane & 15, g = (lane >> 4) & 1;
+    const int pc = ((s & 1) << 1) | ((s >> 1) & 1);
+    const int rl = 8 * h + (s >> 2);
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 b;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[e] = pack_bf16(c[8 * kk + 2 * e], c[8 * kk + 2 * e + 1]);
+      const char* base = S + (r0 + 16 * kk) * T::RB + 8 * (pc & 1);
+#pragma unroll
+      for (int db = 0; db < T::ND; ++db) {
+        const int ch = 4 * db + 2 * g + (pc >> 1);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(const void*)(base + rl * T::RB + ((ch ^ T::swz(rl)) * 16)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(const void*)(base + (rl + 4) * T::RB + ((ch ^ T::swz(rl + 4)) * 16)));
+        u32x4 a;
+        const u32x2 l2 = __builtin_bit_cast(u32x2, lo), h2 = __builtin_bit_cast(u32x2, hi);
+        a[0] = l2[0]; a[1] = l2[1]; a[2] = h2[0]; a[3] = h2[1];
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b),
+                                                          acc[db], 0, 0, 0);
+      }
+    }
+  } else {
+    const int d = tile_row(lane);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = 16 * (i >> 3) + 8 * h + (i & 7);
+      const char* row = S + (r0 + r) * T::RB + 4 * (d & 3);
+#pragma unroll
+      for (int db = 0; db < T::ND; ++db) {
+        const float a = *(const float*)(row + (((8 * db + (d >> 2)) ^ T::swz(r)) * 16));
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, c[i], acc[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// Stream tokens into a tile of ROWS rows by NW waves: straight into LDS where
+// 16-byte loads are allowed, by element through registers elsewhere. Rows from
+// `left` on and columns from D on are zero.
+template <bool BF, int DP, int ROWS, int NW, bool VEC>
+struct Loader {
+  using T = Tile<BF, DP>;
+  static constexpr int JB = ROWS * T::RB / 1024 / NW;
+  static_assert(ROWS * T::RB % (1024 * NW) == 0, "whole instructions for every wave");
+  uint32_t off[JB];
+  int wave, lane, D;
+  int64_t st;
+  __device__ __forceinline__ int row(int j) const { return (1024 * (wave + NW * j) + 16 * lane) / T::RB; }
+  __device__ __forceinline__ int col(int j) const {
+    const int byte = 1024 * (wave + NW * j) + 16 * lane;
+    return (((byte % T::RB) / 16) ^ T::swz(byte / T::RB)) * T::EPC;
+  }
+  __device__ __forceinline__ void init(int wave_, int lane_, int64_t st_, int D_) {
+    wave = wave_;
+    lane = lane_;
+    D = D_;
+    st = st_;
+    if constexpr (VEC) {
+#pragma unroll
+      for (int j = 0; j < JB; ++j) off[j] = col(j) < D ? (uint32_t)((row(j) * (uint32_t)st + col(j)) * T::ES) : kOOB;
+    }
+  }
+  // base: the tile's first token in global memory
+  __device__ __forceinline__ void load(const char* base, int left, char* tile) const {
+    if constexpr (VEC) {
+      const __amdgpu_buffer_rsrc_t r =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(uniform_ptr(base)), (short)0, 0x7fffffff, kRsrcWord3);
+      const uint32_t lds0 = lds_byte_addr(tile);
+#pragma unroll
+      for (int j = 0; j < JB; ++j) dma16(r, row(j) < left ? off[j] : kOOB, lds0 + 1024 * (wave + NW * j));
+    } else {
+      for (int j = 0; j < JB; ++j) {
+        const int rr = row(j), d = col(j);
+        u32x4 v = {0, 0, 0, 0};
+        if (rr < left) {
+          const char* src = base + (rr * st + d) * T::ES;
+          if constexpr (BF) {
+            u16x8 w = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (d + e < D) w[e] = ((const unsigned short*)src)[e];
+            v = __builtin_bit_cast(u32x4, w);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (d + e < D) v[e] = ((const unsigned*)src)[e];
+          }
+        }
+        *(u32x4*)(tile + 1024 * (wave + NW * j) + 16 * lane) = v;
+      }
+    }
+  }
+};
+
+// Result rows: acc[d][n] x mul to token n's row (not written unless ok).
+template <bool BF, int DP, bool VEC>
+__device__ __forceinline__ void store_rows(char* row, bool ok, int D, const f32x16 (&acc)[DP / 32], float mul, bool add,
+                                           int lane) {
+  if (!ok) return;
+  const int h = lane >> 5;
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      const int d = 32 * db + 16 * kk + 8 * h;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = acc[db][8 * kk + e] * mul;
+      if constexpr (VEC && BF) {
+        if (d < D) {
+          u32x4* dst = (u32x4*)(row + d * 2);
+          if (add) {
+            const u32x4 old = *dst;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              v[2 * e] += __uint_as_float(old[e] << 16);
+              v[2 * e + 1] += __uint_as_float(old[e] & 0xffff0000u);
+            }
+          }
+          u32x4 w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+          *dst = w;
+        }
+      } else if constexpr (VEC) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (d + 4 * q < D) {
+            f32x4* dst = (f32x4*)(row + (d + 4 * q) * 4);
+            f32x4 w = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            if (add) w += *dst;
+            *dst = w;
+          }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (d + e < D) {
+            const float w = add ? v[e] + ld_elem(row, d + e, BF) : v[e];
+            if constexpr (BF) ((__bf16*)row)[d + e] = (__bf16)w;
+            else ((float*)row)[d + e] = w;
+          }
+      }
+    }
+}
+
+// Work item of this block: eight runs of consecutive items, one an XCD (blocks
+// go to the XCDs in turn), so that the blocks that read one head's keys share
+// an L2. -1: none.
+__device__ __forceinline__ int work_item(int total) {
+  const int per = (total + 7) >> 3;
+  const int w = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  return (int)(blockIdx.x >> 3) < per && w < total ? w : -1;
+}
+
+// Keys of a batch element, and the key position of its query 0.
+struct Span {
+  int len;
+  int64_t start;
+};
+__device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
+  Span s;
+  s.len = p.TK;
+  if (p.kv_len) {
+    const int n = p.kv_len[b];
+    s.len = n < 0 ? 0 : n < p.TK ? n : p.TK;
+  }
+  s.start = p.q_start ? (int64_t)p.q_start[b] : (int64_t)p.TK - p.TQ;
+  return s;
+}
+// How many keys query i sees (the first ones).
+__device__ __forceinline__ int visible(const AttnParams& p, const Span& s, int i) {
+  if (!p.causal) return s.len;
+  const int64_t n = s.start + i + 1;
+  return n <= 0 ? 0 : n < s.len ? (int)n : s.len;
+}
+
+__device__ __forceinline__ char* row_of(const HeadView& v, int b, int64_t t, int h, int es) {
+  return (char*)v.p + (b * v.sb + t * v.st + h * v.sh) * es;
+}
+
+// The running softmax of a wave's 32 queries.
+template <int DP>
+struct Softmax {
+  float m = -kInf, l = 0.f;  // maximum (log2 units; may lag) and this half's sum
+  // S (scaled by c in here) of N x 32 stream keys becomes P, masked where
+  // key >= lim; acc is rescaled when the maximum has grown enough.
+  template <int N, bool MASK>
+  __device__ __forceinline__ void step(f32x16 (&S)[N], float c, int lim, f32x16 (&acc)[DP / 32]) {
+    float t = -kInf;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (MASK && 32 * n + 16 * (i >> 3) + (i & 7) >= lim) S[n][i] = -kInf;
+        t = fmaxf(t, S[n][i]);
+      }
+    t = max_halves(t) * c;
+    // The result is the same for any m that keeps the terms in range, so m
+    // follows the maximum only once it lags by 2^8.
+    if (__any(t > m + 8.f)) {
+      const float nm = fmaxf(t, m);
+      const float f = nm == -kInf ? 1.f : __builtin_amdgcn_exp2f(m - nm);
+      m = nm;
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < DP / 32; ++db) acc[db] *= f;
+    }
+    const float off = m == -kInf ? 0.f : m;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        S[n][i] = __builtin_amdgcn_exp2f(fmaf(S[n][i], c, -off));
+        l += S[n][i];
+      }
+  }
+};
+
+// ---------------------------------------------------------------- forward
+// A block holds 128 queries of one head (32 a wave) and walks the keys they
+// see in tiles of BK, each tile's loads in flight while the one before is
+// worked on.
+template <bool BF, int DP, bool VEC>
+__global__ __launch_bounds__(256, 2) void fwd_kernel(const AttnParams p) {
+  using T = Tile<BF, DP>;
+  constexpr int BK = BF ? 64 : 32, N = BK / 32, BYTES = BK * T::RB;
+  __shared__ __align__(1024) char lds[2][2][BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nqb = (p.TQ + 127) >> 7;
+  const int w = work_item(p.B * p.HQ * nqb);
+  if (w < 0) return;
+  // a key head's query heads together; the blocks that see most keys first
+  const int g = w % p.G, qb = nqb - 1 - (w / p.G) % nqb, bh = w / p.G / nqb;
+  const int hk = bh % p.HK, b = bh / p.HK, hq = hk * p.G + g;
+  const Span sp = span_of(p, b);
+  const int q0 = qb * 128 + wave * 32, qi = q0 + (lane & 31);
+  const bool ok = qi < p.TQ;
+  const int lim = ok ? visible(p, sp, qi) : 0;
+  const int last = qb * 128 + 127 < p.TQ ? qb * 128 + 127 : p.TQ - 1;
+  const int kend = visible(p, sp, last);  // of the whole block
+  // of this wave: no key past wmax is seen, every key before wmin by all
+  const int wlast = q0 + 31 < p.TQ ? q0 + 31 : p.TQ - 1;
+  const int wmax = q0 < p.TQ ? visible(p, sp, wlast) : 0, wmin = q0 < p.TQ ? visible(p, sp, q0) : 0;
+
+  Own<BF, DP> q;
+  q.template load<VEC>(row_of(p.q, b, ok ? qi : 0, hq, T::ES), ok, p.D, lane);
+  Loader<BF, DP, BK, 4, VEC> lk, lv;
+  lk.init(wave, lane, p.k.st, p.D);
+  lv.init(wave, lane, p.v.st, p.D);
+  const char* kbase = row_of(p.k, b, 0, hk, T::ES);
+  const char* vbase = row_of(p.v, b, 0, hk, T::ES);
+  auto fetch = [&](int k0, int buf) {
+    lk.load(kbase + (int64_t)k0 * p.k.st * T::ES, sp.len - k0, lds[buf][0]);
+    lv.load(vbase + (int64_t)k0 * p.v.st * T::ES, sp.len - k0, lds[buf][1]);
+  };
+  f32x16 acc[T::ND] = {};
+  Softmax<DP> sm;
+  if (kend > 0) fetch(0, 0);
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += BK, buf ^= 1) {
+    wait_all_barrier();
+    if (k0 + BK < kend) fetch(k0 + BK, buf ^ 1);
+    if (k0 >= wmax) continue;
+    const char *K = lds[buf][0], *V = lds[buf][1];
+    f32x16 S[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) S[n] = dot<BF, DP>(K, 32 * n, q, lane);
+    if (k0 + BK > wmin) sm.template step<N, true>(S, p.scale_log2, lim - k0 - 8 * (lane >> 5), acc);
+    else sm.template step<N, false>(S, p.scale_log2, 0, acc);
+#pragma unroll
+    for (int n = 0; n < N; ++n) accum<BF, DP>(V, 32 * n, S[n], acc, lane);
+  }
+  const float l = sum_halves(sm.l);
+  store_rows<BF, DP, VEC>(row_of(p.o, b, ok ? qi : 0, hq, T::ES), ok, p.D, acc, l > 0.f ? 1.f / l : 0.f, false, lane);
+  if (p.lse && ok && lane < 32)
+    p.lse[((int64_t)b * p.HQ + hq) * p.TQ + qi] = l > 0.f ? (sm.m + __builtin_amdgcn_logf(l)) * kLn2 : (l == l ? -kInf : l);
+}
+
+// --------------------------------------------------------------- backward
+// dq: the forward's walk with two tiles' products before and one after the
+// softmax. Also delta, which the dk / dv pass reads.
+template <bool BF, int DP, bool VEC>
+__global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
+  using T = Tile<BF, DP>;
+  constexpr int BK = BF ? 64 : 32, N = BK / 32, BYTES = BK * T::RB;
+  __shared__ __align__(1024) char lds[2][2][BYTES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nqb = (p.TQ + 127) >> 7;
+  const int w = work_item(p.B * p.HQ * nqb);
+  if (w < 0) return;
+  const int g = w % p.G, qb = nqb - 1 - (w / p.G) % nqb, bh = w / p.G / nqb;
+  const int hk = bh % p.HK, b = bh / p.HK, hq = hk * p.G + g;
+  const Span sp = span_of(p, b);
+  const int q0 = qb * 128 + wave * 32, qi = q0 + (lane & 31);
+  const bool ok = qi < p.TQ;
+  const int lim = ok ? visible(p, sp, qi) : 0;
+  const int last = qb * 128 + 127 < p.TQ ? qb * 128 + 127 : p.TQ - 1;
+  const int kend = p.with_dq ? visible(p, sp, last) : 0;
+  const int wlast = q0 + 31 < p.TQ ? q0 + 31 : p.TQ - 1;
+  const int wmax = q0 < p.TQ ? visible(p, sp, wlast) : 0, wmin = q0 < p.TQ ? visible(p, sp, q0) : 0;
+
+  Loader<BF, DP, BK, 4, VEC> lk, lv;
+  lk.init(wave, lane, p.k.st, p.D);
+  lv.init(wave, lane, p.v.st, p.D);
+  const char* kbase = row_of(p.k, b, 0, hk, T::ES);
+  const char* vbase = row_of(p.v, b, 0, hk, T::ES);
+  auto fetch = [&](int k0, int buf) {
+    lk.load(kbase + (int64_t)k0 * p.k.st * T::ES, sp.len - k0, lds[buf][0]);
+    lv.load(vbase + (int64_t)k0 * p.v.st * T::ES, sp.len - k0, lds[buf][1]);
+  };
+  if (kend > 0) fetch(0, 0);
+  Own<BF, DP> q, go;
+  const int64_t qrow = ok ? qi : 0, stat = ((int64_t)b * p.HQ + hq) * p.TQ + qrow;
+  go.template load<VEC>(row_of(p.dout, b, qrow, hq, T::ES), ok, p.D, lane);
+  q.template load<VEC>(row_of(p.o, b, qrow, hq, T::ES), ok, p.D, lane);
+  const float delta = sum_halves(go.dot(q));
+  if (ok && lane < 32) p.delta[stat] = delta;
+  if (!p.with_dq) return;
+  q.template load<VEC>(row_of(p.q, b, qrow, hq, T::ES), ok, p.D, lane);
+  // P = exp2(c S - lse2). A query that sees nothing has lse = -inf; all its
+  // keys are masked.
+  const float lse2 = ok ? p.lse[stat] * kLog2e : 0.f;
+
+  f32x16 acc[T::ND] = {};
+  auto tile = [&](auto masked, const char* K, const char* V, int lm) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      f32x16 S = dot<BF, DP>(K, 32 * n, q, lane);
+      const f32x16 dP = dot<BF, DP>(V, 32 * n, go, lane);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float pr = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse2)) * (dP[i] - delta);
+        S[i] = masked && 32 * n + 16 * (i >> 3) + (i & 7) >= lm ? 0.f : pr;
+      }
+      accum<BF, DP>(K, 32 * n, S, acc, lane);
+    }
+  };
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += BK, buf ^= 1) {
+    wait_all_barrier();
+    if (k0 + BK < kend) fetch(k0 + BK, buf ^ 1);
+    if (k0 >= wmax) continue;
+    if (k0 + BK > wmin) tile(std::true_type{}, lds[buf][0], lds[buf][1], lim - k0 - 8 * (lane >> 5));
+    else tile(std::false_type{}, lds[buf][0], lds[buf][1], 0);
+  }
+  store_rows<BF, DP, VEC>(row_of(p.dq, b, qrow, hq, T::ES), ok, p.D, acc, p.scale, p.accumulate, lane);
+}
+
+// dk and dv: a block holds 128 keys of one head and walks the queries that see
+// them, over all query heads of the group.
+template <bool BF, int DP, bool VEC>
+__global__ __launch_bounds__(256, 2) void dkv_kernel(const AttnParams p) {
+  using T = Tile<BF, DP>;
+  constexpr int BQ = BF ? 64 : 32, N = BQ / 32, BYTES = BQ * T::RB;
+  __shared__ __align__(1024) char lds[2][2][BYTES];
+  __shared__ __align__(256) float stats[2][2][64];  // lse, delta of the tile's queries
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nkb = (p.TK + 127) >> 7;
+  const int w = work_item(p.B * p.HK * nkb);
+  if (w < 0) return;
+  const int kb = w % nkb, bh = w / nkb, hk = bh % p.HK, b = bh / p.HK;
+  const Span sp = span_of(p, b);
+  const int k0 = kb * 128 + wave * 32, kj = k0 + (lane & 31);
+  const bool in = kj < p.TK, ok = kj < sp.len;
+  const int krow = in ? kj : 0;
+  // query tiles from the first that sees a key of the block; per wave, no
+  // query before wfirst sees a key, every query from wall on sees all
+  const bool any = kb * 128 < sp.len;
+  auto first_for = [&](int key) {
+    const int64_t i = p.causal ? (int64_t)key - sp.start : 0;
+    return i < 0 ? 0 : i < p.TQ ? (int)i : p.TQ;
+  };
+  const int q_first = any ? first_for(kb * 128) / BQ * BQ : p.TQ;
+  const int tiles = (p.TQ - q_first + BQ - 1) / BQ;
+  const int wfirst = first_for(k0), wall = first_for(k0 + 31);
+  const bool wave_on = k0 < sp.len;
+  const int64_t see = p.causal ? (int64_t)kj - sp.start : 0;  // queries from here on see the lane's key
+  const int see_i = see < 0 ? 0 : see < p.TQ ? (int)see : p.TQ;
+
+  Loader<BF, DP, BQ, 4, VEC> lq, lo;
+  lq.init(wave, lane, p.q.st, p.D);
+  lo.init(wave, lane, p.dout.st, p.D);
+  auto fetch = [&](int it, int buf) {
+    const int hq = hk * p.G + it / tiles, t0 = q_first + it % tiles * BQ;
+    lq.load(row_of(p.q, b, t0, hq, T::ES), p.TQ - t0, lds[buf][0]);
+    lo.load(row_of(p.dout, b, t0, hq, T::ES), p.TQ - t0, lds[buf][1]);
+    if (wave < 2) {  // a 4-byte statistic a lane
+      const float* s = (wave ? p.delta : p.lse) + ((int64_t)b * p.HQ + hq) * p.TQ + t0;
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<char*>(uniform_ptr((const char*)s)), (short)0, 0x7fffffff, kRsrcWord3);
+      dma4(r, lane < BQ && lane < p.TQ - t0 ? 4u * lane : kOOB, lds_byte_addr(stats[buf][wave]));
+    }
+  };
+  const int iters = tiles * p.G;
+  if (iters > 0) fetch(0, 0);
+  Own<BF, DP> k, v;
+  k.template load<VEC>(row_of(p.k, b, krow, hk, T::ES), ok, p.D, lane);
+  v.template load<VEC>(row_of(p.v, b, krow, hk, T::ES), ok, p.D, lane);
+  f32x16 ak[T::ND] = {}, av[T::ND] = {};
+  // from: of the 64 queries, the lane's key is seen by those from this one on
+  auto tile = [&](auto masked, const char* Q, const char* O, const float (&st)[2][64], int from) {
+    const int h8 = 8 * (lane >> 5);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      f32x16 S = dot<BF, DP>(Q, 32 * n, k, lane);
+      f32x16 dP = dot<BF, DP>(O, 32 * n, v, lane);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int r = 32 * n + 16 * (i >> 3) + (i & 7);
+        const float e = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -st[0][r + h8] * kLog2e));
+        S[i] = masked && r < from ? 0.f : e;
+        dP[i] = S[i] * (dP[i] - st[1][r + h8]);
+      }
+      accum<BF, DP>(O, 32 * n, S, av, lane);
+      accum<BF, DP>(Q, 32 * n, dP, ak, lane);
+    }
+  };
+  for (int it = 0, buf = 0; it < iters; ++it, buf ^= 1) {
+    wait_all_barrier();
+    if (it + 1 < iters) fetch(it + 1, buf ^ 1);
+    const int t0 = q_first + it % tiles * BQ;
+    if (!wave_on || t0 + BQ <= wfirst) continue;
+    if (t0 < wall) tile(std::true_type{}, lds[buf][0], lds[buf][1], stats[buf], see_i - t0 - 8 * (lane >> 5));
+    else tile(std::false_type{}, lds[buf][0], lds[buf][1], stats[buf], 0);
+  }
+  // keys past the batch element's length take no part: zero
+  if (p.dk.p)
+    store_rows<BF, DP, VEC>(row_of(p.dk, b, krow, hk, T::ES), in && (ok || !p.accumulate), p.D, ak, ok ? p.scale : 0.f,
+                            p.accumulate, lane);
+  if (p.dv.p)
+    store_rows<BF, DP, VEC>(row_of(p.dv, b, krow, hk, T::ES), in && (ok || !p.accumulate), p.D, av, ok ? 1.f : 0.f,
+                            p.accumulate, lane);
+}
+
+}  // namespace attn
+
+namespace {
+
+template <typename F>
+hipError_t by_width(int D, F f) {
+  if (D <= 64) return f(std::integral_constant<int, 64>{});
+  if (D <= 96) return f(std::integral_constant<int, 96>{});
+  return f(std::integral_constant<int, 128>{});
+}
+// the grid of `items` work items (attn::work_item)
+dim3 grid_of(int64_t items) { return dim3((unsigned)((items + 7) / 8 * 8)); }
+
+#define MT_ATTN_LAUNCH(kernel, items)                                                               \
+  by_width(p.D, [&](auto dp) {                                                                      \
+    constexpr int DP = decltype(dp)::value;                                                         \
+    const dim3 grid = grid_of(items);                                                               \
+    if (bf16 && vec) attn::kernel<true, DP, true><<<grid, 256, 0, stream>>>(p);                     \
+    else if (bf16) attn::kernel<true, DP, false><<<grid, 256, 0, stream>>>(p);                      \
+    else if (vec) attn::kernel<false, DP, true><<<grid, 256, 0, stream>>>(p);                       \
+    else attn::kernel<false, DP, false><<<grid, 256, 0, stream>>>(p);                               \
+    return hipGetLastError();                                                                       \
+  })
+
+}  // namespace
+
+hipError_t attn_fwd(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
+  return MT_ATTN_LAUNCH(fwd_kernel, (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
+}
+hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
+  return MT_ATTN_LAUNCH(dq_kernel, (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
+}
+hipError_t attn_bwd_dkv(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
+  return MT_ATTN_LAUNCH(dkv_kernel, (int64_t)p.B * p.HK * ((p.TK + 127) / 128));
+}
+
+}  // namespace mt

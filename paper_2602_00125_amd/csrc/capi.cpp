@@ -1,6 +1,7 @@
 // C-ABI of libminitensor_hip: argument validation, shape planning and kernel
-// dispatch (the convolution's planning lives in conv_host.cpp). Declarations
-// and their contracts: include/minitensor_hip.h.
+// dispatch (the convolution's lives in conv_host.cpp; that of attention, the
+// head norms and dropout in attention_host.cpp). Declarations and their
+// contracts: include/minitensor_hip.h.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1276,6 +1277,105 @@ mt_status mt_rmsprop_step(int32_t n, const mt_tensor* params, const mt_tensor* g
   }
 }
 
+mt_status mt_attention_fwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,
+                           const mt_tensor* q_start, const mt_tensor* o, const mt_tensor* lse, float scale,
+                           uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    return attention_fwd_impl(q, k, v, kv_len, q_start, o, lse, scale, flags, ws, ws_bytes, (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_attention_fwd_workspace(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
+                                     const mt_tensor* kv_len, const mt_tensor* q_start, const mt_tensor* o,
+                                     const mt_tensor* lse, uint32_t flags, size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return attention_fwd_impl(q, k, v, kv_len, q_start, o, lse, 1.f, flags, nullptr, 0, nullptr, bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_attention_bwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,
+                           const mt_tensor* q_start, const mt_tensor* o, const mt_tensor* lse, const mt_tensor* dout,
+                           const mt_tensor* dq, const mt_tensor* dk, const mt_tensor* dv, float scale, uint32_t flags,
+                           void* ws, size_t ws_bytes, void* stream) {
+  try {
+    return attention_bwd_impl(q, k, v, kv_len, q_start, o, lse, dout, dq, dk, dv, scale, flags, ws, ws_bytes,
+                              (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_attention_bwd_workspace(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
+                                     const mt_tensor* kv_len, const mt_tensor* q_start, const mt_tensor* o,
+                                     const mt_tensor* lse, const mt_tensor* dout, const mt_tensor* dq,
+                                     const mt_tensor* dk, const mt_tensor* dv, uint32_t flags, size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return attention_bwd_impl(q, k, v, kv_len, q_start, o, lse, dout, dq, dk, dv, 1.f, flags, nullptr, 0, nullptr, bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_qk_norm_rope_fwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq, const mt_tensor* wk,
+                              const mt_tensor* cos, const mt_tensor* sin, const mt_tensor* yq, const mt_tensor* yk,
+                              float eps, uint32_t flags, void* stream) {
+  try {
+    return qk_norm_rope_fwd_impl(q, k, wq, wk, cos, sin, yq, yk, eps, flags, (hipStream_t)stream);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_qk_norm_rope_bwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq, const mt_tensor* wk,
+                              const mt_tensor* cos, const mt_tensor* sin, const mt_tensor* dyq, const mt_tensor* dyk,
+                              const mt_tensor* dq, const mt_tensor* dk, const mt_tensor* dwq, const mt_tensor* dwk,
+                              float eps, uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    return qk_norm_rope_bwd_impl(q, k, wq, wk, cos, sin, dyq, dyk, dq, dk, dwq, dwk, eps, flags, ws, ws_bytes,
+                                 (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_qk_norm_rope_bwd_workspace(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq,
+                                        const mt_tensor* wk, const mt_tensor* cos, const mt_tensor* sin,
+                                        const mt_tensor* dyq, const mt_tensor* dyk, const mt_tensor* dq,
+                                        const mt_tensor* dk, const mt_tensor* dwq, const mt_tensor* dwk,
+                                        size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return qk_norm_rope_bwd_impl(q, k, wq, wk, cos, sin, dyq, dyk, dq, dk, dwq, dwk, 0.f, 0, nullptr, 0, nullptr,
+                                 bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_dropout_fwd(const mt_tensor* x, const mt_tensor* residual, float p, uint64_t seed, uint64_t offset,
+                         const mt_tensor* y, void* stream) {
+  try {
+    return dropout_impl(x, residual, p, seed, offset, y, 0, false, (hipStream_t)stream);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_dropout_bwd(const mt_tensor* dy, float p, uint64_t seed, uint64_t offset, const mt_tensor* dx,
+                         uint32_t flags, void* stream) {
+  try {
+    return dropout_impl(dy, nullptr, p, seed, offset, dx, flags, true, (hipStream_t)stream);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
 mt_status mt_linear_bwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy,
                         const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db,
                         uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
@@ -1505,3 +1605,8 @@ int mt_debug_set(const char* key, int64_t value) {
 }
 
 }  // extern "C"
+
+#ifndef MT_SEPARATE_UNITS
+// one object for the host code: a build that does not compile this on its own
+#include "attention_host.cpp"
+#endif

@@ -23,6 +23,8 @@ mt_status hip_status(hipError_t e);
 mt_status check_tensor(const mt_tensor* t, const char* name, int min_nd, int max_nd);
 mt_status check_vector(const mt_tensor* t, const char* name, int64_t n);
 bool overlaps(const mt_tensor* a, const mt_tensor* b);
+int64_t numel(const mt_tensor* t);
+size_t elem_size(int32_t dt);
 bool is_row_major(const mt_tensor* t);
 bool vec_ok_operand(const void* base, int64_t rows_other, int64_t contig_extent, int64_t ld,
                     const int64_t* bstrides, int nb, int per);
@@ -61,5 +63,25 @@ mt_status conv_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_tensor*
                         const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db, int32_t sh,
                         int32_t sw, int32_t ph, int32_t pw, uint32_t flags, void* ws,
                         size_t ws_bytes, hipStream_t stream, size_t* ws_query);
+
+// the bodies of attention, the head norms with rotation and dropout
+// (attention_host.cpp); ws_query as above
+mt_status attention_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,
+                             const mt_tensor* q_start, const mt_tensor* o, const mt_tensor* lse, float scale,
+                             uint32_t flags, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query);
+mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,
+                             const mt_tensor* q_start, const mt_tensor* o, const mt_tensor* lse, const mt_tensor* dout,
+                             const mt_tensor* dq, const mt_tensor* dk, const mt_tensor* dv, float scale, uint32_t flags,
+                             void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query);
+mt_status qk_norm_rope_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq, const mt_tensor* wk,
+                                const mt_tensor* cos, const mt_tensor* sin, const mt_tensor* yq, const mt_tensor* yk,
+                                float eps, uint32_t flags, hipStream_t stream);
+mt_status qk_norm_rope_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* wq, const mt_tensor* wk,
+                                const mt_tensor* cos, const mt_tensor* sin, const mt_tensor* dyq, const mt_tensor* dyk,
+                                const mt_tensor* dq, const mt_tensor* dk, const mt_tensor* dwq, const mt_tensor* dwk,
+                                float eps, uint32_t flags, void* ws, size_t ws_bytes, hipStream_t stream,
+                                size_t* ws_query);
+mt_status dropout_impl(const mt_tensor* x, const mt_tensor* residual, float p, uint64_t seed, uint64_t offset,
+                       const mt_tensor* y, uint32_t flags, bool backward, hipStream_t stream);
 
 }  // namespace mt::host

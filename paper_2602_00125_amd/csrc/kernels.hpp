@@ -163,4 +163,43 @@ hipError_t adam_step(const OptBatch& b, float lr, float beta1, float beta2, floa
                      float inv_bc1, float inv_bc2, hipStream_t stream);
 hipError_t rmsprop_step(const OptBatch& b, float lr, float alpha, float eps, hipStream_t stream);
 
+// Dropout with the residual sum (dropout.hip) over [M][N] with row pitches:
+// y = res + x keep scale, keep from the generator at (seed, offset). res may
+// be NULL, or y itself (an accumulated gradient).
+struct DropoutParams {
+  const void *x, *res;
+  void* y;
+  int64_t M, N, ldx, ldr, ldy;
+  uint64_t seed, offset;
+  uint32_t drop;  // an element stays where its 16 bits are this or more
+  float scale;
+};
+hipError_t dropout_run(const DropoutParams& p, bool x_bf16, bool y_bf16, bool vec, hipStream_t stream);
+
+// A [B, T, H, D] view: element strides of batch, token and head (D contiguous).
+struct HeadView {
+  void* p;
+  int64_t sb, st, sh;
+};
+
+// The norm of each head with the rotation (head_norm.hip).
+constexpr int kHeadNormMaxD = 1024;
+struct HeadNormParams {
+  HeadView q, k;      // x
+  HeadView yq, yk;    // forward: y; backward: dx (p == NULL: skipped)
+  HeadView dyq, dyk;  // backward
+  const float *wq, *wk, *cos, *sin;  // weights may be NULL (ones)
+  int64_t cos_sb, cos_st, sin_sb, sin_st;
+  int32_t B, T, HQ, HK, D, R;
+  int32_t interleaved, accumulate;
+  int32_t L, L_shift;  // lanes a row (a power of two)
+  float eps;
+  float* part;  // backward: [blocks][2][D] column sums of dw, or NULL
+};
+// vec: values a lane (8, 4: L lanes hold a row; 0: by element, a wave a row);
+// hpg: heads of a token that a group of lanes takes (1 or 4).
+hipError_t head_norm_fwd(const HeadNormParams& p, bool x_bf16, bool y_bf16, int vec, int hpg, hipStream_t stream);
+hipError_t head_norm_bwd(const HeadNormParams& p, bool x_bf16, bool y_bf16, int vec, int blocks, hipStream_t stream);
+hipError_t head_norm_finish(const float* part, int parts, int D, float* dwq, float* dwk, bool add, hipStream_t stream);
+
 }  // namespace mt

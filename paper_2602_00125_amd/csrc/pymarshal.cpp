@@ -4,8 +4,8 @@
 // ctypes and descriptors built in Python a call took 11 us, more than its
 // kernels. Nothing is kept between calls.
 //
-// init(handle, float32, bfloat16, describe, current_stream, stream_of): the
-// library's dlopen handle, torch's two dtypes, binding.desc (called to raise
+// init(handle, float32, bfloat16, int32, describe, current_stream, stream_of):
+// the library's dlopen handle, torch's dtypes, binding.desc (called to raise
 // its error for a tensor that is refused) and how a stream is found (none
 // given / given). Every other function returns the entry point's status.
 #define PY_SSIZE_T_CLEAN
@@ -16,7 +16,7 @@
 
 namespace {
 
-PyObject *g_f32, *g_bf16, *g_describe, *g_current, *g_stream_of;
+PyObject *g_f32, *g_bf16, *g_i32, *g_describe, *g_current, *g_stream_of;
 PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_numel, *s_element_size;
 
 struct Lib {
@@ -32,6 +32,12 @@ struct Lib {
   decltype(&mt_rmsprop_step) rmsprop_step;
   decltype(&mt_conv2d_fwd) conv2d_fwd;
   decltype(&mt_conv2d_bwd) conv2d_bwd;
+  decltype(&mt_attention_fwd) attention_fwd;
+  decltype(&mt_attention_bwd) attention_bwd;
+  decltype(&mt_qk_norm_rope_fwd) qk_norm_rope_fwd;
+  decltype(&mt_qk_norm_rope_bwd) qk_norm_rope_bwd;
+  decltype(&mt_dropout_fwd) dropout_fwd;
+  decltype(&mt_dropout_bwd) dropout_bwd;
 } L;
 
 bool as_i64(PyObject* o, int64_t* v) {
@@ -64,8 +70,9 @@ bool ints(PyObject* tuple, int64_t* out, Py_ssize_t* n) {  // consumes tuple
   return ok;
 }
 
-bool refuse(PyObject* t) {
-  PyObject* r = PyObject_CallOneArg(g_describe, t);  // raises what is wrong with it
+bool refuse(PyObject* t, bool index) {
+  // raises what is wrong with it
+  PyObject* r = PyObject_CallFunctionObjArgs(g_describe, t, index ? Py_True : Py_False, nullptr);
   if (r) {
     Py_DECREF(r);
     PyErr_SetString(PyExc_RuntimeError, "tensor cannot be described");
@@ -73,21 +80,23 @@ bool refuse(PyObject* t) {
   return false;
 }
 
-bool describe(PyObject* t, mt_tensor* d) {
+// index: a tensor of int32 lengths or positions, else one of the two dtypes.
+bool describe(PyObject* t, mt_tensor* d, bool index = false) {
   PyObject* v = PyObject_GetAttr(t, s_is_cuda);
   if (!v) return false;
   Py_DECREF(v);
-  if (v != Py_True) return refuse(t);
+  if (v != Py_True) return refuse(t, index);
   if (!(v = PyObject_GetAttr(t, s_dtype))) return false;
   Py_DECREF(v);
-  if (v == g_f32) d->dtype = MT_F32;
-  else if (v == g_bf16) d->dtype = MT_BF16;
-  else return refuse(t);
+  if (index && v == g_i32) d->dtype = MT_I32;
+  else if (!index && v == g_f32) d->dtype = MT_F32;
+  else if (!index && v == g_bf16) d->dtype = MT_BF16;
+  else return refuse(t, index);
   Py_ssize_t n, m;
   if (!ints(PyObject_GetAttr(t, s_shape), d->shape, &n)) return false;
-  if (n > MT_MAX_DIMS) return refuse(t);
+  if (n > MT_MAX_DIMS) return refuse(t, index);
   if (!ints(PyObject_CallMethodNoArgs(t, s_stride), d->stride, &m)) return false;
-  if (m != n) return refuse(t);
+  if (m != n) return refuse(t, index);
   d->ndim = (int32_t)n;
   return as_address(PyObject_CallMethodNoArgs(t, s_data_ptr), &d->data);
 }
@@ -97,7 +106,7 @@ bool describe(PyObject* t, mt_tensor* d) {
 struct Args {
   PyObject* const* a;
   bool ok = true;
-  mt_tensor d[6];
+  mt_tensor d[12];
   int used = 0;
   Args(PyObject* const* args, Py_ssize_t n, Py_ssize_t want) : a(args) {
     if (n != want) {
@@ -105,11 +114,17 @@ struct Args {
       ok = false;
     }
   }
-  const mt_tensor* tensor(int i) {
+  const mt_tensor* tensor(int i, bool index = false) {
     if (!ok || a[i] == Py_None) return nullptr;
     mt_tensor* t = &d[used++];
-    ok = describe(a[i], t);
+    ok = describe(a[i], t, index);
     return t;
+  }
+  uint64_t u64(int i) {
+    if (!ok) return 0;
+    const unsigned long long v = PyLong_AsUnsignedLongLong(a[i]);
+    ok = v != (unsigned long long)-1 || !PyErr_Occurred();
+    return v;
   }
   int64_t i64(int i) {
     int64_t v = 0;
@@ -239,6 +254,71 @@ FN(conv2d_bwd) {  // x, w, dy, dx, dw, db, sh, sw, ph, pw, flags, ws, stream
   return call(g.ok, [&] { return L.conv2d_bwd(x, w, dy, dx, dw, db, v[0], v[1], v[2], v[3], flags, ws.p, ws.n, st); });
 }
 
+FN(attention_fwd) {  // q, k, v, kv_len, q_start, o, lse, scale, flags, ws, stream
+  Args g(a, n, 11);
+  const mt_tensor *q = g.tensor(0), *k = g.tensor(1), *v = g.tensor(2), *len = g.tensor(3, true),
+                  *start = g.tensor(4, true), *o = g.tensor(5), *lse = g.tensor(6);
+  const float scale = g.f32(7);
+  const uint32_t flags = (uint32_t)g.i64(8);
+  const Args::Ws ws = g.ws(9);
+  void* st = g.stream(10);
+  return call(g.ok, [&] { return L.attention_fwd(q, k, v, len, start, o, lse, scale, flags, ws.p, ws.n, st); });
+}
+FN(attention_bwd) {  // q, k, v, kv_len, q_start, o, lse, dout, dq, dk, dv, scale, flags, ws, stream
+  Args g(a, n, 15);
+  const mt_tensor *q = g.tensor(0), *k = g.tensor(1), *v = g.tensor(2), *len = g.tensor(3, true),
+                  *start = g.tensor(4, true), *o = g.tensor(5), *lse = g.tensor(6), *dout = g.tensor(7),
+                  *dq = g.tensor(8), *dk = g.tensor(9), *dv = g.tensor(10);
+  const float scale = g.f32(11);
+  const uint32_t flags = (uint32_t)g.i64(12);
+  const Args::Ws ws = g.ws(13);
+  void* st = g.stream(14);
+  return call(g.ok, [&] {
+    return L.attention_bwd(q, k, v, len, start, o, lse, dout, dq, dk, dv, scale, flags, ws.p, ws.n, st);
+  });
+}
+FN(qk_norm_rope_fwd) {  // q, k, wq, wk, cos, sin, yq, yk, eps, flags, stream
+  Args g(a, n, 11);
+  const mt_tensor* t[8];
+  for (int i = 0; i < 8; ++i) t[i] = g.tensor(i);
+  const float eps = g.f32(8);
+  const uint32_t flags = (uint32_t)g.i64(9);
+  void* st = g.stream(10);
+  return call(g.ok, [&] { return L.qk_norm_rope_fwd(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], eps, flags, st); });
+}
+FN(qk_norm_rope_bwd) {  // q, k, wq, wk, cos, sin, dyq, dyk, dq, dk, dwq, dwk, eps, flags, ws, stream
+  Args g(a, n, 16);
+  const mt_tensor* t[12];
+  for (int i = 0; i < 12; ++i) t[i] = g.tensor(i);
+  const float eps = g.f32(12);
+  const uint32_t flags = (uint32_t)g.i64(13);
+  const Args::Ws ws = g.ws(14);
+  void* st = g.stream(15);
+  return call(g.ok, [&] {
+    return L.qk_norm_rope_bwd(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], t[8], t[9], t[10], t[11], eps, flags,
+                              ws.p, ws.n, st);
+  });
+}
+FN(dropout_fwd) {  // x, residual, p, seed, offset, y, stream
+  Args g(a, n, 7);
+  const mt_tensor *x = g.tensor(0), *r = g.tensor(1);
+  const float p = g.f32(2);
+  const uint64_t seed = g.u64(3), offset = g.u64(4);
+  const mt_tensor* y = g.tensor(5);
+  void* st = g.stream(6);
+  return call(g.ok, [&] { return L.dropout_fwd(x, r, p, seed, offset, y, st); });
+}
+FN(dropout_bwd) {  // dy, p, seed, offset, dx, flags, stream
+  Args g(a, n, 7);
+  const mt_tensor* dy = g.tensor(0);
+  const float p = g.f32(1);
+  const uint64_t seed = g.u64(2), offset = g.u64(3);
+  const mt_tensor* dx = g.tensor(4);
+  const uint32_t flags = (uint32_t)g.i64(5);
+  void* st = g.stream(6);
+  return call(g.ok, [&] { return L.dropout_bwd(dy, p, seed, offset, dx, flags, st); });
+}
+
 // Descriptors of up to four lists of n tensors each, one list after another.
 // The lists' tensors are held until the call has returned: it runs without
 // the interpreter's lock, while another thread may change a list, and an
@@ -303,8 +383,8 @@ FN(rmsprop_step) {  // params, grads, sq_avg, lr, alpha, eps, stream
 }
 
 FN(init) {
-  if (n != 6) {
-    PyErr_SetString(PyExc_TypeError, "init(handle, float32, bfloat16, describe, current_stream, stream_of)");
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "init(handle, float32, bfloat16, int32, describe, current_stream, stream_of)");
     return nullptr;
   }
   void* h = PyLong_AsVoidPtr(a[0]);
@@ -319,9 +399,11 @@ FN(init) {
   }
   SYM(linear_fwd) SYM(linear_act_fwd) SYM(linear_bwd) SYM(matmul) SYM(reduce_broadcast_grad) SYM(act_bwd)
   SYM(mse_loss) SYM(sgd_step) SYM(adam_step) SYM(rmsprop_step) SYM(conv2d_fwd) SYM(conv2d_bwd)
+  SYM(attention_fwd) SYM(attention_bwd) SYM(qk_norm_rope_fwd) SYM(qk_norm_rope_bwd) SYM(dropout_fwd)
+  SYM(dropout_bwd)
 #undef SYM
-  PyObject** to[] = {&g_f32, &g_bf16, &g_describe, &g_current, &g_stream_of};
-  for (int i = 0; i < 5; ++i) {
+  PyObject** to[] = {&g_f32, &g_bf16, &g_i32, &g_describe, &g_current, &g_stream_of};
+  for (int i = 0; i < 6; ++i) {
     Py_INCREF(a[i + 1]);
     Py_XSETREF(*to[i], a[i + 1]);
   }
@@ -332,6 +414,8 @@ FN(init) {
 PyMethodDef methods[] = {METHOD(init), METHOD(linear_fwd), METHOD(linear_act_fwd), METHOD(linear_bwd), METHOD(matmul),
                          METHOD(reduce_broadcast_grad), METHOD(act_bwd), METHOD(mse_loss), METHOD(sgd_step),
                          METHOD(adam_step), METHOD(rmsprop_step), METHOD(conv2d_fwd), METHOD(conv2d_bwd),
+                         METHOD(attention_fwd), METHOD(attention_bwd), METHOD(qk_norm_rope_fwd),
+                         METHOD(qk_norm_rope_bwd), METHOD(dropout_fwd), METHOD(dropout_bwd),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the binding", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
