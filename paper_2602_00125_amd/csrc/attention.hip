@@ -381,18 +381,15 @@ __device__ __forceinline__ char* row_of(const HeadView& v, int b, int64_t t, int
 template <int DP>
 struct Softmax {
   float m = -kInf, l = 0.f;  // maximum (log2 units; may lag) and this half's sum
-  // S (scaled by c in here) of N x 32 stream keys becomes P, masked where
-  // key >= lim; acc is rescaled when the maximum has grown enough.
-  template <int N, bool MASK>
-  __device__ __forceinline__ void step(f32x16 (&S)[N], float c, int lim, f32x16 (&acc)[DP / 32]) {
+  // S (scaled by c in here) of N x 32 stream keys becomes P; acc is rescaled
+  // when the maximum has grown enough.
+  template <int N>
+  __device__ __forceinline__ void step(f32x16 (&S)[N], float c, f32x16 (&acc)[DP / 32]) {
     float t = -kInf;
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (MASK && 32 * n + 16 * (i >> 3) + (i & 7) >= lim) S[n][i] = -kInf;
-        t = fmaxf(t, S[n][i]);
-      }
+      for (int i = 0; i < 16; ++i) t = fmaxf(t, S[n][i]);
     t = max_halves(t) * c;
     // The result is the same for any m that keeps the terms in range, so m
     // follows the maximum only once it lags by 2^8.
@@ -463,8 +460,15 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(const AttnParams p) {
     f32x16 S[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) S[n] = dot<BF, DP>(K, 32 * n, q, lane);
-    if (k0 + BK > wmin) sm.template step<N, true>(S, p.scale_log2, lim - k0 - 8 * (lane >> 5), acc);
-    else sm.template step<N, false>(S, p.scale_log2, 0, acc);
+    if (k0 + BK > wmin) {  // keys that some of the wave's queries do not see
+      const int lm = lim - k0 - 8 * (lane >> 5);
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * n + 16 * (i >> 3) + (i & 7) >= lm) S[n][i] = -kInf;
+    }
+    sm.step(S, p.scale_log2, acc);
 #pragma unroll
     for (int n = 0; n < N; ++n) accum<BF, DP>(V, 32 * n, S[n], acc, lane);
   }
@@ -520,25 +524,27 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
   const float lse2 = ok ? p.lse[stat] * kLog2e : 0.f;
 
   f32x16 acc[T::ND] = {};
-  auto tile = [&](auto masked, const char* K, const char* V, int lm) {
+  for (int k0 = 0, buf = 0; k0 < kend; k0 += BK, buf ^= 1) {
+    wait_all_barrier();
+    if (k0 + BK < kend) fetch(k0 + BK, buf ^ 1);
+    if (k0 >= wmax) continue;
+    const char *K = lds[buf][0], *V = lds[buf][1];
+    const bool edge = k0 + BK > wmin;  // keys that some of the wave's queries do not see
+    const int lm = lim - k0 - 8 * (lane >> 5);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       f32x16 S = dot<BF, DP>(K, 32 * n, q, lane);
       const f32x16 dP = dot<BF, DP>(V, 32 * n, go, lane);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float pr = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse2)) * (dP[i] - delta);
-        S[i] = masked && 32 * n + 16 * (i >> 3) + (i & 7) >= lm ? 0.f : pr;
+      for (int i = 0; i < 16; ++i)
+        S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse2)) * (dP[i] - delta);
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * n + 16 * (i >> 3) + (i & 7) >= lm) S[i] = 0.f;
       }
       accum<BF, DP>(K, 32 * n, S, acc, lane);
     }
-  };
-  for (int k0 = 0, buf = 0; k0 < kend; k0 += BK, buf ^= 1) {
-    wait_all_barrier();
-    if (k0 + BK < kend) fetch(k0 + BK, buf ^ 1);
-    if (k0 >= wmax) continue;
-    if (k0 + BK > wmin) tile(std::true_type{}, lds[buf][0], lds[buf][1], lim - k0 - 8 * (lane >> 5));
-    else tile(std::false_type{}, lds[buf][0], lds[buf][1], 0);
   }
   store_rows<BF, DP, VEC>(row_of(p.dq, b, qrow, hq, T::ES), ok, p.D, acc, p.scale, p.accumulate, lane);
 }
@@ -546,7 +552,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
 // dk and dv: a block holds 128 keys of one head and walks the queries that see
 // them, over all query heads of the group.
 template <bool BF, int DP, bool VEC>
-__global__ __launch_bounds__(256, 2) void dkv_kernel(const AttnParams p) {
+__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void dkv_kernel(const AttnParams p) {
   using T = Tile<BF, DP>;
   constexpr int BQ = BF ? 64 : 32, N = BQ / 32, BYTES = BQ * T::RB;
   __shared__ __align__(1024) char lds[2][2][BYTES];
@@ -594,31 +600,32 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(const AttnParams p) {
   k.template load<VEC>(row_of(p.k, b, krow, hk, T::ES), ok, p.D, lane);
   v.template load<VEC>(row_of(p.v, b, krow, hk, T::ES), ok, p.D, lane);
   f32x16 ak[T::ND] = {}, av[T::ND] = {};
-  // from: of the 64 queries, the lane's key is seen by those from this one on
-  auto tile = [&](auto masked, const char* Q, const char* O, const float (&st)[2][64], int from) {
-    const int h8 = 8 * (lane >> 5);
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      f32x16 S = dot<BF, DP>(Q, 32 * n, k, lane);
-      f32x16 dP = dot<BF, DP>(O, 32 * n, v, lane);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = 32 * n + 16 * (i >> 3) + (i & 7);
-        const float e = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -st[0][r + h8] * kLog2e));
-        S[i] = masked && r < from ? 0.f : e;
-        dP[i] = S[i] * (dP[i] - st[1][r + h8]);
-      }
-      accum<BF, DP>(O, 32 * n, S, av, lane);
-      accum<BF, DP>(Q, 32 * n, dP, ak, lane);
-    }
-  };
   for (int it = 0, buf = 0; it < iters; ++it, buf ^= 1) {
     wait_all_barrier();
     if (it + 1 < iters) fetch(it + 1, buf ^ 1);
     const int t0 = q_first + it % tiles * BQ;
     if (!wave_on || t0 + BQ <= wfirst) continue;
-    if (t0 < wall) tile(std::true_type{}, lds[buf][0], lds[buf][1], stats[buf], see_i - t0 - 8 * (lane >> 5));
-    else tile(std::false_type{}, lds[buf][0], lds[buf][1], stats[buf], 0);
+    const char *Q = lds[buf][0], *O = lds[buf][1];
+    const float *lse = stats[buf][0] + 8 * (lane >> 5), *delta = stats[buf][1] + 8 * (lane >> 5);
+    const bool edge = t0 < wall;  // queries that do not see some of the wave's keys
+    const int from = see_i - t0 - 8 * (lane >> 5);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      f32x16 S = dot<BF, DP>(Q, 32 * n, k, lane);
+      f32x16 dP = dot<BF, DP>(O, 32 * n, v, lane);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse[32 * n + 16 * (i >> 3) + (i & 7)] * kLog2e));
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * n + 16 * (i >> 3) + (i & 7) < from) S[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dP[i] = S[i] * (dP[i] - delta[32 * n + 16 * (i >> 3) + (i & 7)]);
+      accum<BF, DP>(O, 32 * n, S, av, lane);
+      accum<BF, DP>(Q, 32 * n, dP, ak, lane);
+    }
   }
   // keys past the batch element's length take no part: zero
   if (p.dk.p)
