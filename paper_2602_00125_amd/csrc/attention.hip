@@ -114,11 +114,12 @@ struct Tile {
   }
 };
 
-// What a wave multiplies tiles with: 32 own tokens, one a lane.
+// What a wave multiplies tiles with: 32 own tokens, one a lane, in registers
 template <bool BF, int DP>
 struct Own {
   using T = Tile<BF, DP>;
   u32x4 f[T::NF];
+  __device__ __forceinline__ u32x4 frag(int s) const { return f[s]; }
   // row: the lane's token in global memory (not read unless ok)
   template <bool VEC>
   __device__ __forceinline__ void load(const char* row, bool ok, int D, int lane) {
@@ -162,9 +163,24 @@ struct Own {
   }
 };
 
-// C[r][n] = sum_d tile[r0 + r][d] own[n][d], r in 0..31 (r0 a multiple of 32).
+// or as rows of a tile in LDS (from row n0 of it, a multiple of 32).
 template <bool BF, int DP>
-__device__ __forceinline__ f32x16 dot(const char* S, int r0, const Own<BF, DP>& own, int lane) {
+struct OwnTile {
+  using T = Tile<BF, DP>;
+  const char* row;
+  int h, x;
+  __device__ __forceinline__ OwnTile(const char* tile, int n0, int lane) {
+    const int r = lane & 31;
+    row = tile + (n0 + r) * T::RB;
+    h = lane >> 5;
+    x = T::swz(r);
+  }
+  __device__ __forceinline__ u32x4 frag(int s) const { return *(const u32x4*)(row + (((2 * s + h) ^ x) * 16)); }
+};
+
+// C[r][n] = sum_d tile[r0 + r][d] own[n][d], r in 0..31 (r0 a multiple of 32).
+template <bool BF, int DP, typename O>
+__device__ __forceinline__ f32x16 dot(const char* S, int r0, const O& own, int lane) {
   using T = Tile<BF, DP>;
   const int r = tile_row(lane), h = lane >> 5;
   const char* row = S + (r0 + r) * T::RB;
@@ -172,15 +188,13 @@ __device__ __forceinline__ f32x16 dot(const char* S, int r0, const Own<BF, DP>& 
   f32x16 c = {};
 #pragma unroll
   for (int s = 0; s < T::NF; ++s) {
-    const u32x4 a = *(const u32x4*)(row + (((2 * s + h) ^ x) * 16));
+    const u32x4 a = *(const u32x4*)(row + (((2 * s + h) ^ x) * 16)), b = own.frag(s);
     if constexpr (BF) {
-      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, own.f[s]), c,
-                                                  0, 0, 0);
+      c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(own.f[s][e]), c,
-                                                 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
     }
   }
   return c;
@@ -291,10 +305,10 @@ struct Loader {
   }
 };
 
-// Result rows: acc[d][n] x mul to token n's row (not written unless ok).
+// Result rows: acc[d][n] x mul (or zero) to token n's row (not written unless ok).
 template <bool BF, int DP, bool VEC>
-__device__ __forceinline__ void store_rows(char* row, bool ok, int D, const f32x16 (&acc)[DP / 32], float mul, bool add,
-                                           int lane) {
+__device__ __forceinline__ void store_rows(char* row, bool ok, int D, const f32x16 (&acc)[DP / 32], float mul, bool zero,
+                                           bool add, int lane) {
   if (!ok) return;
   const int h = lane >> 5;
 #pragma unroll
@@ -304,7 +318,7 @@ __device__ __forceinline__ void store_rows(char* row, bool ok, int D, const f32x
       const int d = 32 * db + 16 * kk + 8 * h;
       float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = acc[db][8 * kk + e] * mul;
+      for (int e = 0; e < 8; ++e) v[e] = zero ? 0.f : acc[db][8 * kk + e] * mul;
       if constexpr (VEC && BF) {
         if (d < D) {
           u32x4* dst = (u32x4*)(row + d * 2);
@@ -434,9 +448,9 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(const AttnParams p) {
   const int lim = ok ? visible(p, sp, qi) : 0;
   const int last = qb * 128 + 127 < p.TQ ? qb * 128 + 127 : p.TQ - 1;
   const int kend = visible(p, sp, last);  // of the whole block
-  // of this wave: no key past wmax is seen, every key before wmin by all
+  const int kall = visible(p, sp, qb * 128) / BK * BK;  // tiles that all its queries see whole
   const int wlast = q0 + 31 < p.TQ ? q0 + 31 : p.TQ - 1;
-  const int wmax = q0 < p.TQ ? visible(p, sp, wlast) : 0, wmin = q0 < p.TQ ? visible(p, sp, q0) : 0;
+  const int wmax = q0 < p.TQ ? visible(p, sp, wlast) : 0;  // of this wave
 
   Own<BF, DP> q;
   q.template load<VEC>(row_of(p.q, b, ok ? qi : 0, hq, T::ES), ok, p.D, lane);
@@ -451,16 +465,14 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(const AttnParams p) {
   };
   f32x16 acc[T::ND] = {};
   Softmax<DP> sm;
-  if (kend > 0) fetch(0, 0);
-  for (int k0 = 0, buf = 0; k0 < kend; k0 += BK, buf ^= 1) {
+  auto tile = [&](auto masked, int k0, int buf) {
     wait_all_barrier();
     if (k0 + BK < kend) fetch(k0 + BK, buf ^ 1);
-    if (k0 >= wmax) continue;
-    const char *K = lds[buf][0], *V = lds[buf][1];
+    if (masked && k0 >= wmax) return;
     f32x16 S[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) S[n] = dot<BF, DP>(K, 32 * n, q, lane);
-    if (k0 + BK > wmin) {  // keys that some of the wave's queries do not see
+    for (int n = 0; n < N; ++n) S[n] = dot<BF, DP>(lds[buf][0], 32 * n, q, lane);
+    if constexpr (masked) {
       const int lm = lim - k0 - 8 * (lane >> 5);
 #pragma unroll
       for (int n = 0; n < N; ++n)
@@ -470,12 +482,16 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(const AttnParams p) {
     }
     sm.step(S, p.scale_log2, acc);
 #pragma unroll
-    for (int n = 0; n < N; ++n) accum<BF, DP>(V, 32 * n, S[n], acc, lane);
-  }
+    for (int n = 0; n < N; ++n) accum<BF, DP>(lds[buf][1], 32 * n, S[n], acc, lane);
+  };
+  int k0 = 0, buf = 0;
+  if (kend > 0) fetch(0, 0);
+  for (; k0 < kall; k0 += BK, buf ^= 1) tile(std::false_type{}, k0, buf);
+  for (; k0 < kend; k0 += BK, buf ^= 1) tile(std::true_type{}, k0, buf);
   const float l = sum_halves(sm.l);
-  store_rows<BF, DP, VEC>(row_of(p.o, b, ok ? qi : 0, hq, T::ES), ok, p.D, acc, l > 0.f ? 1.f / l : 0.f, false, lane);
+  store_rows<BF, DP, VEC>(row_of(p.o, b, ok ? qi : 0, hq, T::ES), ok, p.D, acc, 1.f / l, l == 0.f, false, lane);
   if (p.lse && ok && lane < 32)
-    p.lse[((int64_t)b * p.HQ + hq) * p.TQ + qi] = l > 0.f ? (sm.m + __builtin_amdgcn_logf(l)) * kLn2 : (l == l ? -kInf : l);
+    p.lse[((int64_t)b * p.HQ + hq) * p.TQ + qi] = l == 0.f ? -kInf : (sm.m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // --------------------------------------------------------------- backward
@@ -497,9 +513,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
   const bool ok = qi < p.TQ;
   const int lim = ok ? visible(p, sp, qi) : 0;
   const int last = qb * 128 + 127 < p.TQ ? qb * 128 + 127 : p.TQ - 1;
-  const int kend = p.with_dq ? visible(p, sp, last) : 0;
+  const int kend = p.with_dq ? visible(p, sp, last) : 0, kall = visible(p, sp, qb * 128) / BK * BK;
   const int wlast = q0 + 31 < p.TQ ? q0 + 31 : p.TQ - 1;
-  const int wmax = q0 < p.TQ ? visible(p, sp, wlast) : 0, wmin = q0 < p.TQ ? visible(p, sp, q0) : 0;
+  const int wmax = q0 < p.TQ ? visible(p, sp, wlast) : 0;
 
   Loader<BF, DP, BK, 4, VEC> lk, lv;
   lk.init(wave, lane, p.k.st, p.D);
@@ -524,50 +540,63 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
   const float lse2 = ok ? p.lse[stat] * kLog2e : 0.f;
 
   f32x16 acc[T::ND] = {};
-  for (int k0 = 0, buf = 0; k0 < kend; k0 += BK, buf ^= 1) {
+  auto tile = [&](auto masked, int k0, int buf) {
     wait_all_barrier();
     if (k0 + BK < kend) fetch(k0 + BK, buf ^ 1);
-    if (k0 >= wmax) continue;
+    if (masked && k0 >= wmax) return;
     const char *K = lds[buf][0], *V = lds[buf][1];
-    const bool edge = k0 + BK > wmin;  // keys that some of the wave's queries do not see
-    const int lm = lim - k0 - 8 * (lane >> 5);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       f32x16 S = dot<BF, DP>(K, 32 * n, q, lane);
       const f32x16 dP = dot<BF, DP>(V, 32 * n, go, lane);
+      const int lm = lim - k0 - 8 * (lane >> 5);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
+      for (int i = 0; i < 16; ++i) {
         S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse2)) * (dP[i] - delta);
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * n + 16 * (i >> 3) + (i & 7) >= lm) S[i] = 0.f;
+        if (masked && 32 * n + 16 * (i >> 3) + (i & 7) >= lm) S[i] = 0.f;
       }
       accum<BF, DP>(K, 32 * n, S, acc, lane);
     }
-  }
-  store_rows<BF, DP, VEC>(row_of(p.dq, b, qrow, hq, T::ES), ok, p.D, acc, p.scale, p.accumulate, lane);
+  };
+  int k0 = 0, buf = 0;
+  for (; k0 < kall; k0 += BK, buf ^= 1) tile(std::false_type{}, k0, buf);
+  for (; k0 < kend; k0 += BK, buf ^= 1) tile(std::true_type{}, k0, buf);
+  store_rows<BF, DP, VEC>(row_of(p.dq, b, qrow, hq, T::ES), ok, p.D, acc, p.scale, false, p.accumulate, lane);
 }
 
 // dk and dv: a block holds 128 keys of one head and walks the queries that see
-// them, over all query heads of the group.
+// them, over all query heads of the group. Two accumulators leave no room for
+// both keys and values of wide bf16 heads in the registers of two waves a
+// SIMD, and with one wave the matrix cores wait for LDS (measured on 4 x 4096
+// x 32 heads of 128: 1.8 ms against 1.5): the values stay in LDS there.
 template <bool BF, int DP, bool VEC>
-__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void dkv_kernel(const AttnParams p) {
+__global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const AttnParams p) {
   using T = Tile<BF, DP>;
-  constexpr int BQ = BF ? 64 : 32, N = BQ / 32, BYTES = BQ * T::RB;
+  constexpr bool VLDS = BF && DP > 64;
+  constexpr int BQ = BF && !VLDS ? 64 : 32, N = BQ / 32, BYTES = BQ * T::RB;
   __shared__ __align__(1024) char lds[2][2][BYTES];
+  __shared__ __align__(1024) char vlds[VLDS ? 128 * T::RB : 16];
   __shared__ __align__(256) float stats[2][2][64];  // lse, delta of the tile's queries
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nkb = (p.TK + 127) >> 7;
-  const int w = work_item(p.B * p.HK * nkb);
-  if (w < 0) return;
-  const int kb = w % nkb, bh = w / nkb, hk = bh % p.HK, b = bh / p.HK;
+  // the blocks that see most queries first, over all heads of an XCD
+  const int heads = p.B * p.HK, per = heads >> 3;
+  int kb, bh;
+  if (heads & 7) {
+    if ((int)blockIdx.x >= heads * nkb) return;
+    kb = blockIdx.x / heads;
+    bh = blockIdx.x - kb * heads;
+  } else {
+    kb = (blockIdx.x >> 3) / per;
+    bh = (blockIdx.x & 7) * per + ((blockIdx.x >> 3) - kb * per);
+  }
+  const int hk = bh % p.HK, b = bh / p.HK;
   const Span sp = span_of(p, b);
   const int k0 = kb * 128 + wave * 32, kj = k0 + (lane & 31);
   const bool in = kj < p.TK, ok = kj < sp.len;
   const int krow = in ? kj : 0;
-  // query tiles from the first that sees a key of the block; per wave, no
-  // query before wfirst sees a key, every query from wall on sees all
+  // query tiles from the first that sees a key of the block; from q_all on
+  // every query sees all of them, before wfirst none sees a key of the wave
   const bool any = kb * 128 < sp.len;
   auto first_for = [&](int key) {
     const int64_t i = p.causal ? (int64_t)key - sp.start : 0;
@@ -575,7 +604,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void dkv_kernel(const AttnPa
   };
   const int q_first = any ? first_for(kb * 128) / BQ * BQ : p.TQ;
   const int tiles = (p.TQ - q_first + BQ - 1) / BQ;
-  const int wfirst = first_for(k0), wall = first_for(k0 + 31);
+  const int q_all = first_for(kb * 128 + 127), wfirst = first_for(k0);
   const bool wave_on = k0 < sp.len;
   const int64_t see = p.causal ? (int64_t)kj - sp.start : 0;  // queries from here on see the lane's key
   const int see_i = see < 0 ? 0 : see < p.TQ ? (int)see : p.TQ;
@@ -584,7 +613,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void dkv_kernel(const AttnPa
   lq.init(wave, lane, p.q.st, p.D);
   lo.init(wave, lane, p.dout.st, p.D);
   auto fetch = [&](int it, int buf) {
-    const int hq = hk * p.G + it / tiles, t0 = q_first + it % tiles * BQ;
+    const int hq = hk * p.G + it / tiles, t0 = q_first + (tiles - 1 - it % tiles) * BQ;
     lq.load(row_of(p.q, b, t0, hq, T::ES), p.TQ - t0, lds[buf][0]);
     lo.load(row_of(p.dout, b, t0, hq, T::ES), p.TQ - t0, lds[buf][1]);
     if (wave < 2) {  // a 4-byte statistic a lane
@@ -596,43 +625,59 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void dkv_kernel(const AttnPa
   };
   const int iters = tiles * p.G;
   if (iters > 0) fetch(0, 0);
-  Own<BF, DP> k, v;
+  Own<BF, DP> k;
   k.template load<VEC>(row_of(p.k, b, krow, hk, T::ES), ok, p.D, lane);
-  v.template load<VEC>(row_of(p.v, b, krow, hk, T::ES), ok, p.D, lane);
+  const auto v = [&] {
+    if constexpr (VLDS) {
+      Loader<BF, DP, 128, 4, VEC> l;
+      l.init(wave, lane, p.v.st, p.D);
+      if (iters > 0) l.load(row_of(p.v, b, kb * 128, hk, T::ES), sp.len - kb * 128, vlds);
+      return OwnTile<BF, DP>(vlds, 32 * wave, lane);
+    } else {
+      Own<BF, DP> o;
+      o.template load<VEC>(row_of(p.v, b, krow, hk, T::ES), ok, p.D, lane);
+      return o;
+    }
+  }();
   f32x16 ak[T::ND] = {}, av[T::ND] = {};
-  for (int it = 0, buf = 0; it < iters; ++it, buf ^= 1) {
+  int it = 0, buf = 0;
+  auto tile = [&](auto masked, int t0) {
     wait_all_barrier();
     if (it + 1 < iters) fetch(it + 1, buf ^ 1);
-    const int t0 = q_first + it % tiles * BQ;
-    if (!wave_on || t0 + BQ <= wfirst) continue;
     const char *Q = lds[buf][0], *O = lds[buf][1];
     const float *lse = stats[buf][0] + 8 * (lane >> 5), *delta = stats[buf][1] + 8 * (lane >> 5);
-    const bool edge = t0 < wall;  // queries that do not see some of the wave's keys
+    ++it;
+    buf ^= 1;
+    if (!wave_on || (masked && t0 + BQ <= wfirst)) return;
     const int from = see_i - t0 - 8 * (lane >> 5);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       f32x16 S = dot<BF, DP>(Q, 32 * n, k, lane);
       f32x16 dP = dot<BF, DP>(O, 32 * n, v, lane);
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse[32 * n + 16 * (i >> 3) + (i & 7)] * kLog2e));
-      if (edge) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (32 * n + 16 * (i >> 3) + (i & 7) < from) S[i] = 0.f;
+      for (int i = 0; i < 16; ++i) {
+        const int r = 16 * (i >> 3) + (i & 7) + 32 * n;
+        S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse[r] * kLog2e));
+        if (masked && r < from) S[i] = 0.f;
+        dP[i] = S[i] * (dP[i] - delta[r]);
       }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) dP[i] = S[i] * (dP[i] - delta[32 * n + 16 * (i >> 3) + (i & 7)]);
       accum<BF, DP>(O, 32 * n, S, av, lane);
       accum<BF, DP>(Q, 32 * n, dP, ak, lane);
     }
+  };
+  // from the last query on, so that the blocks of a head read the same tiles at
+  // a time whatever their first query is
+  for (int g = 0; g < p.G && iters > 0; ++g) {
+    int t0 = q_first + (tiles - 1) * BQ;
+    for (; t0 >= q_first && t0 >= q_all; t0 -= BQ) tile(std::false_type{}, t0);
+    for (; t0 >= q_first; t0 -= BQ) tile(std::true_type{}, t0);
   }
   // keys past the batch element's length take no part: zero
   if (p.dk.p)
-    store_rows<BF, DP, VEC>(row_of(p.dk, b, krow, hk, T::ES), in && (ok || !p.accumulate), p.D, ak, ok ? p.scale : 0.f,
+    store_rows<BF, DP, VEC>(row_of(p.dk, b, krow, hk, T::ES), in && (ok || !p.accumulate), p.D, ak, p.scale, !ok,
                             p.accumulate, lane);
   if (p.dv.p)
-    store_rows<BF, DP, VEC>(row_of(p.dv, b, krow, hk, T::ES), in && (ok || !p.accumulate), p.D, av, ok ? 1.f : 0.f,
+    store_rows<BF, DP, VEC>(row_of(p.dv, b, krow, hk, T::ES), in && (ok || !p.accumulate), p.D, av, 1.f, !ok,
                             p.accumulate, lane);
 }
 
