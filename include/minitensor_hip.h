@@ -536,7 +536,9 @@ mt_status mt_matmul_shape(int32_t na, const int64_t* a, int32_t nb, const int64_
  * last round of blocks would be ragged, 2 always), "sk_blocks" (0..65535
  * stream-K blocks, 0 = one per CU), "phase_grid" (strided input gradient:
  * 0 a launch per sub-pixel phase, 1 = the default: one grid when large,
- * 2 always one grid). Results stay within the documented accuracy for
+ * 2 always one grid); "attn_splits" (forward attention: -1 = the default,
+ * automatic; 0 = blocks of 128 queries; 1..64 = 32 queries a block and so many
+ * shares of the keys). Results stay within the documented accuracy for
  * every setting. */
 int mt_debug_set(const char* key, int64_t value);
 

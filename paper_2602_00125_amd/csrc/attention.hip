@@ -494,6 +494,211 @@ __global__ __launch_bounds__(256, 2) void fwd_kernel(const AttnParams p) {
     p.lse[((int64_t)b * p.HQ + hq) * p.TQ + qi] = l == 0.f ? -kInf : (sm.m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Few queries against many keys (a token of each sequence against its cache;
+// short chunks): too few blocks of 128 queries to fill the chip, and the keys'
+// bytes are what counts. The queries of all heads of a key head are columns
+// side by side, 32 to a block, so that each key is read once for all of them;
+// the keys are shared by `splits` blocks and within a block by its waves, each
+// with LDS buffers of its own and no barrier between them: a wave's next tile
+// is in flight while it works on one. The waves' results are joined in LDS,
+// the blocks' by join_kernel, in order.
+template <bool BF, int DP>
+struct SplitGeom {
+  static constexpr int HALF = 32 * Tile<BF, DP>::RB;  // 32 keys, or their values
+  // Two tiles in flight where they fit; wide fp32 heads work long enough on
+  // either half of one to load the other meanwhile.
+  static constexpr int NBUF = HALF > 8192 ? 1 : 2;
+  static constexpr int NW = 4;
+  static constexpr int PITCH = DP + 4;  // floats a column in the join
+};
+template <bool BF, int DP, bool VEC>
+__global__ __launch_bounds__(256, 1) void split_kernel(const AttnParams p) {
+  using T = Tile<BF, DP>;
+  using Gm = SplitGeom<BF, DP>;
+  constexpr int NW = Gm::NW, NBUF = Gm::NBUF;
+  constexpr int LOADS = VEC ? Loader<BF, DP, 32, 1, VEC>::JB : 0;  // in flight from fetching half a tile
+  __shared__ __align__(1024) char lds[NW][NBUF][2][Gm::HALF];
+  __shared__ float stat[2][NW][32];
+  static_assert(NW * 32 * Gm::PITCH * 4 <= (int)sizeof(lds), "the join fits the tiles' LDS");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cols = p.G * p.TQ, ncb = (cols + 31) >> 5;
+  // the blocks of one head on one XCD
+  const int w = work_item(p.B * p.HK * ncb * p.splits);
+  if (w < 0) return;
+  const int split = w % p.splits, cb = w / p.splits % ncb, bh = w / p.splits / ncb;
+  const int hk = bh % p.HK, b = bh / p.HK;
+  const Span sp = span_of(p, b);
+  const int c = cb * 32 + (lane & 31);
+  const bool ok = c < cols;
+  const int g = ok ? c / p.TQ : 0, qi = ok ? c - g * p.TQ : 0, hq = hk * p.G + g;
+  const int lim = ok ? visible(p, sp, qi) : 0;
+  int kend = lim;  // of any column
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int x = __shfl_xor(kend, o, 64);
+    kend = x > kend ? x : kend;
+  }
+  // this block's share of the tiles, an equal number a split
+  const int tiles = (kend + 31) >> 5, t_end = (int)((int64_t)tiles * (split + 1) / p.splits);
+  const int t_first = __builtin_amdgcn_readfirstlane((int)((int64_t)tiles * split / p.splits) + wave);
+  const int t_last = __builtin_amdgcn_readfirstlane(t_end);
+
+  Own<BF, DP> q;
+  q.template load<VEC>(row_of(p.q, b, qi, hq, T::ES), ok, p.D, lane);
+  Loader<BF, DP, 32, 1, VEC> lk, lv;
+  lk.init(0, lane, p.k.st, p.D);
+  lv.init(0, lane, p.v.st, p.D);
+  const char* kbase = row_of(p.k, b, 0, hk, T::ES);
+  const char* vbase = row_of(p.v, b, 0, hk, T::ES);
+  auto fetch_k = [&](int t, int buf) {
+    lk.load(kbase + (int64_t)32 * t * p.k.st * T::ES, sp.len - 32 * t, lds[wave][buf][0]);
+  };
+  auto fetch_v = [&](int t, int buf) {
+    lv.load(vbase + (int64_t)32 * t * p.v.st * T::ES, sp.len - 32 * t, lds[wave][buf][1]);
+  };
+  // this wave's LDS reads are done (before their bytes are loaded over)
+  auto reads_done = [] { __asm__ __volatile__("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+  // all its loads but the last N are done
+  auto loads_done = [](auto n) {
+    gemm::wait_vmcnt<decltype(n)::value>();
+    __asm__ __volatile__("" ::: "memory");
+  };
+  using std::integral_constant;
+  f32x16 acc[T::ND] = {};
+  Softmax<DP> sm;
+  if (t_first < t_last) {
+    fetch_k(t_first, 0);
+    fetch_v(t_first, 0);
+  }
+  for (int t = t_first, buf = 0; t < t_last; t += NW, buf ^= NBUF - 1) {
+    const bool more = t + NW < t_last;
+    if (NBUF == 2) {
+      reads_done();
+      if (more) {
+        fetch_k(t + NW, buf ^ 1);
+        fetch_v(t + NW, buf ^ 1);
+        loads_done(integral_constant<int, 2 * LOADS>{});
+      } else {
+        loads_done(integral_constant<int, 0>{});
+      }
+    } else {
+      loads_done(integral_constant<int, LOADS>{});
+    }
+    f32x16 S[1] = {dot<BF, DP>(lds[wave][buf][0], 0, q, lane)};
+    if (NBUF == 1 && more) {
+      reads_done();
+      fetch_k(t + NW, 0);
+    }
+    const int lm = lim - 32 * t - 8 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (16 * (i >> 3) + (i & 7) >= lm) S[0][i] = -kInf;
+    sm.step(S, p.scale_log2, acc);
+    if (NBUF == 1) {
+      if (more) loads_done(integral_constant<int, LOADS>{});
+      else loads_done(integral_constant<int, 0>{});
+    }
+    accum<BF, DP>(lds[wave][buf][1], 0, S[0], acc, lane);
+    if (NBUF == 1 && more) {
+      reads_done();
+      fetch_v(t + NW, 0);
+    }
+  }
+  // The waves' results meet: m, l, and acc by column.
+  __syncthreads();
+  float* join = (float*)&lds[0][0][0][0];
+  const float l = sum_halves(sm.l);
+  if (lane < 32) {
+    stat[0][wave][lane] = sm.m;
+    stat[1][wave][lane] = l;
+  }
+  {
+    float* row = join + (wave * 32 + (lane & 31)) * Gm::PITCH + 8 * (lane >> 5);
+#pragma unroll
+    for (int db = 0; db < T::ND; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4*)(row + 32 * db + 16 * (i >> 3) + (i & 7)) = f32x4{acc[db][i], acc[db][i + 1], acc[db][i + 2], acc[db][i + 3]};
+  }
+  __syncthreads();
+  constexpr int TPC = NW * 2;  // threads a column
+  const int col = threadIdx.x / TPC, part = threadIdx.x % TPC, cc = cb * 32 + col;
+  if (cc >= cols) return;
+  const int64_t row = ((int64_t)b * p.HQ + hk * p.G + cc / p.TQ) * p.TQ + cc % p.TQ;
+  float M = -kInf, L = 0.f, f[NW];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) M = fmaxf(M, stat[0][i][col]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    f[i] = stat[0][i][col] == -kInf ? 0.f : __builtin_amdgcn_exp2f(stat[0][i][col] - M);
+    L += f[i] * stat[1][i][col];
+  }
+  auto sum = [&](int d) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) s += f[i] * join[(i * 32 + col) * Gm::PITCH + d];
+    return s;
+  };
+  if (p.splits > 1) {
+    float* out = p.part + (row * p.splits + split) * (p.D + 2);
+    for (int d = part; d < p.D; d += TPC) out[d] = sum(d);
+    if (part == 0) {
+      out[p.D] = M;
+      out[p.D + 1] = L;
+    }
+    return;
+  }
+  const float inv = 1.f / L;
+  char* dst = row_of(p.o, b, cc % p.TQ, hk * p.G + cc / p.TQ, T::ES);
+  for (int d = part; d < p.D; d += TPC) {
+    const float v = L == 0.f ? 0.f : sum(d) * inv;
+    if constexpr (BF) ((__bf16*)dst)[d] = (__bf16)v;
+    else ((float*)dst)[d] = v;
+  }
+  if (p.lse && part == 0) p.lse[row] = L == 0.f ? -kInf : (M + __builtin_amdgcn_logf(L)) * kLn2;
+}
+
+// The splits' results of one row, a block each: o = sum of f_s acc_s over sum
+// of f_s l_s with f_s = 2^(m_s - max m). Wave w adds the splits w, w + 4, ..;
+// the waves' sums are added in order.
+template <bool BF>
+__global__ __launch_bounds__(256) void join_kernel(const AttnParams p) {
+  __shared__ float sums[4][kAttnMaxD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = blockIdx.x;
+  const float* part = p.part + row * p.splits * (p.D + 2);
+  // lane s holds split s's statistics (at most 64 splits)
+  const bool in = lane < p.splits;
+  const float m = in ? part[lane * (p.D + 2) + p.D] : -kInf, l = in ? part[lane * (p.D + 2) + p.D + 1] : 0.f;
+  float M = m;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o, 64));
+  const float f = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(m - M);
+  float L = f * l, a = 0.f, a2 = 0.f;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) L += __shfl_xor(L, o, 64);
+  const bool d0 = lane < p.D, d1 = lane + 64 < p.D;
+#pragma unroll 4
+  for (int s = wave; s < p.splits; s += 4) {
+    const float* x = part + s * (p.D + 2);
+    const float fs = __shfl(f, s, 64);
+    a += fs * (d0 ? x[lane] : 0.f);
+    a2 += fs * (d1 ? x[lane + 64] : 0.f);
+  }
+  sums[wave][lane] = a;
+  sums[wave][lane + 64] = a2;
+  __syncthreads();
+  const int d = threadIdx.x;
+  if (d < p.D) {
+    const int64_t bh = row / p.TQ;
+    char* dst = row_of(p.o, (int)(bh / p.HQ), row - bh * p.TQ, (int)(bh % p.HQ), BF ? 2 : 4);
+    const float v = L == 0.f ? 0.f : ((sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d])) * (1.f / L);
+    if constexpr (BF) ((__bf16*)dst)[d] = (__bf16)v;
+    else ((float*)dst)[d] = v;
+  }
+  if (p.lse && d == 0) p.lse[row] = L == 0.f ? -kInf : (M + __builtin_amdgcn_logf(L)) * kLn2;
+}
+
 // --------------------------------------------------------------- backward
 // dq: the forward's walk with two tiles' products before and one after the
 // softmax. Also delta, which the dk / dv pass reads.
@@ -709,6 +914,23 @@ dim3 grid_of(int64_t items) { return dim3((unsigned)((items + 7) / 8 * 8)); }
 
 hipError_t attn_fwd(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
   return MT_ATTN_LAUNCH(fwd_kernel, (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
+}
+hipError_t attn_fwd_split(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
+  const int64_t items = (int64_t)p.B * p.HK * (((int64_t)p.G * p.TQ + 31) / 32) * p.splits;
+  const hipError_t e = by_width(p.D, [&](auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    const dim3 grid = grid_of(items);
+    if (bf16 && vec) attn::split_kernel<true, DP, true><<<grid, 256, 0, stream>>>(p);
+    else if (bf16) attn::split_kernel<true, DP, false><<<grid, 256, 0, stream>>>(p);
+    else if (vec) attn::split_kernel<false, DP, true><<<grid, 256, 0, stream>>>(p);
+    else attn::split_kernel<false, DP, false><<<grid, 256, 0, stream>>>(p);
+    return hipGetLastError();
+  });
+  if (e != hipSuccess || p.splits == 1) return e;
+  const dim3 grid((unsigned)((int64_t)p.B * p.HQ * p.TQ));
+  if (bf16) attn::join_kernel<true><<<grid, 256, 0, stream>>>(p);
+  else attn::join_kernel<false><<<grid, 256, 0, stream>>>(p);
+  return hipGetLastError();
 }
 hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
   return MT_ATTN_LAUNCH(dq_kernel, (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));

@@ -26,6 +26,10 @@ struct AttnParams {
 // D <= 128. bf16 inputs, or fp32. vec: every base and stride allows 16-byte
 // accesses and D is a multiple of a 16-byte chunk; else element accesses.
 hipError_t attn_fwd(const AttnParams& p, bool bf16, bool vec, hipStream_t stream);
+// The same with 32 queries (of all heads of a key head) and a share of the
+// keys a block: p.splits shares, whose results (D + 2 floats for each query and
+// head) meet in p.part unless there is one.
+hipError_t attn_fwd_split(const AttnParams& p, bool bf16, bool vec, hipStream_t stream);
 // The dq pass (which also writes p.delta; with_dq = 0: nothing else) and the
 // dk / dv pass.
 hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t stream);

@@ -136,7 +136,7 @@ mt_status check_attention(const AttnArgs& a, float scale, mt::AttnParams* p) {
   if (a.kv_len && (s = check_index(a.kv_len, "kv_len", B))) return s;
   if (a.q_start && (s = check_index(a.q_start, "q_start", B))) return s;
   if (B * HQ > INT32_MAX / 2 || B * HQ * cdiv(TQ, mt::kAttnRows) > INT32_MAX / 2 ||
-      B * HK * cdiv(TK, mt::kAttnRows) > INT32_MAX / 2)
+      B * HK * cdiv(TK, mt::kAttnRows) > INT32_MAX / 2 || B * HQ * TQ > INT32_MAX / 64)
     return fail(MT_ERR_SHAPE, "too many blocks of tokens and heads");
   *p = mt::AttnParams{};
   p->q = view(a.q);
@@ -177,6 +177,39 @@ bool attn_vector_ok(const mt_tensor* const* ts, int n) {
   return true;
 }
 
+// Shares of the keys for the split forward, 0 for the forward by blocks of 128
+// queries: whichever is estimated shorter, in us a key from what was measured
+// (bf16 / fp32, heads of up to 64 / 128; one block a CU, then two):
+//   by blocks of 128: 16 x 64 queries, 32 heads, 2048 keys, bf16: 74 us against
+//   116 split; 2 x 400, 12 heads of 96: 10.9 against 14.5;
+//   split: 1 query, 32 heads, 16384 keys, bf16: 21 us (32 shares) against 358;
+//   16 x 1 query, 32 over 8 heads, 4096 keys, fp32: 110 us (2 shares) against
+//   1066; 1 x 2000, 8 heads, fp32: 133 (1 share) against 290.
+int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
+  if (const int fs = g_attn_splits; fs >= 0) return fs;
+  const int64_t whole = (int64_t)p.B * p.HQ * cdiv(p.TQ, mt::kAttnRows);
+  if (whole > 512 && p.TQ > 32) return 0;
+  const int64_t blocks = (int64_t)p.B * p.HK * cdiv((int64_t)p.G * p.TQ, 32);
+  const bool wide = p.D > 64;
+  const double one = bf16 ? (wide ? 0.0217 : 0.018) : (wide ? 0.145 : 0.082);
+  const double round = bf16 ? (wide ? 0.0106 : 0.0117) : (wide ? 0.043 : 0.0245);
+  const int64_t slots = bf16 && !wide ? 512 : 256;  // blocks at a time, by their LDS
+  double best = 4.0 + p.TK * one * (whole <= 256 ? 1.0 : 1.7 * cdiv(whole, 512));
+  int splits = 0;
+  // what the shares of every row write and the join reads, at 4 TB/s
+  const double bytes = 8.0 * p.B * p.HQ * p.TQ * (p.D + 2) / 4e6;
+  // a share holds a tile of 32 keys a wave
+  for (int s = 1; s <= 64 && (s == 1 || s * 128 <= p.TK); ++s) {
+    const double join = s > 1 ? 3.0 + (0.12 + bytes) * s : 0.0;
+    const double t = cdiv(blocks * s, slots) * (5.0 + p.TK * round / s) + join;
+    if (t < best) {
+      best = t;
+      splits = s;
+    }
+  }
+  return splits;
+}
+
 }  // namespace
 
 mt_status attention_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,
@@ -195,16 +228,22 @@ mt_status attention_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
   for (int i = 0; i < 2; ++i)
     if (index_overlaps(outs[i], kv_len) || index_overlaps(outs[i], q_start))
       return fail(MT_ERR_ALIAS, std::string(names[i]) + " overlaps kv_len or q_start");
+  const bool empty = p.B == 0 || p.TQ == 0 || p.HQ == 0;
+  const int splits = empty ? 0 : choose_attn_splits(p, q->dtype == MT_BF16);
+  const size_t need = splits > 1 ? (size_t)splits * p.B * p.HQ * p.TQ * (p.D + 2) * sizeof(float) : 0;
   if (ws_query) {
-    *ws_query = 0;
+    *ws_query = need;
     return MT_OK;
   }
   if (ws && ((uintptr_t)ws & 255)) return fail(MT_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (p.B == 0 || p.TQ == 0 || p.HQ == 0) return MT_OK;
+  if (empty) return MT_OK;
   p.causal = (flags & MT_CAUSAL) != 0;
+  p.splits = ws && ws_bytes >= need ? splits : std::min(splits, 1);
+  p.part = (float*)ws;
   const mt_tensor* all[] = {q, k, v, o};
+  const bool bf = q->dtype == MT_BF16, vec = attn_vector_ok(all, 4);
   (void)hipGetLastError();
-  return hip_status(mt::attn_fwd(p, q->dtype == MT_BF16, attn_vector_ok(all, 4), stream));
+  return hip_status(splits ? mt::attn_fwd_split(p, bf, vec, stream) : mt::attn_fwd(p, bf, vec, stream));
 }
 
 mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,

@@ -34,6 +34,7 @@ std::atomic<int> g_stream_k{1};     // gathered 256x256 convolution products: 0 
 std::atomic<int> g_sk_blocks{0};    // stream-K blocks (0: one per CU, 256)
 std::atomic<int> g_persist{1};      // plain products on the 256x256 DMA tiles: one block per CU walking its tiles
 std::atomic<int> g_phase_grid{1};   // strided input gradient: 0 a launch per phase, 1 one grid when large, 2 always
+std::atomic<int> g_attn_splits{-1};  // forward attention: -1 automatic, 0 by blocks of 128 queries, n by n shares of the keys
 
 mt_status fail(mt_status s, const std::string& msg) {
   g_err = msg;
@@ -1592,6 +1593,9 @@ int mt_debug_set(const char* key, int64_t value) {
   } else if (!std::strcmp(key, "phase_grid")) {
     if (value < 0 || value > 2) return -2;
     g_phase_grid = (int)value;
+  } else if (!std::strcmp(key, "attn_splits")) {
+    if (value < -1 || value > 64) return -2;
+    g_attn_splits = (int)value;
   } else if (!std::strcmp(key, "sk_blocks")) {
     if (value < 0 || value > 65535) return -2;
     g_sk_blocks = (int)value;

@@ -60,6 +60,13 @@ def run_case(dtype, B, TQ, TK, HQ, HK, D, causal=False, lens=None, start=None, s
         check(name, got, *ref[name])
 
 
+@pytest.fixture
+def splits():
+    """Sets how the forward shares out the keys (see mt_debug_set) for one test."""
+    yield lambda n: b.debug_set("attn_splits", n)
+    b.debug_set("attn_splits", -1)
+
+
 # lengths around the tiles of 32, 64 and 128 tokens; every head width class; grouped heads
 SIZES = [(1, 1, 1, 1, 1, 8), (2, 1, 5, 4, 2, 64), (1, 33, 31, 3, 1, 32), (2, 64, 64, 2, 2, 64), (1, 65, 129, 4, 4, 128),
          (2, 127, 200, 6, 2, 96), (1, 128, 128, 8, 1, 80), (1, 257, 383, 2, 1, 112), (1, 509, 383, 4, 2, 128),
@@ -71,6 +78,35 @@ SIZES = [(1, 1, 1, 1, 1, 8), (2, 1, 5, 4, 2, 64), (1, 33, 31, 3, 1, 32), (2, 64,
 @pytest.mark.parametrize("size", SIZES, ids=str)
 def test_sizes(dtype, causal, size):
     run_case(dtype, *size, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [0, 1, 3, 64])
+def test_forward_by_blocks_and_by_shares_of_the_keys(dtype, n, splits):
+    """Every size by blocks of 128 queries, by one share and by shares of a few tiles or none, ragged too."""
+    splits(n)
+    for size in SIZES:
+        for causal in (False, True):
+            B, TQ, TK, HQ, HK, D = size
+            lens = None if causal else [max(0, TK - 40 * i) for i in range(B)]
+            run_case(dtype, *size, causal=causal, lens=lens)
+    run_case(dtype, 2, 20, 90, 4, 2, 33, causal=True)
+    run_case(dtype, 2, 50, 50, 4, 2, 64, causal=True, lens=[0, 33])
+    run_case(dtype, 1, 8, 2000, 4, 1, 128, causal=True, lens=[1500], use_ws=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_one_token_against_long_caches(dtype):
+    """Single tokens and short chunks at the ends of ragged caches, given as views of a longer buffer."""
+    B, TK, HQ, HK, D = 3, 5000, 8, 2, 128
+    k, v = (draw((B, TK + 100, HK, D), dtype, i)[:, :TK] for i in range(2))
+    lens = torch.tensor([5000, 1, 2777], dtype=torch.int32, device=DEV)
+    for TQ in (1, 3):
+        q = draw((B, TQ, HQ, D), dtype, 7 + TQ)
+        kw = dict(causal=True, kv_len=lens, q_start=(lens - TQ).int())
+        ref = reference(q, k, v, D ** -0.5, **kw)
+        for name, got in zip(("o", "lse"), forward(q, k, v, **kw)):
+            check(name, got, *ref[name])
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
