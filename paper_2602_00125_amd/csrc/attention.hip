@@ -769,20 +769,34 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
   store_rows<BF, DP, VEC>(row_of(p.dq, b, qrow, hq, T::ES), ok, p.D, acc, p.scale, false, p.accumulate, lane);
 }
 
-// dk and dv: a block holds 128 keys of one head and walks the queries that see
-// them, over all query heads of the group. Two accumulators leave no room for
-// both keys and values of wide bf16 heads in the registers of two waves a
-// SIMD, and with one wave the matrix cores wait for LDS (measured on 4 x 4096
-// x 32 heads of 128: 1.8 ms against 1.5): the values stay in LDS there.
-template <bool BF, int DP, bool VEC>
-__global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const AttnParams p) {
+// dk and dv: a block holds 128 keys of one head, 32 a wave, and walks the
+// queries that see them, over all query heads of the group. QS waves share the
+// same keys, each with its 32 queries of every tile; their accumulators are
+// added in LDS at the end. So a block fills a CU with two waves a SIMD, which a
+// wave alone could not hide LDS's latency with (measured on 4 x 4096 x 32 heads
+// of 128, bf16: 1.8 ms with one wave a SIMD, 1.1 with two), and few blocks take
+// half as long. Two accumulators leave no room for both keys and values of wide
+// bf16 heads in 256 registers: the values stay in LDS there. Wide fp32 heads
+// take all registers of a SIMD for one wave.
+template <bool BF, int DP>
+struct KvGeom {
   using T = Tile<BF, DP>;
-  constexpr bool VLDS = BF && DP > 64;
-  constexpr int BQ = BF && !VLDS ? 64 : 32, N = BQ / 32, BYTES = BQ * T::RB;
-  __shared__ __align__(1024) char lds[2][2][BYTES];
+  static constexpr bool VLDS = BF && DP > 64;
+  static constexpr int QS = BF || DP <= 64 ? 2 : 1;
+  static constexpr int NW = 4 * QS, BQ = 32 * QS;
+  static constexpr int BYTES = BQ * T::RB;
+};
+template <bool BF, int DP, bool VEC>
+__global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) void dkv_kernel(const AttnParams p) {
+  using T = Tile<BF, DP>;
+  using Gm = KvGeom<BF, DP>;
+  constexpr bool VLDS = Gm::VLDS;
+  constexpr int BQ = Gm::BQ, NW = Gm::NW;
+  __shared__ __align__(1024) char lds[2][2][Gm::BYTES];
   __shared__ __align__(1024) char vlds[VLDS ? 128 * T::RB : 16];
   __shared__ __align__(256) float stats[2][2][64];  // lse, delta of the tile's queries
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = wave & 3, qs = wave >> 2;  // which 32 keys, which queries of a tile
   const int nkb = (p.TK + 127) >> 7;
   // the blocks that see most queries first, over all heads of an XCD
   const int heads = p.B * p.HK, per = heads >> 3;
@@ -797,7 +811,7 @@ __global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const 
   }
   const int hk = bh % p.HK, b = bh / p.HK;
   const Span sp = span_of(p, b);
-  const int k0 = kb * 128 + wave * 32, kj = k0 + (lane & 31);
+  const int k0 = kb * 128 + kg * 32, kj = k0 + (lane & 31);
   const bool in = kj < p.TK, ok = kj < sp.len;
   const int krow = in ? kj : 0;
   // query tiles from the first that sees a key of the block; from q_all on
@@ -811,10 +825,9 @@ __global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const 
   const int tiles = (p.TQ - q_first + BQ - 1) / BQ;
   const int q_all = first_for(kb * 128 + 127), wfirst = first_for(k0);
   const bool wave_on = k0 < sp.len;
-  const int64_t see = p.causal ? (int64_t)kj - sp.start : 0;  // queries from here on see the lane's key
-  const int see_i = see < 0 ? 0 : see < p.TQ ? (int)see : p.TQ;
+  const int see = first_for(kj);  // queries from here on see the lane's key
 
-  Loader<BF, DP, BQ, 4, VEC> lq, lo;
+  Loader<BF, DP, BQ, NW, VEC> lq, lo;
   lq.init(wave, lane, p.q.st, p.D);
   lo.init(wave, lane, p.dout.st, p.D);
   auto fetch = [&](int it, int buf) {
@@ -834,10 +847,10 @@ __global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const 
   k.template load<VEC>(row_of(p.k, b, krow, hk, T::ES), ok, p.D, lane);
   const auto v = [&] {
     if constexpr (VLDS) {
-      Loader<BF, DP, 128, 4, VEC> l;
+      Loader<BF, DP, 128, NW, VEC> l;
       l.init(wave, lane, p.v.st, p.D);
       if (iters > 0) l.load(row_of(p.v, b, kb * 128, hk, T::ES), sp.len - kb * 128, vlds);
-      return OwnTile<BF, DP>(vlds, 32 * wave, lane);
+      return OwnTile<BF, DP>(vlds, 32 * kg, lane);
     } else {
       Own<BF, DP> o;
       o.template load<VEC>(row_of(p.v, b, krow, hk, T::ES), ok, p.D, lane);
@@ -850,25 +863,23 @@ __global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const 
     wait_all_barrier();
     if (it + 1 < iters) fetch(it + 1, buf ^ 1);
     const char *Q = lds[buf][0], *O = lds[buf][1];
-    const float *lse = stats[buf][0] + 8 * (lane >> 5), *delta = stats[buf][1] + 8 * (lane >> 5);
+    const int r0 = 32 * qs;
+    const float *lse = stats[buf][0] + r0 + 8 * (lane >> 5), *delta = stats[buf][1] + r0 + 8 * (lane >> 5);
     ++it;
     buf ^= 1;
-    if (!wave_on || (masked && t0 + BQ <= wfirst)) return;
-    const int from = see_i - t0 - 8 * (lane >> 5);
+    if (!wave_on || (masked && t0 + r0 + 32 <= wfirst)) return;
+    const int from = see - t0 - r0 - 8 * (lane >> 5);
+    f32x16 S = dot<BF, DP>(Q, r0, k, lane);
+    f32x16 dP = dot<BF, DP>(O, r0, v, lane);
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      f32x16 S = dot<BF, DP>(Q, 32 * n, k, lane);
-      f32x16 dP = dot<BF, DP>(O, 32 * n, v, lane);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = 16 * (i >> 3) + (i & 7) + 32 * n;
-        S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse[r] * kLog2e));
-        if (masked && r < from) S[i] = 0.f;
-        dP[i] = S[i] * (dP[i] - delta[r]);
-      }
-      accum<BF, DP>(O, 32 * n, S, av, lane);
-      accum<BF, DP>(Q, 32 * n, dP, ak, lane);
+    for (int i = 0; i < 16; ++i) {
+      const int r = 16 * (i >> 3) + (i & 7);
+      S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse[r] * kLog2e));
+      if (masked && r < from) S[i] = 0.f;
+      dP[i] = S[i] * (dP[i] - delta[r]);
     }
+    accum<BF, DP>(O, r0, S, av, lane);
+    accum<BF, DP>(Q, r0, dP, ak, lane);
   };
   // from the last query on, so that the blocks of a head read the same tiles at
   // a time whatever their first query is
@@ -876,6 +887,36 @@ __global__ __launch_bounds__(256, BF || DP <= 64 ? 2 : 1) void dkv_kernel(const 
     int t0 = q_first + (tiles - 1) * BQ;
     for (; t0 >= q_first && t0 >= q_all; t0 -= BQ) tile(std::false_type{}, t0);
     for (; t0 >= q_first; t0 -= BQ) tile(std::true_type{}, t0);
+  }
+  // the waves of the same keys meet, one accumulator at a time
+  if constexpr (Gm::QS > 1) {
+    constexpr int FL = 16 * T::ND * 64;  // floats of a wave's accumulator
+    static_assert(4 * FL * 4 <= (int)sizeof(lds), "the accumulators of four waves fit the tiles' LDS");
+    auto meet = [&](f32x16 (&a)[T::ND]) {
+      f32x4* mine = (f32x4*)&lds[0][0][0] + kg * (FL / 4) + lane;
+      __syncthreads();
+      if (qs == 1) {
+#pragma unroll
+        for (int db = 0; db < T::ND; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            mine[(4 * db + i) * 64] = f32x4{a[db][4 * i], a[db][4 * i + 1], a[db][4 * i + 2], a[db][4 * i + 3]};
+      }
+      __syncthreads();
+      if (qs == 0) {
+#pragma unroll
+        for (int db = 0; db < T::ND; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 x = mine[(4 * db + i) * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[db][4 * i + e] += x[e];
+          }
+      }
+    };
+    meet(ak);
+    meet(av);
+    if (qs) return;
   }
   // keys past the batch element's length take no part: zero
   if (p.dk.p)
@@ -936,7 +977,16 @@ hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t str
   return MT_ATTN_LAUNCH(dq_kernel, (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
 }
 hipError_t attn_bwd_dkv(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  return MT_ATTN_LAUNCH(dkv_kernel, (int64_t)p.B * p.HK * ((p.TK + 127) / 128));
+  const dim3 grid = grid_of((int64_t)p.B * p.HK * ((p.TK + 127) / 128));
+  return by_width(p.D, [&](auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    constexpr int TB = 64 * attn::KvGeom<true, DP>::NW, TF = 64 * attn::KvGeom<false, DP>::NW;
+    if (bf16 && vec) attn::dkv_kernel<true, DP, true><<<grid, TB, 0, stream>>>(p);
+    else if (bf16) attn::dkv_kernel<true, DP, false><<<grid, TB, 0, stream>>>(p);
+    else if (vec) attn::dkv_kernel<false, DP, true><<<grid, TF, 0, stream>>>(p);
+    else attn::dkv_kernel<false, DP, false><<<grid, TF, 0, stream>>>(p);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace mt

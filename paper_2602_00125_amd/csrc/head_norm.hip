@@ -399,18 +399,23 @@ __global__ __launch_bounds__(256) void bwd_elem_kernel(const HeadNormParams p) {
   }
 }
 
-// dwq, dwk (+)= the blocks' parts, in order within each of 16 interleaved
-// shares, then over the shares. A block covers 16 of the 2 D columns.
-__global__ __launch_bounds__(256) void finish_kernel(const float* part, int parts, int D, float* dwq, float* dwk, int add) {
-  __shared__ float sums[16][17];
+// dwq, dwk (+)= the blocks' parts, in order within each of 64 interleaved
+// shares, then over the shares. A block covers 16 of the 2 D columns; a thread
+// keeps eight loads in flight (4 x 16 shares of 64 parts one by one: 20 us).
+__global__ __launch_bounds__(1024) void finish_kernel(const float* part, int parts, int D, float* dwq, float* dwk, int add) {
+  __shared__ float sums[64][17];
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
   float s = 0.f;
-  if (c < 2 * D)
-    for (int i = share; i < parts; i += 16) s += part[(int64_t)i * 2 * D + c];
+  if (c < 2 * D) {
+#pragma unroll 8
+    for (int i = share; i < parts; i += 64) s += part[(int64_t)i * 2 * D + c];
+  }
   sums[share][threadIdx.x & 15] = s;
   __syncthreads();
   if (share || c >= 2 * D) return;
-  for (int i = 1; i < 16; ++i) s += sums[i][threadIdx.x];
+  s = 0.f;
+#pragma unroll 16
+  for (int i = 0; i < 64; ++i) s += sums[i][threadIdx.x];
   float* out = c < D ? dwq : dwk;
   if (!out) return;
   out += c < D ? c : c - D;
@@ -457,7 +462,7 @@ hipError_t head_norm_bwd(const HeadNormParams& p, bool x_bf16, bool y_bf16, int 
 }
 
 hipError_t head_norm_finish(const float* part, int parts, int D, float* dwq, float* dwk, bool add, hipStream_t stream) {
-  headnorm::finish_kernel<<<dim3((unsigned)((2 * D + 15) / 16)), 256, 0, stream>>>(part, parts, D, dwq, dwk, add);
+  headnorm::finish_kernel<<<dim3((unsigned)((2 * D + 15) / 16)), 1024, 0, stream>>>(part, parts, D, dwq, dwk, add);
   return hipGetLastError();
 }
 
