@@ -798,7 +798,8 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = wave & 3, qs = wave >> 2;  // which 32 keys, which queries of a tile
   const int nkb = (p.TK + 127) >> 7;
-  // the blocks that see most queries first, over all heads of an XCD
+  // As many heads of an XCD at a time as fill its 32 CUs (their queries share
+  // the L2), the blocks that see most queries first
   const int heads = p.B * p.HK, per = heads >> 3;
   int kb, bh;
   if (heads & 7) {
@@ -806,8 +807,10 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
     kb = blockIdx.x / heads;
     bh = blockIdx.x - kb * heads;
   } else {
-    kb = (blockIdx.x >> 3) / per;
-    bh = (blockIdx.x & 7) * per + ((blockIdx.x >> 3) - kb * per);
+    const int i = blockIdx.x >> 3, some = (32 + nkb - 1) / nkb, most = some < per ? some : per;
+    const int h0 = i / (most * nkb) * most, now = per - h0 < most ? per - h0 : most, r = i - h0 * nkb;
+    kb = r / now;
+    bh = (blockIdx.x & 7) * per + h0 + (r - kb * now);
   }
   const int hk = bh % p.HK, b = bh / p.HK;
   const Span sp = span_of(p, b);
