@@ -95,6 +95,12 @@ __device__ __forceinline__ float ld_elem(const char* p, int64_t i, bool bf) {
   return bf ? __uint_as_float((unsigned)((const unsigned short*)p)[i] << 16) : ((const float*)p)[i];
 }
 
+typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+__device__ __forceinline__ u32x4 lds_read16(uint32_t at) { return *(lds_u32x4*)(uintptr_t)at; }
+__device__ __forceinline__ u32x2 lds_read_tr(uint32_t at) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at));
+}
+
 // A tile of stream tokens in LDS, rows of RB bytes in 16-byte chunks whose
 // index is XORed with a function of the row, so that both kinds of reads hit
 // distinct banks: `dot` reads one chunk of 16 rows that differ modulo 16,
@@ -167,16 +173,49 @@ struct Own {
 template <bool BF, int DP>
 struct OwnTile {
   using T = Tile<BF, DP>;
-  const char* row;
-  int h, x;
+  uint32_t at;  // the lane's row; chunk bits as in Left
   __device__ __forceinline__ OwnTile(const char* tile, int n0, int lane) {
     const int r = lane & 31;
-    row = tile + (n0 + r) * T::RB;
-    h = lane >> 5;
-    x = T::swz(r);
+    at = lds_byte_addr(tile) + (n0 + r) * T::RB + (((lane >> 5) ^ T::swz(r)) * 16);
   }
-  __device__ __forceinline__ u32x4 frag(int s) const { return *(const u32x4*)(row + (((2 * s + h) ^ x) * 16)); }
+  __device__ __forceinline__ u32x4 frag(int s) const { return lds_read16(at ^ (32 * s)); }
 };
+
+// A lane's left operands from a bf16 tile: for `dot`, 16-byte chunks of the
+// tile's rows (in the order of tile_row); for `accum`, 16 rows x 32 columns
+// transposed. Places in the tile as byte offsets whose chunk bits (from bit 4
+// on, below the rows') a step changes by XOR alone: one instruction a read, and
+// no address kept from one read to another.
+template <bool BF, int DP>
+struct Left {
+  using T = Tile<BF, DP>;
+  uint32_t row, lo, hi;
+  __device__ __forceinline__ explicit Left(int lane) {
+    const int r = tile_row(lane), h = lane >> 5;
+    row = r * T::RB + ((h ^ T::swz(r)) * 16);
+    // ds_read_b64_tr_b16: lane s of a 16-lane group addresses four columns of
+    // row s / 4; lane i receives the rows' column 4 p(i / 4) + i % 4, where
+    // p swaps the middle two of four column groups (the order of tile_row)
+    const int s = lane & 15, g = (lane >> 4) & 1;
+    const int pc = ((s & 1) << 1) | ((s >> 1) & 1);
+    const int rl = 8 * h + (s >> 2), c = 2 * g + (pc >> 1);
+    lo = rl * T::RB + ((c ^ T::swz(rl)) * 16) + 8 * (pc & 1);
+    hi = (rl + 4) * T::RB + ((c ^ T::swz(rl + 4)) * 16) + 8 * (pc & 1);
+  }
+  // at: LDS address of a tile's row (a multiple of 32 rows from its start);
+  // chunks 2 s + h of the 32 rows from there
+  __device__ __forceinline__ u32x4 rows(uint32_t at, int s) const { return lds_read16((at + row) ^ (32 * s)); }
+  // rows 16 kk .. + 15 and columns 32 db .. + 31 from there
+  __device__ __forceinline__ u32x4 cols(uint32_t at, int kk, int db) const {
+    const u32x2 a = lds_read_tr(((at + lo) ^ (64 * db)) + 16 * kk * T::RB);
+    const u32x2 b = lds_read_tr(((at + hi) ^ (64 * db)) + 16 * kk * T::RB);
+    return u32x4{a[0], a[1], b[0], b[1]};
+  }
+};
+
+__device__ __forceinline__ f32x16 mfma_bf16(const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
 
 // C[r][n] = sum_d tile[r0 + r][d] own[n][d], r in 0..31 (r0 a multiple of 32).
 template <bool BF, int DP, typename O>
@@ -861,6 +900,7 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
     }
   }();
   f32x16 ak[T::ND] = {}, av[T::ND] = {};
+  const Left<BF, DP> left(lane);
   int it = 0, buf = 0;
   auto tile = [&](auto masked, int t0) {
     wait_all_barrier();
@@ -872,6 +912,68 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
     buf ^= 1;
     if (!wave_on || (masked && t0 + r0 + 32 <= wfirst)) return;
     const int from = see - t0 - r0 - 8 * (lane >> 5);
+    if constexpr (BF) {
+      // The MFMAs in order, each step's left operand read AHEAD steps before it,
+      // and the softmax's arithmetic between them: P under the product for dP,
+      // dS under the one for dv.
+      constexpr int NF = T::NF, NA = 2 * T::ND, STEPS = 2 * NF + 2 * NA;
+      constexpr int AHEAD = 4, VA = 3;
+      const uint32_t Qr = lds_byte_addr(Q) + r0 * T::RB, Or = lds_byte_addr(O) + r0 * T::RB;
+      auto load = [&](int i) {
+        if (i < NF) return left.rows(Qr, i);
+        if (i < 2 * NF) return left.rows(Or, i - NF);
+        const int j = (i - 2 * NF) % NA;
+        return left.cols(i < 2 * NF + NA ? Or : Qr, j / T::ND, j % T::ND);
+      };
+      auto vt = v;
+      if constexpr (VLDS) __asm__ __volatile__("" : "+v"(vt.at));  // its addresses are not kept across tiles
+      u32x4 ring[AHEAD], vring[VA];
+      f32x16 S = {}, dP = {};
+      u32x4 P[2], dS[2];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) ring[i] = load(i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const u32x4 a = ring[i % AHEAD];
+        if (i < NF) {
+          S = mfma_bf16(a, k.frag(i), S);
+        } else if (i < 2 * NF) {
+          dP = mfma_bf16(a, VLDS ? vring[(i - NF) % VA] : vt.frag(i - NF), dP);
+        } else {
+          const int j = (i - 2 * NF) % NA, kk = j / T::ND, db = j % T::ND;
+          if (i < 2 * NF + NA) av[db] = mfma_bf16(a, P[kk], av[db]);
+          else ak[db] = mfma_bf16(a, dS[kk], ak[db]);
+        }
+        if (i + AHEAD < STEPS) ring[i % AHEAD] = load(i + AHEAD);
+        if constexpr (VLDS) {
+          const int f = i + VA - NF;
+          if (f >= 0 && f < NF) vring[f % VA] = vt.frag(f);
+        }
+        // pairs of elements: NF steps share the 8 of P, NA those of dS
+        if (i >= NF && i < 2 * NF) {
+#pragma unroll
+          for (int e = (i - NF) * 8 / NF; e < (i - NF + 1) * 8 / NF; ++e) {
+#pragma unroll
+            for (int x = 2 * e; x < 2 * e + 2; ++x) {
+              const int r = 16 * (x >> 3) + (x & 7);
+              S[x] = __builtin_amdgcn_exp2f(fmaf(S[x], p.scale_log2, -lse[r] * kLog2e));
+              if (masked && r < from) S[x] = 0.f;
+            }
+            P[e >> 2][e & 3] = pack_bf16(S[2 * e], S[2 * e + 1]);
+          }
+        } else if (i >= 2 * NF && i < 2 * NF + NA) {
+#pragma unroll
+          for (int e = (i - 2 * NF) * 8 / NA; e < (i - 2 * NF + 1) * 8 / NA; ++e) {
+#pragma unroll
+            for (int x = 2 * e; x < 2 * e + 2; ++x) dP[x] = S[x] * (dP[x] - delta[16 * (x >> 3) + (x & 7)]);
+            dS[e >> 2][e & 3] = pack_bf16(dP[2 * e], dP[2 * e + 1]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      return;
+    }
     f32x16 S = dot<BF, DP>(Q, r0, k, lane);
     f32x16 dP = dot<BF, DP>(O, r0, v, lane);
 #pragma unroll
