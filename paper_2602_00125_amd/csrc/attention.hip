@@ -33,6 +33,9 @@
 // sums of 4 bytes a d for every 128 keys, which cost more than the products.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+#include <utility>
+
 #include "attention.hpp"
 #include "gemm_dma.hpp"
 
@@ -58,6 +61,16 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kInf = __builtin_inff();
+
+// f(0), f(1), .. f(N - 1) with constant arguments.
+template <typename F, int... I>
+__device__ __forceinline__ void unroll_seq(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void unroll(F f) {
+  unroll_seq(f, std::make_integer_sequence<int, N>{});
+}
 
 // All loads and LDS accesses of this wave done, then every wave's.
 __device__ __forceinline__ void wait_all_barrier() {
@@ -202,13 +215,13 @@ struct Left {
     lo = rl * T::RB + ((c ^ T::swz(rl)) * 16) + 8 * (pc & 1);
     hi = (rl + 4) * T::RB + ((c ^ T::swz(rl + 4)) * 16) + 8 * (pc & 1);
   }
-  // at: LDS address of a tile's row (a multiple of 32 rows from its start);
-  // chunks 2 s + h of the 32 rows from there
-  __device__ __forceinline__ u32x4 rows(uint32_t at, int s) const { return lds_read16((at + row) ^ (32 * s)); }
+  // at + off: LDS address of a tile's row (off, a constant, and the row's place
+  // multiples of 32 rows); chunks 2 s + h of the 32 rows from there
+  __device__ __forceinline__ u32x4 rows(uint32_t at, int off, int s) const { return lds_read16(((at + row) ^ (32 * s)) + off); }
   // rows 16 kk .. + 15 and columns 32 db .. + 31 from there
-  __device__ __forceinline__ u32x4 cols(uint32_t at, int kk, int db) const {
-    const u32x2 a = lds_read_tr(((at + lo) ^ (64 * db)) + 16 * kk * T::RB);
-    const u32x2 b = lds_read_tr(((at + hi) ^ (64 * db)) + 16 * kk * T::RB);
+  __device__ __forceinline__ u32x4 cols(uint32_t at, int off, int kk, int db) const {
+    const u32x2 a = lds_read_tr(((at + lo) ^ (64 * db)) + 16 * kk * T::RB + off);
+    const u32x2 b = lds_read_tr(((at + hi) ^ (64 * db)) + 16 * kk * T::RB + off);
     return u32x4{a[0], a[1], b[0], b[1]};
   }
 };
@@ -776,7 +789,10 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
   go.template load<VEC>(row_of(p.dout, b, qrow, hq, T::ES), ok, p.D, lane);
   q.template load<VEC>(row_of(p.o, b, qrow, hq, T::ES), ok, p.D, lane);
   const float delta = sum_halves(go.dot(q));
-  if (ok && lane < 32) p.delta[stat] = delta;
+  if (ok && lane < 32) {  // as the dk / dv pass adds them to its products
+    p.delta[stat] = -p.lse[stat] / p.scale;
+    p.delta[(int64_t)p.B * p.HQ * p.TQ + stat] = -delta;
+  }
   if (!p.with_dq) return;
   q.template load<VEC>(row_of(p.q, b, qrow, hq, T::ES), ok, p.D, lane);
   // P = exp2(c S - lse2). A query that sees nothing has lse = -inf; all its
@@ -817,26 +833,27 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const AttnParams p) {
 // half as long. Two accumulators leave no room for both keys and values of wide
 // bf16 heads in 256 registers: the values stay in LDS there. Wide fp32 heads
 // take all registers of a SIMD for one wave.
-template <bool BF, int DP>
+template <bool BF, int DP, int KG, int QS, int SUB>
 struct KvGeom {
   using T = Tile<BF, DP>;
   static constexpr bool VLDS = BF && DP > 64;
-  static constexpr int QS = BF || DP <= 64 ? 2 : 1;
-  static constexpr int NW = 4 * QS, BQ = 32 * QS;
+  static constexpr int NW = KG * QS, BQ = 32 * QS * SUB, BKV = 32 * KG;
   static constexpr int BYTES = BQ * T::RB;
+  // waves a SIMD that its registers are for
+  static constexpr int OCC = BF || DP <= 64 ? 2 : 1;
 };
-template <bool BF, int DP, bool VEC>
-__global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) void dkv_kernel(const AttnParams p) {
+template <bool BF, int DP, bool VEC, int KG, int QS, int SUB>
+__global__ __launch_bounds__((64 * KG * QS), (KvGeom<BF, DP, KG, QS, SUB>::OCC)) void dkv_kernel(const AttnParams p) {
   using T = Tile<BF, DP>;
-  using Gm = KvGeom<BF, DP>;
+  using Gm = KvGeom<BF, DP, KG, QS, SUB>;
   constexpr bool VLDS = Gm::VLDS;
-  constexpr int BQ = Gm::BQ, NW = Gm::NW;
+  constexpr int BQ = Gm::BQ, NW = Gm::NW, BKV = Gm::BKV;
   __shared__ __align__(1024) char lds[2][2][Gm::BYTES];
-  __shared__ __align__(1024) char vlds[VLDS ? 128 * T::RB : 16];
+  __shared__ __align__(1024) char vlds[VLDS ? BKV * T::RB : 16];
   __shared__ __align__(256) float stats[2][2][64];  // lse, delta of the tile's queries
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kg = wave & 3, qs = wave >> 2;  // which 32 keys, which queries of a tile
-  const int nkb = (p.TK + 127) >> 7;
+  const int kg = wave % KG, qs = wave / KG;  // which 32 keys, which queries of a tile
+  const int nkb = (p.TK + BKV - 1) / BKV;
   // As many heads of an XCD at a time as fill its 32 CUs (their queries share
   // the L2), the blocks that see most queries first
   const int heads = p.B * p.HK, per = heads >> 3;
@@ -853,19 +870,19 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
   }
   const int hk = bh % p.HK, b = bh / p.HK;
   const Span sp = span_of(p, b);
-  const int k0 = kb * 128 + kg * 32, kj = k0 + (lane & 31);
+  const int k0 = kb * BKV + kg * 32, kj = k0 + (lane & 31);
   const bool in = kj < p.TK, ok = kj < sp.len;
   const int krow = in ? kj : 0;
   // query tiles from the first that sees a key of the block; from q_all on
   // every query sees all of them, before wfirst none sees a key of the wave
-  const bool any = kb * 128 < sp.len;
+  const bool any = kb * BKV < sp.len;
   auto first_for = [&](int key) {
     const int64_t i = p.causal ? (int64_t)key - sp.start : 0;
     return i < 0 ? 0 : i < p.TQ ? (int)i : p.TQ;
   };
-  const int q_first = any ? first_for(kb * 128) / BQ * BQ : p.TQ;
+  const int q_first = any ? first_for(kb * BKV) / BQ * BQ : p.TQ;
   const int tiles = (p.TQ - q_first + BQ - 1) / BQ;
-  const int q_all = first_for(kb * 128 + 127), wfirst = first_for(k0);
+  const int q_all = first_for(kb * BKV + BKV - 1), wfirst = first_for(k0);
   const bool wave_on = k0 < sp.len;
   const int see = first_for(kj);  // queries from here on see the lane's key
 
@@ -877,7 +894,7 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
     lq.load(row_of(p.q, b, t0, hq, T::ES), p.TQ - t0, lds[buf][0]);
     lo.load(row_of(p.dout, b, t0, hq, T::ES), p.TQ - t0, lds[buf][1]);
     if (wave < 2) {  // a 4-byte statistic a lane
-      const float* s = (wave ? p.delta : p.lse) + ((int64_t)b * p.HQ + hq) * p.TQ + t0;
+      const float* s = p.delta + ((int64_t)wave * p.B * p.HQ + (int64_t)b * p.HQ + hq) * p.TQ + t0;
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<char*>(uniform_ptr((const char*)s)), (short)0, 0x7fffffff, kRsrcWord3);
       dma4(r, lane < BQ && lane < p.TQ - t0 ? 4u * lane : kOOB, lds_byte_addr(stats[buf][wave]));
@@ -889,9 +906,9 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
   k.template load<VEC>(row_of(p.k, b, krow, hk, T::ES), ok, p.D, lane);
   const auto v = [&] {
     if constexpr (VLDS) {
-      Loader<BF, DP, 128, NW, VEC> l;
+      Loader<BF, DP, BKV, NW, VEC> l;
       l.init(wave, lane, p.v.st, p.D);
-      if (iters > 0) l.load(row_of(p.v, b, kb * 128, hk, T::ES), sp.len - kb * 128, vlds);
+      if (iters > 0) l.load(row_of(p.v, b, kb * BKV, hk, T::ES), sp.len - kb * BKV, vlds);
       return OwnTile<BF, DP>(vlds, 32 * kg, lane);
     } else {
       Own<BF, DP> o;
@@ -906,36 +923,45 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
     wait_all_barrier();
     if (it + 1 < iters) fetch(it + 1, buf ^ 1);
     const char *Q = lds[buf][0], *O = lds[buf][1];
-    const int r0 = 32 * qs;
-    const float *lse = stats[buf][0] + r0 + 8 * (lane >> 5), *delta = stats[buf][1] + r0 + 8 * (lane >> 5);
+    const float *lse = stats[buf][0] + 8 * (lane >> 5), *delta = stats[buf][1] + 8 * (lane >> 5);
     ++it;
     buf ^= 1;
-    if (!wave_on || (masked && t0 + r0 + 32 <= wfirst)) return;
-    const int from = see - t0 - r0 - 8 * (lane >> 5);
+    if (!wave_on || (masked && t0 + BQ <= wfirst)) return;
+    const int from = see - t0 - 8 * (lane >> 5);
     if constexpr (BF) {
       // The MFMAs in order, each step's left operand read AHEAD steps before it,
       // and the softmax's arithmetic between them: P under the product for dP,
       // dS under the one for dv.
-      constexpr int NF = T::NF, NA = 2 * T::ND, STEPS = 2 * NF + 2 * NA;
+      constexpr int NF = T::NF, NA = 2 * T::ND, PER = 2 * NF + 2 * NA, STEPS = SUB * PER;
       constexpr int AHEAD = 4, VA = 3;
-      const uint32_t Qr = lds_byte_addr(Q) + r0 * T::RB, Or = lds_byte_addr(O) + r0 * T::RB;
-      auto load = [&](int i) {
-        if (i < NF) return left.rows(Qr, i);
-        if (i < 2 * NF) return left.rows(Or, i - NF);
+      const uint32_t Qr = lds_byte_addr(Q) + 32 * SUB * qs * T::RB;
+      auto load = [&](int step) {
+        const int i = step % PER, at = step / PER * 32 * T::RB, O = at + Gm::BYTES;
+        if (i < NF) return left.rows(Qr, at, i);
+        if (i < 2 * NF) return left.rows(Qr, O, i - NF);
         const int j = (i - 2 * NF) % NA;
-        return left.cols(i < 2 * NF + NA ? Or : Qr, j / T::ND, j % T::ND);
+        return left.cols(Qr, i < 2 * NF + NA ? O : at, j / T::ND, j % T::ND);
       };
       auto vt = v;
       if constexpr (VLDS) __asm__ __volatile__("" : "+v"(vt.at));  // its addresses are not kept across tiles
       u32x4 ring[AHEAD], vring[VA];
-      f32x16 S = {}, dP = {};
+      f32x16 S, dP;
       u32x4 P[2], dS[2];
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) ring[i] = load(i);
       __builtin_amdgcn_sched_barrier(0);
+      unroll<STEPS>([&](auto step) {
+        constexpr int i = step % PER;
+        const int r0 = 32 * (step / PER + SUB * qs);
+        const u32x4 a = ring[step % AHEAD];
+        if (i == 0) {  // lse and delta come in as the products' first terms
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const u32x4 a = ring[i % AHEAD];
+          for (int x = 0; x < 16; ++x) S[x] = lse[r0 + 16 * (x >> 3) + (x & 7)];
+        }
+        if (i == NF - 2) {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) dP[x] = delta[r0 + 16 * (x >> 3) + (x & 7)];
+        }
         if (i < NF) {
           S = mfma_bf16(a, k.frag(i), S);
         } else if (i < 2 * NF) {
@@ -945,7 +971,7 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
           if (i < 2 * NF + NA) av[db] = mfma_bf16(a, P[kk], av[db]);
           else ak[db] = mfma_bf16(a, dS[kk], ak[db]);
         }
-        if (i + AHEAD < STEPS) ring[i % AHEAD] = load(i + AHEAD);
+        if (step + AHEAD < STEPS) ring[step % AHEAD] = load(step + AHEAD);
         if constexpr (VLDS) {
           const int f = i + VA - NF;
           if (f >= 0 && f < NF) vring[f % VA] = vt.frag(f);
@@ -956,9 +982,8 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
           for (int e = (i - NF) * 8 / NF; e < (i - NF + 1) * 8 / NF; ++e) {
 #pragma unroll
             for (int x = 2 * e; x < 2 * e + 2; ++x) {
-              const int r = 16 * (x >> 3) + (x & 7);
-              S[x] = __builtin_amdgcn_exp2f(fmaf(S[x], p.scale_log2, -lse[r] * kLog2e));
-              if (masked && r < from) S[x] = 0.f;
+              S[x] = __builtin_amdgcn_exp2f(S[x] * p.scale_log2);
+              if (masked && r0 + 16 * (x >> 3) + (x & 7) < from) S[x] = 0.f;
             }
             P[e >> 2][e & 3] = pack_bf16(S[2 * e], S[2 * e + 1]);
           }
@@ -966,25 +991,29 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
 #pragma unroll
           for (int e = (i - 2 * NF) * 8 / NA; e < (i - 2 * NF + 1) * 8 / NA; ++e) {
 #pragma unroll
-            for (int x = 2 * e; x < 2 * e + 2; ++x) dP[x] = S[x] * (dP[x] - delta[16 * (x >> 3) + (x & 7)]);
+            for (int x = 2 * e; x < 2 * e + 2; ++x) dP[x] *= S[x];
             dS[e >> 2][e & 3] = pack_bf16(dP[2 * e], dP[2 * e + 1]);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
-      }
-      return;
-    }
-    f32x16 S = dot<BF, DP>(Q, r0, k, lane);
-    f32x16 dP = dot<BF, DP>(O, r0, v, lane);
+      });
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int r = 16 * (i >> 3) + (i & 7);
-      S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], p.scale_log2, -lse[r] * kLog2e));
-      if (masked && r < from) S[i] = 0.f;
-      dP[i] = S[i] * (dP[i] - delta[r]);
+      for (int n = 0; n < SUB; ++n) {
+        const int r0 = 32 * (n + SUB * qs);
+        f32x16 S = dot<BF, DP>(Q, r0, k, lane);
+        f32x16 dP = dot<BF, DP>(O, r0, v, lane);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = r0 + 16 * (i >> 3) + (i & 7);
+          S[i] = __builtin_amdgcn_exp2f((S[i] + lse[r]) * p.scale_log2);
+          if (masked && r < from) S[i] = 0.f;
+          dP[i] = S[i] * (dP[i] + delta[r]);
+        }
+        accum<BF, DP>(O, r0, S, av, lane);
+        accum<BF, DP>(Q, r0, dP, ak, lane);
+      }
     }
-    accum<BF, DP>(O, r0, S, av, lane);
-    accum<BF, DP>(Q, r0, dP, ak, lane);
   };
   // from the last query on, so that the blocks of a head read the same tiles at
   // a time whatever their first query is
@@ -994,9 +1023,9 @@ __global__ __launch_bounds__((64 * KvGeom<BF, DP>::NW), (KvGeom<BF, DP>::QS)) vo
     for (; t0 >= q_first; t0 -= BQ) tile(std::true_type{}, t0);
   }
   // the waves of the same keys meet, one accumulator at a time
-  if constexpr (Gm::QS > 1) {
+  if constexpr (QS > 1) {
     constexpr int FL = 16 * T::ND * 64;  // floats of a wave's accumulator
-    static_assert(4 * FL * 4 <= (int)sizeof(lds), "the accumulators of four waves fit the tiles' LDS");
+    static_assert(QS == 2 && KG * FL * 4 <= (int)sizeof(lds), "the accumulators of a wave of each pair fit the tiles' LDS");
     auto meet = [&](f32x16 (&a)[T::ND]) {
       f32x4* mine = (f32x4*)&lds[0][0][0] + kg * (FL / 4) + lane;
       __syncthreads();
@@ -1082,14 +1111,20 @@ hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t str
   return MT_ATTN_LAUNCH(dq_kernel, (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
 }
 hipError_t attn_bwd_dkv(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  const dim3 grid = grid_of((int64_t)p.B * p.HK * ((p.TK + 127) / 128));
   return by_width(p.D, [&](auto dp) {
     constexpr int DP = decltype(dp)::value;
-    constexpr int TB = 64 * attn::KvGeom<true, DP>::NW, TF = 64 * attn::KvGeom<false, DP>::NW;
-    if (bf16 && vec) attn::dkv_kernel<true, DP, true><<<grid, TB, 0, stream>>>(p);
-    else if (bf16) attn::dkv_kernel<true, DP, false><<<grid, TB, 0, stream>>>(p);
-    else if (vec) attn::dkv_kernel<false, DP, true><<<grid, TF, 0, stream>>>(p);
-    else attn::dkv_kernel<false, DP, false><<<grid, TF, 0, stream>>>(p);
+    const int64_t heads = (int64_t)p.B * p.HK;
+    if (bf16) {
+      const dim3 grid = grid_of(heads * ((p.TK + 32 * 4 - 1) / (32 * 4)));
+      constexpr int T = 64 * 4 * 2;
+      if (vec) attn::dkv_kernel<true, DP, true, 4, 2, 1><<<grid, T, 0, stream>>>(p);
+      else attn::dkv_kernel<true, DP, false, 4, 2, 1><<<grid, T, 0, stream>>>(p);
+    } else {
+      const dim3 grid = grid_of(heads * ((p.TK + 127) / 128));
+      constexpr int QS = DP <= 64 ? 2 : 1;
+      if (vec) attn::dkv_kernel<false, DP, true, 4, QS, 1><<<grid, 256 * QS, 0, stream>>>(p);
+      else attn::dkv_kernel<false, DP, false, 4, QS, 1><<<grid, 256 * QS, 0, stream>>>(p);
+    }
     return hipGetLastError();
   });
 }

@@ -12,7 +12,7 @@ namespace mt {
 struct AttnParams {
   HeadView q, k, v, o, dout, dq, dk, dv;
   float* lse;           // [B, HQ, TQ]: written by the forward (NULL: skipped), read by the backward
-  float* delta;         // [B, HQ, TQ]: sum_d do o, from the dq pass to the dk / dv pass
+  float* delta;         // [2][B, HQ, TQ]: -lse / scale and -sum_d do o, from the dq pass to the dk / dv pass
   const int32_t* kv_len;   // [B] or NULL: keys of each batch element
   const int32_t* q_start;  // [B] or NULL: key position of query 0 (causal)
   int32_t B, TQ, TK, HQ, HK, G, D;

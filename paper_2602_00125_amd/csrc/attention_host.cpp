@@ -271,7 +271,7 @@ mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
       return fail(MT_ERR_ALIAS, std::string(names[i]) + " overlaps kv_len or q_start");
   }
   if ((s = check_apart(outs, names, 3, ins, 6, any_overlap))) return s;
-  const size_t need = (size_t)p.B * p.HQ * p.TQ * sizeof(float);
+  const size_t need = 2 * (size_t)p.B * p.HQ * p.TQ * sizeof(float);
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
