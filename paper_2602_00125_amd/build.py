@@ -20,7 +20,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["gemm_f32.hip", "gemm_bf16.hip", "reduce.hip", "elementwise.hip", "conv.hip", "noalloc.hip",
-           "attention.hip", "dropout.hip", "head_norm.hip", "shape.cpp", "capi.cpp", "conv_host.cpp",
+           "attention.hip", "attention_split.hip", "dropout.hip", "head_norm.hip", "shape.cpp", "capi.cpp", "conv_host.cpp",
            "attention_host.cpp"]
 # what is compiled: (source, extra flags); the fp32 products take most of the
 # time and compile in parts, side by side

@@ -398,6 +398,7 @@ hipError_t rmsprop_step(const OptBatch& b, float lr, float alpha, float eps, hip
 #ifndef MT_SEPARATE_UNITS
 // one object for these kernels: a build that does not compile them on their own
 #include "attention.hip"
+#include "attention_split.hip"
 #include "dropout.hip"
 #include "head_norm.hip"
 #endif
