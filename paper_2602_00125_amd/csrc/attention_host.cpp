@@ -180,21 +180,21 @@ bool attn_vector_ok(const mt_tensor* const* ts, int n) {
 // Shares of the keys for the split forward, 0 for the forward by blocks of 128
 // queries: whichever is estimated shorter, in us a key from what was measured
 // (bf16 / fp32, heads of up to 64 / 128; one block a CU, then two):
-//   by blocks of 128: 16 x 64 queries, 32 heads, 2048 keys, bf16: 74 us against
-//   116 split; 2 x 400, 12 heads of 96: 10.9 against 14.5;
+//   by blocks of 128: 8 x 500 queries, 16 heads, 2000 keys, bf16: 81 us against
+//   217 split; 2 x 400, 12 heads of 96: 11.4 against 14.4;
 //   split: 1 query, 32 heads, 16384 keys, bf16: 21 us (32 shares) against 358;
 //   16 x 1 query, 32 over 8 heads, 4096 keys, fp32: 110 us (2 shares) against
-//   1066; 1 x 2000, 8 heads, fp32: 133 (1 share) against 290.
+//   757; 1 x 2000, 8 heads, fp32: 131 (1 share) against 163.
 int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
   if (const int fs = g_attn_splits; fs >= 0) return fs;
   const int64_t whole = (int64_t)p.B * p.HQ * cdiv(p.TQ, mt::kAttnRows);
   if (whole > 512 && p.TQ > 32) return 0;
   const int64_t blocks = (int64_t)p.B * p.HK * cdiv((int64_t)p.G * p.TQ, 32);
   const bool wide = p.D > 64;
-  const double one = bf16 ? (wide ? 0.0217 : 0.018) : (wide ? 0.145 : 0.082);
+  const double one = bf16 ? (wide ? 0.0165 : 0.012) : (wide ? 0.08 : 0.0445);
   const double round = bf16 ? (wide ? 0.0106 : 0.0117) : (wide ? 0.043 : 0.0245);
   const int64_t slots = bf16 && !wide ? 512 : 256;  // blocks at a time, by their LDS
-  double best = 4.0 + p.TK * one * (whole <= 256 ? 1.0 : 1.7 * cdiv(whole, 512));
+  double best = 4.0 + p.TK * one * (whole <= 256 ? 1.0 : !bf16 && wide ? cdiv(whole, 256) : 1.7 * cdiv(whole, 512));
   int splits = 0;
   // what the shares of every row write and the join reads, at 4 TB/s
   const double bytes = 8.0 * p.B * p.HQ * p.TQ * (p.D + 2) / 4e6;
