@@ -239,23 +239,42 @@ struct Planes {
   }
 };
 
-// What holds for both kernels that stream keys past 128 queries a block.
-template <int PL, int DP>
+// What holds for both kernels that stream keys past 128 queries a block. KS = 2:
+// two waves for each 32 queries, which take halves of every tile and meet at the
+// end, for grids that would leave SIMDs with one wave.
+template <int PL, int DP, int KS>
 struct QGeom {
   using T = Tile<true, DP>;
-  static constexpr int BK = PL == 1 ? 64 : 32, N = BK / 32;  // keys a tile, and in parts of 32
-  static constexpr int PLANE = BK * T::RB, BYTES = PL * PLANE;
+  static constexpr int BK = PL == 1 ? 64 : 32, N = BK / 32;  // keys of a tile a wave takes, and in parts of 32
+  static constexpr int BT = BK * KS, NW = 4 * KS;            // keys a tile
+  static constexpr int PLANE = BT * T::RB, BYTES = PL * PLANE;
   static constexpr int NF = DP / 16, ND = DP / 32;
-  static constexpr int AHEAD = PL == 1 ? 4 : 2;     // steps that operands are read ahead
-  static constexpr int OCC = PL == 1 || DP <= 64 ? 2 : 1;  // waves a SIMD that its registers are for
+  static constexpr int AHEAD = PL == 1 ? 4 : 2;  // steps that operands are read ahead
+  static constexpr bool TWO = PL == 1 || DP <= 64;  // registers (and LDS) for two waves a SIMD
+  static constexpr int OCC = TWO ? 2 : 1;
+  static_assert(KS == 1 || TWO, "two waves a SIMD");
 };
+// Where wave (qg, 1) leaves a f32x16 for (qg, 0): 16-byte places a lane.
+__device__ __forceinline__ void leave(f32x4* at, const f32x16& a) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) at[64 * i] = f32x4{a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3]};
+}
+// a = a f + what was left g
+__device__ __forceinline__ void take(const f32x4* at, f32x16& a, float f, float g) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x4 x = at[64 * i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[4 * i + e] = a[4 * i + e] * f + x[e] * g;
+  }
+}
 
 // A block's queries (128 of a head, 32 a wave) and the keys they see.
 struct QBlock {
   int b, hq, hk, qi, lim, kend, kall;
   bool ok;
   Span sp;
-  __device__ __forceinline__ bool init(const AttnParams& p, int wave, int lane, int BK) {
+  __device__ __forceinline__ bool init(const AttnParams& p, int qg, int lane, int BT) {
     const int nqb = (p.TQ + 127) >> 7, w = work_item(p.B * p.HQ * nqb);
     if (w < 0) return false;
     // a key head's query heads together; the blocks that see most keys first
@@ -264,12 +283,12 @@ struct QBlock {
     b = bh / p.HK;
     hq = hk * p.G + g;
     sp = span_of(p, b);
-    qi = qb * 128 + wave * 32 + (lane & 31);
+    qi = qb * 128 + qg * 32 + (lane & 31);
     ok = qi < p.TQ;
     lim = ok ? visible(p, sp, qi) : 0;
     kend = __builtin_amdgcn_readfirstlane(visible(p, sp, qb * 128 + 127 < p.TQ ? qb * 128 + 127 : p.TQ - 1));
     // tiles that every query sees whole
-    kall = __builtin_amdgcn_readfirstlane(visible(p, sp, qb * 128)) / BK * BK;
+    kall = __builtin_amdgcn_readfirstlane(visible(p, sp, qb * 128)) / BT * BT;
     if (!ok) qi = 0;
     return true;
   }
@@ -279,18 +298,19 @@ struct QBlock {
 // Two tiles are worked on at a time: the product for tile t + 1's scores runs
 // over tile t's exponentials, and the product of tile t's P and values over
 // tile t + 1's maximum. Keys are fetched two tiles ahead, values one.
-template <int PL, int DP, bool VEC>
-__global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void fwd_kernel(const AttnParams p) {
-  using Gm = QGeom<PL, DP>;
-  constexpr int ES = PL == 1 ? 2 : 4, BK = Gm::BK, N = Gm::N, NF = Gm::NF, ND = Gm::ND, RB = Gm::T::RB;
+template <int PL, int DP, bool VEC, int KS>
+__global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kernel(const AttnParams p) {
+  using Gm = QGeom<PL, DP, KS>;
+  constexpr int ES = PL == 1 ? 2 : 4, BK = Gm::BK, BT = Gm::BT, N = Gm::N, NF = Gm::NF, ND = Gm::ND, RB = Gm::T::RB;
   __shared__ __align__(1024) char lds[2][2][Gm::BYTES];  // keys, values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qg = wave & 3, ks = wave >> 2;
   QBlock blk;
-  if (!blk.init(p, wave, lane, BK)) return;
+  if (!blk.init(p, qg, lane, BT)) return;
   const int kend = blk.kend, kall = blk.kall;
   Own32<PL, DP> q;
   q.template load<VEC>(row_of(p.q, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, lane);
-  Stream<PL, DP, BK, 4, VEC> lk, lv;
+  Stream<PL, DP, BT, Gm::NW, VEC> lk, lv;
   lk.init(wave, lane, p.k.st, p.D);
   lv.init(wave, lane, p.v.st, p.D);
   const char* kbase = row_of(p.k, blk.b, 0, blk.hk, ES);
@@ -331,13 +351,13 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void fwd_kernel(const At
   // Tile k0 (its scores in S) is finished, the scores of the next one begun in
   // X, masked or not; or there is none.
   auto tile = [&](auto next, auto masked, const f32x16 (&S)[N], f32x16 (&X)[N], int k0) {
-    const int buf = k0 / BK & 1;
+    const int buf = k0 / BT & 1;
     wait_all_barrier();
-    const bool more_v = k0 + BK < kend, more_k = k0 + 2 * BK < kend;
-    if (more_k) fetch_k(k0 + 2 * BK, buf);
-    if (more_v) fetch_v(k0 + BK, buf ^ 1);
+    const bool more_v = k0 + BT < kend, more_k = k0 + 2 * BT < kend;
+    if (more_k) fetch_k(k0 + 2 * BT, buf);
+    if (more_v) fetch_v(k0 + BT, buf ^ 1);
     constexpr int NS = next ? N * NF : 0, NV = N * 2 * ND, PAIRS = 8 * N;
-    const uint32_t K = lds_byte_addr(lds[0][buf ^ 1]), V = lds_byte_addr(lds[1][buf]);
+    const uint32_t K = lds_byte_addr(lds[0][buf ^ 1]) + ks * BK * RB, V = lds_byte_addr(lds[1][buf]) + ks * BK * RB;
     Frag<PL> P[N][2], ring[Gm::AHEAD];
     auto load = [&](auto i) {
       if constexpr (i < NS) {
@@ -353,7 +373,7 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void fwd_kernel(const At
       for (int e = 0; e < PAIRS; ++e) probability(S, P, e);
     }
     float t = -kInf;
-    const int lm = blk.lim - k0 - BK - 8 * (lane >> 5);
+    const int lm = blk.lim - k0 - BT - ks * BK - 8 * (lane >> 5);
     __builtin_amdgcn_sched_barrier(0);
     unroll<NS + NV>([&](auto i) {
       const Frag<PL> a = ring[i % Gm::AHEAD];
@@ -389,13 +409,13 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void fwd_kernel(const At
     fetch_k(0, 0);
     lk.commit(lds[0][0]);
     fetch_v(0, 0);
-    if (BK < kend) fetch_k(BK, 1);
+    if (BT < kend) fetch_k(BT, 1);
     wait_all_barrier();
     f32x16 S[N], X[N];
     {
-      const uint32_t K = lds_byte_addr(lds[0][0]);
+      const uint32_t K = lds_byte_addr(lds[0][0]) + ks * BK * RB;
       float t = -kInf;
-      const int lm = blk.lim - 8 * (lane >> 5);
+      const int lm = blk.lim - ks * BK - 8 * (lane >> 5);
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         S[n] = f32x16{};
@@ -408,21 +428,41 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void fwd_kernel(const At
       follow(t);
     }
     lv.commit(lds[1][0]);
-    if (BK < kend) lk.commit(lds[0][1]);
+    if (BT < kend) lk.commit(lds[0][1]);
     int k0 = 0;
     // two at a time: the scores change places without a copy
-    for (; k0 + 3 * BK <= kall; k0 += 2 * BK) {
+    for (; k0 + 3 * BT <= kall; k0 += 2 * BT) {
       tile(true_type{}, false_type{}, S, X, k0);
-      tile(true_type{}, false_type{}, X, S, k0 + BK);
+      tile(true_type{}, false_type{}, X, S, k0 + BT);
     }
-    for (; k0 + BK < kend; k0 += BK) {
+    for (; k0 + BT < kend; k0 += BT) {
       tile(true_type{}, true_type{}, S, X, k0);
 #pragma unroll
       for (int n = 0; n < N; ++n) S[n] = X[n];
     }
     tile(false_type{}, false_type{}, S, X, k0);
   }
-  const float l = sum_halves(l0 + l1);
+  float l = sum_halves(l0 + l1);
+  if constexpr (KS == 2) {
+    static_assert(4 * 64 * 4 * (16 * ND + 2) <= (int)sizeof(lds), "a wave's results of each pair fit the tiles' LDS");
+    f32x4* mine = (f32x4*)&lds[0][0][0] + qg * (4 * ND * 64) + lane;
+    float* stat = (float*)&lds[0][0][0] + 4 * 16 * ND * 64 + qg * 128 + lane;
+    __syncthreads();
+    if (ks) {
+      stat[0] = m;
+      stat[64] = l;
+#pragma unroll
+      for (int db = 0; db < ND; ++db) leave(mine + 256 * db, acc[db]);
+    }
+    __syncthreads();
+    if (ks) return;
+    const float m2 = stat[0], top = fmaxf(m, m2);
+    const float f = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(m - top), g = m2 == -kInf ? 0.f : __builtin_amdgcn_exp2f(m2 - top);
+    l = l * f + stat[64] * g;
+    m = top;
+#pragma unroll
+    for (int db = 0; db < ND; ++db) take(mine + 256 * db, acc[db], f, g);
+  }
   store_rows<PL == 1, DP, VEC>(row_of(p.o, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, acc, 1.f / l, l == 0.f, false, lane);
   if (p.lse && blk.ok && lane < 32)
     p.lse[((int64_t)blk.b * p.HQ + blk.hq) * p.TQ + blk.qi] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -432,16 +472,17 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void fwd_kernel(const At
 // dq, and for the dk / dv pass the statistics as it adds them to its products.
 // Of a tile's parts of 32 keys the products for S and dP come first, P under the
 // one for dP, dS under the next part's; then the products with the keys.
-template <int PL, int DP, bool VEC>
-__global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void dq_kernel(const AttnParams p) {
-  using Gm = QGeom<PL, DP>;
-  constexpr int ES = PL == 1 ? 2 : 4, BK = Gm::BK, N = Gm::N, NF = Gm::NF, ND = Gm::ND, RB = Gm::T::RB;
+template <int PL, int DP, bool VEC, int KS>
+__global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void dq_kernel(const AttnParams p) {
+  using Gm = QGeom<PL, DP, KS>;
+  constexpr int ES = PL == 1 ? 2 : 4, BK = Gm::BK, BT = Gm::BT, N = Gm::N, NF = Gm::NF, ND = Gm::ND, RB = Gm::T::RB;
   __shared__ __align__(1024) char lds[2][2][Gm::BYTES];  // buffer: keys, values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int qg = wave & 3, ks = wave >> 2;
   QBlock blk;
-  if (!blk.init(p, wave, lane, BK)) return;
+  if (!blk.init(p, qg, lane, BT)) return;
   const int kend = p.with_dq ? blk.kend : 0, kall = blk.kall;
-  Stream<PL, DP, BK, 4, VEC> lk, lv;
+  Stream<PL, DP, BT, Gm::NW, VEC> lk, lv;
   lk.init(wave, lane, p.k.st, p.D);
   lv.init(wave, lane, p.v.st, p.D);
   const char* kbase = row_of(p.k, blk.b, 0, blk.hk, ES);
@@ -461,7 +502,7 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void dq_kernel(const Att
   // P = exp2(c S - lse2). A query that sees nothing has lse = -inf; all its
   // keys are masked.
   const float lse = blk.ok ? p.lse[stat] : 0.f, lse2 = lse * kLog2e;
-  if (blk.ok && lane < 32) {
+  if (blk.ok && lane < 32 && ks == 0) {
     p.delta[stat] = -lse / p.scale;
     p.delta[(int64_t)p.B * p.HQ * p.TQ + stat] = -delta;
   }
@@ -474,12 +515,12 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void dq_kernel(const Att
   const float c = p.scale_log2;
   f32x16 acc[ND] = {};
   auto tile = [&](auto masked, int k0) {
-    const int buf = k0 / BK & 1;
+    const int buf = k0 / BT & 1;
     wait_all_barrier();
-    const bool more = k0 + BK < kend;
-    if (more) fetch(k0 + BK, buf ^ 1);
+    const bool more = k0 + BT < kend;
+    if (more) fetch(k0 + BT, buf ^ 1);
     constexpr int NS = N * 2 * NF, NA = N * 2 * ND;
-    const uint32_t K = lds_byte_addr(lds[buf][0]);
+    const uint32_t K = lds_byte_addr(lds[buf][0]) + ks * BK * RB;
     auto load = [&](auto i) {
       if constexpr (i < NS) {
         constexpr int n = i / (2 * NF), r = i % (2 * NF);
@@ -491,7 +532,7 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void dq_kernel(const Att
     };
     Frag<PL> ring[Gm::AHEAD], dS[N][2];
     f32x16 S[N], dP[N];
-    const int lm = blk.lim - k0 - 8 * (lane >> 5);
+    const int lm = blk.lim - k0 - ks * BK - 8 * (lane >> 5);
     auto probability = [&](int n, int x) {
       S[n][x] = __builtin_amdgcn_exp2f(fmaf(S[n][x], c, -lse2));
       if (masked && 32 * n + 16 * (x >> 3) + (x & 7) >= lm) S[n][x] = 0.f;
@@ -532,41 +573,55 @@ __global__ __launch_bounds__(256, (QGeom<PL, DP>::OCC)) void dq_kernel(const Att
     if (more) commit(buf ^ 1);
   };
   int k0 = 0;
-  for (; k0 < kall; k0 += BK) tile(std::false_type{}, k0);
-  for (; k0 < kend; k0 += BK) tile(std::true_type{}, k0);
+  for (; k0 < kall; k0 += BT) tile(std::false_type{}, k0);
+  for (; k0 < kend; k0 += BT) tile(std::true_type{}, k0);
+  if constexpr (KS == 2) {
+    static_assert(4 * 64 * 4 * 16 * ND <= (int)sizeof(lds), "a wave's results of each pair fit the tiles' LDS");
+    f32x4* mine = (f32x4*)&lds[0][0][0] + qg * (4 * ND * 64) + lane;
+    __syncthreads();
+    if (ks) {
+#pragma unroll
+      for (int db = 0; db < ND; ++db) leave(mine + 256 * db, acc[db]);
+    }
+    __syncthreads();
+    if (ks) return;
+#pragma unroll
+    for (int db = 0; db < ND; ++db) take(mine + 256 * db, acc[db], 1.f, 1.f);
+  }
   store_rows<PL == 1, DP, VEC>(row_of(p.dq, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, acc, p.scale, false, p.accumulate, lane);
 }
 
-// dk and dv: a block holds 128 keys of one head and walks the queries that see
-// them, over all query heads of the group. QS waves share the same 32 keys, each
-// with its 32 queries of every tile; their accumulators are added in LDS at the
-// end. So a block fills a CU with two waves a SIMD (measured on 4 x 4096 x 32
-// heads of 128, bf16: 1.8 ms with one, 1.05 with two; 1.19 with 256 keys a block
-// or blocks of four waves), and few blocks take half as long. Two accumulators
+// dk and dv: a block holds 32 KG = 128 keys of one head and walks the queries
+// that see them, over all query heads of the group. QS waves share the same 32
+// keys, each with its 32 queries of every tile; their accumulators are added in
+// LDS at the end. So a block fills a CU with two waves a SIMD (measured on 4 x
+// 4096 x 32 heads of 128, bf16: 1.8 ms with one, 1.05 with two; 1.19 with 256
+// keys a block or blocks of four waves). Grids that leave CUs without a block
+// hold 64 keys a block in bf16 (6 x 777 ragged, 4 heads of 96: 59 us against 41). Two accumulators
 // leave no room for both keys and values in 256 registers, so the values stay
 // in LDS, but for narrow bf16 heads, which have the room; wide fp32 heads take
 // all registers of a SIMD for one wave, their LDS being full.
-template <int PL, int DP>
+template <int PL, int DP, int KG>
 struct KvGeom {
   using T = Tile<true, DP>;
-  static constexpr int OCC = PL == 1 || DP <= 64 ? 2 : 1, QS = OCC;
-  static constexpr int NW = 4 * QS, BQ = 32 * QS;
+  static constexpr int OCC = PL == 1 || DP <= 64 ? 2 : 1, QS = 4 * OCC / KG;
+  static constexpr int NW = KG * QS, BQ = 32 * QS, BKV = 32 * KG;
   static constexpr bool VLDS = PL == 1 ? DP > 64 : DP <= 64;
-  static constexpr int PLANE = BQ * T::RB, BYTES = PL * PLANE, VPLANE = 128 * T::RB;
+  static constexpr int PLANE = BQ * T::RB, BYTES = PL * PLANE, VPLANE = BKV * T::RB;
   static constexpr int AHEAD = PL == 1 ? 4 : 2, VAHEAD = PL == 1 ? 3 : 1;
 };
-template <int PL, int DP, bool VEC>
-__global__ __launch_bounds__((64 * KvGeom<PL, DP>::NW), (KvGeom<PL, DP>::OCC)) void dkv_kernel(const AttnParams p) {
-  using Gm = KvGeom<PL, DP>;
-  constexpr int ES = PL == 1 ? 2 : 4, BQ = Gm::BQ, NW = Gm::NW, QS = Gm::QS, RB = Gm::T::RB;
+template <int PL, int DP, bool VEC, int KG>
+__global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>::OCC)) void dkv_kernel(const AttnParams p) {
+  using Gm = KvGeom<PL, DP, KG>;
+  constexpr int ES = PL == 1 ? 2 : 4, BQ = Gm::BQ, NW = Gm::NW, QS = Gm::QS, BKV = Gm::BKV, RB = Gm::T::RB;
   constexpr int NF = DP / 16, ND = DP / 32, NA = 2 * ND, AHEAD = Gm::AHEAD, VA = Gm::VAHEAD;
   constexpr bool VLDS = Gm::VLDS;
   __shared__ __align__(1024) char lds[2][2][Gm::BYTES];  // buffer: queries, output gradients
   __shared__ __align__(1024) char vlds[VLDS ? PL * Gm::VPLANE : 16];
-  __shared__ __align__(256) float stats[2][2][64];  // -lse / scale, -delta of the tile's queries
+  __shared__ __align__(256) float stats[2][2][BQ < 64 ? 64 : BQ];  // -lse / scale, -delta of the tile's queries
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kg = wave & 3, qs = wave >> 2;  // which 32 keys, which queries of a tile
-  const int nkb = (p.TK + 127) >> 7;
+  const int kg = wave % KG, qs = wave / KG;  // which 32 keys, which queries of a tile
+  const int nkb = (p.TK + BKV - 1) / BKV;
   // As many heads of an XCD at a time as fill its 32 CUs (their queries share
   // the L2), the blocks that see most queries first
   const int heads = p.B * p.HK, per = heads >> 3;
@@ -583,19 +638,19 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP>::NW), (KvGeom<PL, DP>::OCC)) v
   }
   const int hk = bh % p.HK, b = bh / p.HK;
   const Span sp = span_of(p, b);
-  const int k0 = kb * 128 + kg * 32, kj = k0 + (lane & 31);
+  const int k0 = kb * BKV + kg * 32, kj = k0 + (lane & 31);
   const bool in = kj < p.TK, ok = kj < sp.len;
   const int krow = in ? kj : 0;
   // query tiles from the first that sees a key of the block; from q_all on
   // every query sees all of them, before wfirst none sees a key of the wave
-  const bool any = kb * 128 < sp.len;
+  const bool any = kb * BKV < sp.len;
   auto first_for = [&](int key) {
     const int64_t i = p.causal ? (int64_t)key - sp.start : 0;
     return i < 0 ? 0 : i < p.TQ ? (int)i : p.TQ;
   };
-  const int q_first = any ? first_for(kb * 128) / BQ * BQ : p.TQ;
+  const int q_first = any ? first_for(kb * BKV) / BQ * BQ : p.TQ;
   const int tiles = (p.TQ - q_first + BQ - 1) / BQ;
-  const int q_all = first_for(kb * 128 + 127), wfirst = first_for(k0);
+  const int q_all = first_for(kb * BKV + BKV - 1), wfirst = first_for(k0);
   const bool wave_on = k0 < sp.len;
   const int see = first_for(kj);  // queries from here on see the lane's key
 
@@ -606,11 +661,12 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP>::NW), (KvGeom<PL, DP>::OCC)) v
     const int hq = hk * p.G + it / tiles, t0 = q_first + (tiles - 1 - it % tiles) * BQ;
     lq.fetch(row_of(p.q, b, t0, hq, ES), p.TQ - t0, lds[buf][0]);
     lo.fetch(row_of(p.dout, b, t0, hq, ES), p.TQ - t0, lds[buf][1]);
-    if (wave < 2) {  // a 4-byte statistic a lane
-      const float* s = p.delta + ((int64_t)wave * p.B * p.HQ + (int64_t)b * p.HQ + hq) * p.TQ + t0;
+    if (wave < 2 * ((BQ + 63) / 64)) {  // a 4-byte statistic a lane
+      const int which = wave & 1, q = 64 * (wave >> 1) + lane;
+      const float* s = p.delta + ((int64_t)which * p.B * p.HQ + (int64_t)b * p.HQ + hq) * p.TQ + t0;
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<char*>(uniform_ptr((const char*)s)), (short)0, 0x7fffffff, kRsrcWord3);
-      dma4(r, lane < BQ && lane < p.TQ - t0 ? 4u * lane : kOOB, lds_byte_addr(stats[buf][wave]));
+      dma4(r, q < BQ && q < p.TQ - t0 ? 4u * q : kOOB, lds_byte_addr(stats[buf][which]) + 256 * (wave >> 1));
     }
   };
   auto commit = [&](int buf) {
@@ -623,10 +679,10 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP>::NW), (KvGeom<PL, DP>::OCC)) v
   k.template load<VEC>(row_of(p.k, b, krow, hk, ES), ok, p.D, lane);
   auto v = [&] {
     if constexpr (VLDS) {
-      Stream<PL, DP, 128, NW, VEC> l;
+      Stream<PL, DP, BKV, NW, VEC> l;
       l.init(wave, lane, p.v.st, p.D);
       if (iters > 0) {
-        l.fetch(row_of(p.v, b, kb * 128, hk, ES), sp.len - kb * 128, vlds);
+        l.fetch(row_of(p.v, b, kb * BKV, hk, ES), sp.len - kb * BKV, vlds);
         l.commit(vlds);
       }
       return OwnRows<PL, DP, Gm::VPLANE>(vlds, 32 * kg, lane);
@@ -723,27 +779,20 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP>::NW), (KvGeom<PL, DP>::OCC)) v
   // the waves of the same keys meet, one accumulator at a time
   if constexpr (QS > 1) {
     constexpr int FL = 16 * ND * 64;  // floats of a wave's accumulator
-    static_assert(QS == 2 && 4 * FL * 4 <= (int)sizeof(lds), "the accumulators of a wave of each pair fit the tiles' LDS");
+    static_assert((QS - 1) * KG * FL * 4 <= (int)sizeof(lds), "the accumulators fit the tiles' LDS");
     auto meet = [&](f32x16 (&a)[ND]) {
-      f32x4* mine = (f32x4*)&lds[0][0][0] + kg * (FL / 4) + lane;
+      auto at = [&](int w) { return (f32x4*)&lds[0][0][0] + ((w - 1) * KG + kg) * (FL / 4) + lane; };
       __syncthreads();
-      if (qs == 1) {
+      if (qs) {
 #pragma unroll
-        for (int db = 0; db < ND; ++db)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            mine[(4 * db + i) * 64] = f32x4{a[db][4 * i], a[db][4 * i + 1], a[db][4 * i + 2], a[db][4 * i + 3]};
+        for (int db = 0; db < ND; ++db) leave(at(qs) + 256 * db, a[db]);
       }
       __syncthreads();
       if (qs == 0) {
 #pragma unroll
-        for (int db = 0; db < ND; ++db)
+        for (int w = 1; w < QS; ++w)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x4 x = mine[(4 * db + i) * 64];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) a[db][4 * i + e] += x[e];
-          }
+          for (int db = 0; db < ND; ++db) take(at(w) + 256 * db, a[db], 1.f, 1.f);
       }
     };
     meet(ak);
@@ -776,22 +825,47 @@ hipError_t attn_launch(const AttnParams& p, bool bf16, bool vec, F launch) {
 }  // namespace
 
 hipError_t attn_fwd(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  const dim3 grid = attn_grid((int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
+  const int64_t items = (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128);
+  const dim3 grid = attn_grid(items);
   return attn_launch(p, bf16, vec, [&](auto pl, auto dp, auto v) {
-    attn::fwd_kernel<decltype(pl)::value, decltype(dp)::value, decltype(v)::value><<<grid, 256, 0, stream>>>(p);
+    constexpr int PL = decltype(pl)::value, DP = decltype(dp)::value;
+    constexpr bool V = decltype(v)::value;
+    if constexpr (attn::QGeom<PL, DP, 1>::TWO) {
+      if (items <= 256) {  // a block a CU
+        attn::fwd_kernel<PL, DP, V, 2><<<grid, 512, 0, stream>>>(p);
+        return;
+      }
+    }
+    attn::fwd_kernel<PL, DP, V, 1><<<grid, 256, 0, stream>>>(p);
   });
 }
 hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  const dim3 grid = attn_grid((int64_t)p.B * p.HQ * ((p.TQ + 127) / 128));
+  const int64_t items = (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128);
+  const dim3 grid = attn_grid(items);
   return attn_launch(p, bf16, vec, [&](auto pl, auto dp, auto v) {
-    attn::dq_kernel<decltype(pl)::value, decltype(dp)::value, decltype(v)::value><<<grid, 256, 0, stream>>>(p);
+    constexpr int PL = decltype(pl)::value, DP = decltype(dp)::value;
+    constexpr bool V = decltype(v)::value;
+    if constexpr (attn::QGeom<PL, DP, 1>::TWO) {
+      if (items <= 256) {
+        attn::dq_kernel<PL, DP, V, 2><<<grid, 512, 0, stream>>>(p);
+        return;
+      }
+    }
+    attn::dq_kernel<PL, DP, V, 1><<<grid, 256, 0, stream>>>(p);
   });
 }
 hipError_t attn_bwd_dkv(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  const dim3 grid = attn_grid((int64_t)p.B * p.HK * ((p.TK + 127) / 128));
+  const int64_t heads = (int64_t)p.B * p.HK, items = heads * ((p.TK + 127) / 128);
   return attn_launch(p, bf16, vec, [&](auto pl, auto dp, auto v) {
     constexpr int PL = decltype(pl)::value, DP = decltype(dp)::value;
-    attn::dkv_kernel<PL, DP, decltype(v)::value><<<grid, 64 * attn::KvGeom<PL, DP>::NW, 0, stream>>>(p);
+    constexpr bool V = decltype(v)::value;
+    if constexpr (PL == 1) {
+      if (items < 256) {
+        attn::dkv_kernel<PL, DP, V, 2><<<attn_grid(heads * ((p.TK + 63) / 64)), 512, 0, stream>>>(p);
+        return;
+      }
+    }
+    attn::dkv_kernel<PL, DP, V, 4><<<attn_grid(items), 64 * attn::KvGeom<PL, DP, 4>::NW, 0, stream>>>(p);
   });
 }
 

@@ -194,14 +194,18 @@ int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
   const double one = bf16 ? (wide ? 0.0165 : 0.012) : (wide ? 0.08 : 0.0445);
   const double round = bf16 ? (wide ? 0.0106 : 0.0117) : (wide ? 0.043 : 0.0245);
   const int64_t slots = bf16 && !wide ? 512 : 256;  // blocks at a time, by their LDS
-  double best = 4.0 + p.TK * one * (whole <= 256 ? 1.0 : !bf16 && wide ? cdiv(whole, 256) : 1.7 * cdiv(whole, 512));
+  // causal blocks of unequal length fill rounds after the first better
+  const double later = p.causal ? 1.0 - 0.25 * std::min(1.0, (double)p.TQ / std::max(p.TK, 1)) : 1.0;
+  double best = 4.0 + p.TK * one *
+                          (whole <= 256 ? 1.0 : later * (!bf16 && wide ? cdiv(whole, 256) : 1.7 * cdiv(whole, 512)));
   int splits = 0;
   // what the shares of every row write and the join reads, at 4 TB/s
   const double bytes = 8.0 * p.B * p.HQ * p.TQ * (p.D + 2) / 4e6;
   // a share holds a tile of 32 keys a wave
   for (int s = 1; s <= 64 && (s == 1 || s * 128 <= p.TK); ++s) {
     const double join = s > 1 ? 3.0 + (0.12 + bytes) * s : 0.0;
-    const double t = cdiv(blocks * s, slots) * (5.0 + p.TK * round / s) + join;
+    const int64_t rounds = cdiv(blocks * s, slots);
+    const double t = rounds * (5.0 + p.TK * round / s) * (rounds > 1 ? later : 1.0) + join;
     if (t < best) {
       best = t;
       splits = s;
@@ -228,6 +232,7 @@ mt_status attention_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
   for (int i = 0; i < 2; ++i)
     if (index_overlaps(outs[i], kv_len) || index_overlaps(outs[i], q_start))
       return fail(MT_ERR_ALIAS, std::string(names[i]) + " overlaps kv_len or q_start");
+  p.causal = (flags & MT_CAUSAL) != 0;
   const bool empty = p.B == 0 || p.TQ == 0 || p.HQ == 0;
   const int splits = empty ? 0 : choose_attn_splits(p, q->dtype == MT_BF16);
   const size_t need = splits > 1 ? (size_t)splits * p.B * p.HQ * p.TQ * (p.D + 2) * sizeof(float) : 0;
@@ -237,7 +242,6 @@ mt_status attention_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
   }
   if (ws && ((uintptr_t)ws & 255)) return fail(MT_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (empty) return MT_OK;
-  p.causal = (flags & MT_CAUSAL) != 0;
   p.splits = ws && ws_bytes >= need ? splits : std::min(splits, 1);
   p.part = (float*)ws;
   const mt_tensor* all[] = {q, k, v, o};

@@ -96,6 +96,16 @@ def test_forward_by_blocks_and_by_shares_of_the_keys(dtype, n, splits):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 96, 128, 50])
+def test_more_blocks_than_compute_units(dtype, D, splits):
+    """Grids of more than 256 blocks of 128 queries (or keys), where fewer waves share those of a block."""
+    splits(0)
+    run_case(dtype, 5, 260, 200, 20, 4, D, causal=True, lens=[200, 0, 77, 130, 199])
+    run_case(dtype, 4, 290, 290, 24, 8, D, causal=True)
+    run_case(dtype, 5, 150, 300, 20, 20, D, causal=True, lens=[300, 300, 0, 1, 170])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_one_token_against_long_caches(dtype):
     """Single tokens and short chunks at the ends of ragged caches, given as views of a longer buffer."""
     B, TK, HQ, HK, D = 3, 5000, 8, 2, 128
