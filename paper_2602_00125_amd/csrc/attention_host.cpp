@@ -368,6 +368,7 @@ mt_status check_norm(const NormArgs& a, float eps, uint32_t flags, mt::HeadNormP
   p->R = (int32_t)R;
   p->interleaved = (flags & MT_ROPE_INTERLEAVED) != 0;
   p->eps = eps;
+  p->inv_D = 1.f / (float)D;
   if ((int64_t)p->HQ + p->HK > INT32_MAX / 2 || B * T > INT32_MAX / 2 || B * T * (p->HQ + p->HK) > INT32_MAX / 2)
     return fail(MT_ERR_SHAPE, "too many rows");
   return MT_OK;

@@ -95,7 +95,19 @@ __device__ __forceinline__ char* row_of(const HeadView& q, const HeadView& k, in
   return (char*)v.p + (b * v.sb + t * v.st + (head < HQ ? head : head - HQ) * v.sh) * es;
 }
 
+// The value of the lane n places on, in turn within a row of 16 lanes (a vector
+// instruction's own operand path; __shfl goes through LDS).
+template <int N>
+__device__ __forceinline__ float row16(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + N, 0xf, 0xf, false));
+}
 __device__ __forceinline__ float group_sum(float v, int L) {
+  if (L == 16) {
+    v += row16<8>(v);
+    v += row16<4>(v);
+    v += row16<2>(v);
+    return v + row16<1>(v);
+  }
   for (int o = L >> 1; o; o >>= 1) v += __shfl_xor(v, o, 64);
   return v;
 }
@@ -136,15 +148,18 @@ struct Angles {
 // v := rotate(v) (TRANSPOSED: by the negated angles). partner: the lane that
 // holds the other halves of this lane's pairs.
 template <int VEC, bool TRANSPOSED>
-__device__ __forceinline__ void rotate(float (&v)[VEC], const Angles<VEC>& a, bool interleaved, int partner) {
+__device__ __forceinline__ void rotate(float (&v)[VEC], const Angles<VEC>& a, const HeadNormParams& p, int partner) {
   const float sg = TRANSPOSED ? -1.f : 1.f;
-  if (interleaved) {
+  if (p.interleaved) {
 #pragma unroll
     for (int e = 0; e < VEC / 2; ++e) {
       const float x = v[2 * e], y = v[2 * e + 1], s = sg * a.s[e];
       v[2 * e] = x * a.c[e] - y * s;
       v[2 * e + 1] = y * a.c[e] + x * s;
     }
+  } else if (p.L == 16 && p.R == 16 * VEC) {  // whole heads of 16 lanes: the other half is 8 lanes on
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) v[e] = v[e] * a.c[e] - row16<8>(v[e]) * (sg * a.s[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[e] = v[e] * a.c[e] - __shfl(v[e], partner, 64) * (sg * a.s[e]);
@@ -194,7 +209,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(const HeadNormParams p) {
     float ss = 0.f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) ss = fmaf(x[i][e], x[i][e], ss);
-    const float r = 1.f / sqrtf(group_sum(ss, p.L) / (float)p.D + p.eps);
+    const float r = rsqrtf(group_sum(ss, p.L) * p.inv_D + p.eps);
     const float* w = head < p.HQ ? p.wq : p.wk;
     float wv[VEC];
 #pragma unroll
@@ -202,7 +217,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(const HeadNormParams p) {
     if (w && ln.on && head < heads) load<false, VEC>((const char*)(w + ln.d0), wv);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) x[i][e] = x[i][e] * r * wv[e];
-    rotate<VEC, false>(x[i], a, p.interleaved, ln.partner);
+    rotate<VEC, false>(x[i], a, p, ln.partner);
     if (ln.on && head < heads)
       store<YB, VEC>(row_of(p.yq, p.yk, p.HQ, b, t, head, YB ? 2 : 4) + ln.d0 * (YB ? 2 : 4), x[i]);
   }
@@ -263,7 +278,7 @@ __global__ __launch_bounds__(256) void bwd_kernel(const HeadNormParams p) {
     for (int i = 0; i < HPG; ++i) {
       const int head = h0 + i;
       const bool isq = head < p.HQ;
-      rotate<VEC, true>(g[i], a, p.interleaved, ln.partner);
+      rotate<VEC, true>(g[i], a, p, ln.partner);
       float ss = 0.f, xe = 0.f;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -272,8 +287,8 @@ __global__ __launch_bounds__(256) void bwd_kernel(const HeadNormParams p) {
       }
       ss = group_sum(ss, p.L);
       xe = group_sum(xe, p.L);
-      const float r = 1.f / sqrtf(ss / (float)p.D + p.eps);
-      const float mean = xe * r / (float)p.D;  // of n e
+      const float r = rsqrtf(ss * p.inv_D + p.eps);
+      const float mean = xe * r * p.inv_D;  // of n e
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const float n = x[i][e] * r, gn = g[i][e] * n;
@@ -357,7 +372,7 @@ __global__ __launch_bounds__(256) void fwd_elem_kernel(const HeadNormParams p) {
     const float v = load1<XB>(row.x, d);
     ss = fmaf(v, v, ss);
   }
-  const float r = 1.f / sqrtf(group_sum(ss, 64) / (float)p.D + p.eps);
+  const float r = rsqrtf(group_sum(ss, 64) * p.inv_D + p.eps);
   char* dst = row_of(p.yq, p.yk, p.HQ, b, t, head, YB ? 2 : 4);
   for (int d = lane; d < p.D; d += 64) store1<YB>(dst, d, row.y(p, d, r));
 }
@@ -379,8 +394,8 @@ __global__ __launch_bounds__(256) void bwd_elem_kernel(const HeadNormParams p) {
       ss = fmaf(v, v, ss);
       xe = fmaf(v, row.g(p, d) * row.weight(d), xe);
     }
-    const float r = 1.f / sqrtf(group_sum(ss, 64) / (float)p.D + p.eps);
-    const float mean = group_sum(xe, 64) * r / (float)p.D;
+    const float r = rsqrtf(group_sum(ss, 64) * p.inv_D + p.eps);
+    const float mean = group_sum(xe, 64) * r * p.inv_D;
     char* dst = p.yq.p ? row_of(p.yq, p.yk, p.HQ, b, t, head, YB ? 2 : 4) : nullptr;
     for (int d = lane; d < p.D; d += 64) {
       const float n = load1<XB>(row.x, d) * r, g = row.g(p, d);

@@ -193,7 +193,7 @@ struct HeadNormParams {
   int32_t B, T, HQ, HK, D, R;
   int32_t interleaved, accumulate;
   int32_t L, L_shift;  // lanes a row (a power of two)
-  float eps;
+  float eps, inv_D;    // 1 / D
   float* part;  // backward: [blocks][2][D] column sums of dw, or NULL
 };
 // vec: values a lane (8, 4: L lanes hold a row; 0: by element, a wave a row);
