@@ -194,8 +194,9 @@ int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
   const double one = bf16 ? (wide ? 0.0165 : 0.012) : (wide ? 0.08 : 0.0445);
   const double round = bf16 ? (wide ? 0.0106 : 0.0117) : (wide ? 0.043 : 0.0245);
   const int64_t slots = bf16 && !wide ? 512 : 256;  // blocks at a time, by their LDS
-  // causal blocks of unequal length fill rounds after the first better
-  const double later = p.causal ? 1.0 - 0.25 * std::min(1.0, (double)p.TQ / std::max(p.TK, 1)) : 1.0;
+  // blocks of unequal length (causal, ragged) fill rounds after the first better
+  const double later = (p.causal ? 1.0 - 0.25 * std::min(1.0, (double)p.TQ / std::max(p.TK, 1)) : 1.0) *
+                       (p.kv_len ? 0.88 : 1.0);
   double best = 4.0 + p.TK * one *
                           (whole <= 256 ? 1.0 : later * (!bf16 && wide ? cdiv(whole, 256) : 1.7 * cdiv(whole, 512)));
   int splits = 0;
