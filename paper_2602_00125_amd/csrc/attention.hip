@@ -269,19 +269,39 @@ __device__ __forceinline__ void take(const f32x4* at, f32x16& a, float f, float 
   }
 }
 
-// A block's queries (128 of a head, 32 a wave) and the keys they see.
-struct QBlock {
-  int b, hq, hk, qi, lim, kend, kall;
-  bool ok;
-  Span sp;
-  __device__ __forceinline__ bool init(const AttnParams& p, int qg, int lane, int BT) {
-    const int nqb = (p.TQ + 127) >> 7, w = work_item(p.B * p.HQ * nqb);
-    if (w < 0) return false;
-    // a key head's query heads together; the blocks that see most keys first
-    const int g = w % p.G, qb = nqb - 1 - (w / p.G) % nqb, bh = w / p.G / nqb;
+// Which queries a block holds: 128 of a head, or (paired) two such sets one
+// after the other. The heads of a key head run on the same XCDs, whose L2 their
+// keys share: 8 / gcd(groups, 8) XCDs take a set of groups between them, block
+// by block, those that see most keys first.
+struct QBlocks {
+  int b, hq, hk, qb[2], n;
+  __device__ __forceinline__ bool init(const AttnParams& p) {
+    const int nqb = (p.TQ + 127) >> 7, rows = p.paired ? (nqb + 1) >> 1 : nqb;
+    const int groups = p.B * p.HK, S = groups & 1 ? 8 : groups & 2 ? 4 : groups & 4 ? 2 : 1, sets = 8 / S;
+    const int x = blockIdx.x & 7, t = (blockIdx.x >> 3) * S + x % S, per = groups / sets;
+    if (t >= per * p.G * rows) return false;
+    const int g = t % p.G, r = t / p.G % rows, bh = x / S * per + t / p.G / rows;
     hk = bh % p.HK;
     b = bh / p.HK;
     hq = hk * p.G + g;
+    qb[0] = nqb - 1 - r;
+    qb[1] = r;
+    n = p.paired && r < nqb - 1 - r ? 2 : 1;
+    return true;
+  }
+};
+inline dim3 qblock_grid(const AttnParams& p) {
+  const int nqb = (p.TQ + 127) >> 7, rows = p.paired ? (nqb + 1) >> 1 : nqb;
+  const int groups = p.B * p.HK, S = groups & 1 ? 8 : groups & 2 ? 4 : groups & 4 ? 2 : 1, sets = 8 / S;
+  return dim3((unsigned)(8 * ((groups / sets * p.G * rows + S - 1) / S)));
+}
+
+// The lane's query of a set, and the keys the set sees.
+struct QSet {
+  int qi, lim, kend, kall;
+  bool ok;
+  Span sp;
+  __device__ __forceinline__ QSet(const AttnParams& p, int b, int qb, int qg, int lane, int BT) {
     sp = span_of(p, b);
     qi = qb * 128 + qg * 32 + (lane & 31);
     ok = qi < p.TQ;
@@ -290,7 +310,6 @@ struct QBlock {
     // tiles that every query sees whole
     kall = __builtin_amdgcn_readfirstlane(visible(p, sp, qb * 128)) / BT * BT;
     if (!ok) qi = 0;
-    return true;
   }
 };
 
@@ -299,24 +318,23 @@ struct QBlock {
 // over tile t's exponentials, and the product of tile t's P and values over
 // tile t + 1's maximum. Keys are fetched two tiles ahead, values one.
 template <int PL, int DP, bool VEC, int KS>
-__global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kernel(const AttnParams p) {
+__device__ __forceinline__ void fwd_set(const AttnParams& p, char (&lds)[2][2][QGeom<PL, DP, KS>::BYTES],  // keys, values
+                                        const QBlocks& at, int qb) {
   using Gm = QGeom<PL, DP, KS>;
   constexpr int ES = PL == 1 ? 2 : 4, BK = Gm::BK, BT = Gm::BT, N = Gm::N, NF = Gm::NF, ND = Gm::ND, RB = Gm::T::RB;
-  __shared__ __align__(1024) char lds[2][2][Gm::BYTES];  // keys, values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qg = wave & 3, ks = wave >> 2;
-  QBlock blk;
-  if (!blk.init(p, qg, lane, BT)) return;
-  const int kend = blk.kend, kall = blk.kall;
+  const QSet set(p, at.b, qb, qg, lane, BT);
+  const int kend = set.kend, kall = set.kall;
   Own32<PL, DP> q;
-  q.template load<VEC>(row_of(p.q, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, lane);
+  q.template load<VEC>(row_of(p.q, at.b, set.qi, at.hq, ES), set.ok, p.D, lane);
   Stream<PL, DP, BT, Gm::NW, VEC> lk, lv;
   lk.init(wave, lane, p.k.st, p.D);
   lv.init(wave, lane, p.v.st, p.D);
-  const char* kbase = row_of(p.k, blk.b, 0, blk.hk, ES);
-  const char* vbase = row_of(p.v, blk.b, 0, blk.hk, ES);
-  auto fetch_k = [&](int k0, int buf) { lk.fetch(kbase + (int64_t)k0 * p.k.st * ES, blk.sp.len - k0, lds[0][buf]); };
-  auto fetch_v = [&](int k0, int buf) { lv.fetch(vbase + (int64_t)k0 * p.v.st * ES, blk.sp.len - k0, lds[1][buf]); };
+  const char* kbase = row_of(p.k, at.b, 0, at.hk, ES);
+  const char* vbase = row_of(p.v, at.b, 0, at.hk, ES);
+  auto fetch_k = [&](int k0, int buf) { lk.fetch(kbase + (int64_t)k0 * p.k.st * ES, set.sp.len - k0, lds[0][buf]); };
+  auto fetch_v = [&](int k0, int buf) { lv.fetch(vbase + (int64_t)k0 * p.v.st * ES, set.sp.len - k0, lds[1][buf]); };
   const Planes<PL, DP, Gm::PLANE> left(lane);
   const float c = p.scale_log2;
   f32x16 acc[ND] = {};
@@ -373,7 +391,7 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kern
       for (int e = 0; e < PAIRS; ++e) probability(S, P, e);
     }
     float t = -kInf;
-    const int lm = blk.lim - k0 - BT - ks * BK - 8 * (lane >> 5);
+    const int lm = set.lim - k0 - BT - ks * BK - 8 * (lane >> 5);
     __builtin_amdgcn_sched_barrier(0);
     unroll<NS + NV>([&](auto i) {
       const Frag<PL> a = ring[i % Gm::AHEAD];
@@ -415,7 +433,7 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kern
     {
       const uint32_t K = lds_byte_addr(lds[0][0]) + ks * BK * RB;
       float t = -kInf;
-      const int lm = blk.lim - ks * BK - 8 * (lane >> 5);
+      const int lm = set.lim - ks * BK - 8 * (lane >> 5);
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         S[n] = f32x16{};
@@ -463,9 +481,21 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kern
 #pragma unroll
     for (int db = 0; db < ND; ++db) take(mine + 256 * db, acc[db], f, g);
   }
-  store_rows<PL == 1, DP, VEC>(row_of(p.o, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, acc, 1.f / l, l == 0.f, false, lane);
-  if (p.lse && blk.ok && lane < 32)
-    p.lse[((int64_t)blk.b * p.HQ + blk.hq) * p.TQ + blk.qi] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  store_rows<PL == 1, DP, VEC>(row_of(p.o, at.b, set.qi, at.hq, ES), set.ok, p.D, acc, 1.f / l, l == 0.f, false, lane);
+  if (p.lse && set.ok && lane < 32)
+    p.lse[((int64_t)at.b * p.HQ + at.hq) * p.TQ + set.qi] = l == 0.f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+template <int PL, int DP, bool VEC, int KS>
+__global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kernel(const AttnParams p) {
+  __shared__ __align__(1024) char lds[2][2][QGeom<PL, DP, KS>::BYTES];
+  QBlocks at;
+  if (!at.init(p)) return;
+  fwd_set<PL, DP, VEC, KS>(p, lds, at, at.qb[0]);
+  if constexpr (KS == 2) {
+    if (at.n < 2) return;
+    wait_all_barrier();  // the first set's tiles and results are read
+    fwd_set<PL, DP, VEC, KS>(p, lds, at, at.qb[1]);
+  }
 }
 
 // --------------------------------------------------------------- backward
@@ -473,43 +503,42 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void fwd_kern
 // Of a tile's parts of 32 keys the products for S and dP come first, P under the
 // one for dP, dS under the next part's; then the products with the keys.
 template <int PL, int DP, bool VEC, int KS>
-__global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void dq_kernel(const AttnParams p) {
+__device__ __forceinline__ void dq_set(const AttnParams& p, char (&lds)[2][2][QGeom<PL, DP, KS>::BYTES],  // buffer: keys, values
+                                       const QBlocks& at, int qb) {
   using Gm = QGeom<PL, DP, KS>;
   constexpr int ES = PL == 1 ? 2 : 4, BK = Gm::BK, BT = Gm::BT, N = Gm::N, NF = Gm::NF, ND = Gm::ND, RB = Gm::T::RB;
-  __shared__ __align__(1024) char lds[2][2][Gm::BYTES];  // buffer: keys, values
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int qg = wave & 3, ks = wave >> 2;
-  QBlock blk;
-  if (!blk.init(p, qg, lane, BT)) return;
-  const int kend = p.with_dq ? blk.kend : 0, kall = blk.kall;
+  const QSet set(p, at.b, qb, qg, lane, BT);
+  const int kend = p.with_dq ? set.kend : 0, kall = set.kall;
   Stream<PL, DP, BT, Gm::NW, VEC> lk, lv;
   lk.init(wave, lane, p.k.st, p.D);
   lv.init(wave, lane, p.v.st, p.D);
-  const char* kbase = row_of(p.k, blk.b, 0, blk.hk, ES);
-  const char* vbase = row_of(p.v, blk.b, 0, blk.hk, ES);
+  const char* kbase = row_of(p.k, at.b, 0, at.hk, ES);
+  const char* vbase = row_of(p.v, at.b, 0, at.hk, ES);
   auto fetch = [&](int k0, int buf) {
-    lk.fetch(kbase + (int64_t)k0 * p.k.st * ES, blk.sp.len - k0, lds[buf][0]);
-    lv.fetch(vbase + (int64_t)k0 * p.v.st * ES, blk.sp.len - k0, lds[buf][1]);
+    lk.fetch(kbase + (int64_t)k0 * p.k.st * ES, set.sp.len - k0, lds[buf][0]);
+    lv.fetch(vbase + (int64_t)k0 * p.v.st * ES, set.sp.len - k0, lds[buf][1]);
   };
   auto commit = [&](int buf) {
     lk.commit(lds[buf][0]);
     lv.commit(lds[buf][1]);
   };
   if (kend > 0) fetch(0, 0);
-  const char* gorow = row_of(p.dout, blk.b, blk.qi, blk.hq, ES);
-  const int64_t stat = ((int64_t)blk.b * p.HQ + blk.hq) * p.TQ + blk.qi;
-  const float delta = sum_halves(row_dot<PL, DP, VEC>(gorow, row_of(p.o, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, lane));
+  const char* gorow = row_of(p.dout, at.b, set.qi, at.hq, ES);
+  const int64_t stat = ((int64_t)at.b * p.HQ + at.hq) * p.TQ + set.qi;
+  const float delta = sum_halves(row_dot<PL, DP, VEC>(gorow, row_of(p.o, at.b, set.qi, at.hq, ES), set.ok, p.D, lane));
   // P = exp2(c S - lse2). A query that sees nothing has lse = -inf; all its
   // keys are masked.
-  const float lse = blk.ok ? p.lse[stat] : 0.f, lse2 = lse * kLog2e;
-  if (blk.ok && lane < 32 && ks == 0) {
+  const float lse = set.ok ? p.lse[stat] : 0.f, lse2 = lse * kLog2e;
+  if (set.ok && lane < 32 && ks == 0) {
     p.delta[stat] = -lse / p.scale;
     p.delta[(int64_t)p.B * p.HQ * p.TQ + stat] = -delta;
   }
   if (!p.with_dq) return;
   Own32<PL, DP> q, go;
-  q.template load<VEC>(row_of(p.q, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, lane);
-  go.template load<VEC>(gorow, blk.ok, p.D, lane);
+  q.template load<VEC>(row_of(p.q, at.b, set.qi, at.hq, ES), set.ok, p.D, lane);
+  go.template load<VEC>(gorow, set.ok, p.D, lane);
   if (kend > 0) commit(0);
   const Planes<PL, DP, Gm::PLANE> left(lane);
   const float c = p.scale_log2;
@@ -532,7 +561,7 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void dq_kerne
     };
     Frag<PL> ring[Gm::AHEAD], dS[N][2];
     f32x16 S[N], dP[N];
-    const int lm = blk.lim - k0 - ks * BK - 8 * (lane >> 5);
+    const int lm = set.lim - k0 - ks * BK - 8 * (lane >> 5);
     auto probability = [&](int n, int x) {
       S[n][x] = __builtin_amdgcn_exp2f(fmaf(S[n][x], c, -lse2));
       if (masked && 32 * n + 16 * (x >> 3) + (x & 7) >= lm) S[n][x] = 0.f;
@@ -588,7 +617,20 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void dq_kerne
 #pragma unroll
     for (int db = 0; db < ND; ++db) take(mine + 256 * db, acc[db], 1.f, 1.f);
   }
-  store_rows<PL == 1, DP, VEC>(row_of(p.dq, blk.b, blk.qi, blk.hq, ES), blk.ok, p.D, acc, p.scale, false, p.accumulate, lane);
+  store_rows<PL == 1, DP, VEC>(row_of(p.dq, at.b, set.qi, at.hq, ES), set.ok, p.D, acc, p.scale, false, p.accumulate, lane);
+}
+
+template <int PL, int DP, bool VEC, int KS>
+__global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void dq_kernel(const AttnParams p) {
+  __shared__ __align__(1024) char lds[2][2][QGeom<PL, DP, KS>::BYTES];
+  QBlocks at;
+  if (!at.init(p)) return;
+  dq_set<PL, DP, VEC, KS>(p, lds, at, at.qb[0]);
+  if constexpr (KS == 2) {
+    if (at.n < 2) return;
+    wait_all_barrier();
+    dq_set<PL, DP, VEC, KS>(p, lds, at, at.qb[1]);
+  }
 }
 
 // dk and dv: a block holds 32 KG = 128 keys of one head and walks the queries
@@ -822,36 +864,37 @@ hipError_t attn_launch(const AttnParams& p, bool bf16, bool vec, F launch) {
   });
 }
 
-}  // namespace
-
-hipError_t attn_fwd(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  const int64_t items = (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128);
-  const dim3 grid = attn_grid(items);
+// Blocks of 128 queries: one a CU has two waves for each 32 queries, and so have
+// two a CU of causal attention, as pairs of a long and a short one: side by side
+// the long ones would meet on some CUs.
+template <typename F>
+hipError_t attn_queries(AttnParams p, bool bf16, bool vec, F launch) {
+  const int64_t sets = (p.TQ + 127) / 128, items = (int64_t)p.B * p.HQ * sets;
+  const int64_t pairs = (int64_t)p.B * p.HQ * ((sets + 1) / 2);
   return attn_launch(p, bf16, vec, [&](auto pl, auto dp, auto v) {
-    constexpr int PL = decltype(pl)::value, DP = decltype(dp)::value;
-    constexpr bool V = decltype(v)::value;
-    if constexpr (attn::QGeom<PL, DP, 1>::TWO) {
-      if (items <= 256) {  // a block a CU
-        attn::fwd_kernel<PL, DP, V, 2><<<grid, 512, 0, stream>>>(p);
+    if constexpr (attn::QGeom<decltype(pl)::value, decltype(dp)::value, 1>::TWO) {
+      p.paired = p.causal && items > 256 && pairs <= 256;
+      if (items <= 256 || p.paired) {
+        launch(pl, dp, v, std::integral_constant<int, 2>{}, attn::qblock_grid(p), p);
         return;
       }
     }
-    attn::fwd_kernel<PL, DP, V, 1><<<grid, 256, 0, stream>>>(p);
+    launch(pl, dp, v, std::integral_constant<int, 1>{}, attn::qblock_grid(p), p);
   });
 }
-hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {
-  const int64_t items = (int64_t)p.B * p.HQ * ((p.TQ + 127) / 128);
-  const dim3 grid = attn_grid(items);
-  return attn_launch(p, bf16, vec, [&](auto pl, auto dp, auto v) {
-    constexpr int PL = decltype(pl)::value, DP = decltype(dp)::value;
-    constexpr bool V = decltype(v)::value;
-    if constexpr (attn::QGeom<PL, DP, 1>::TWO) {
-      if (items <= 256) {
-        attn::dq_kernel<PL, DP, V, 2><<<grid, 512, 0, stream>>>(p);
-        return;
-      }
-    }
-    attn::dq_kernel<PL, DP, V, 1><<<grid, 256, 0, stream>>>(p);
+
+}  // namespace
+
+hipError_t attn_fwd(const AttnParams& params, bool bf16, bool vec, hipStream_t stream) {
+  return attn_queries(params, bf16, vec, [&](auto pl, auto dp, auto v, auto ks, dim3 grid, const AttnParams& p) {
+    constexpr int KS = decltype(ks)::value;
+    attn::fwd_kernel<decltype(pl)::value, decltype(dp)::value, decltype(v)::value, KS><<<grid, 256 * KS, 0, stream>>>(p);
+  });
+}
+hipError_t attn_bwd_dq(const AttnParams& params, bool bf16, bool vec, hipStream_t stream) {
+  return attn_queries(params, bf16, vec, [&](auto pl, auto dp, auto v, auto ks, dim3 grid, const AttnParams& p) {
+    constexpr int KS = decltype(ks)::value;
+    attn::dq_kernel<decltype(pl)::value, decltype(dp)::value, decltype(v)::value, KS><<<grid, 256 * KS, 0, stream>>>(p);
   });
 }
 hipError_t attn_bwd_dkv(const AttnParams& p, bool bf16, bool vec, hipStream_t stream) {

@@ -16,7 +16,7 @@ struct AttnParams {
   const int32_t* kv_len;   // [B] or NULL: keys of each batch element
   const int32_t* q_start;  // [B] or NULL: key position of query 0 (causal)
   int32_t B, TQ, TK, HQ, HK, G, D;
-  int32_t causal, accumulate, with_dq;
+  int32_t causal, accumulate, with_dq, paired;
   float scale, scale_log2;  // scale and scale * log2(e)
   // keys shared out over splits (forward) / query tiles over splits (dk, dv)
   int32_t splits;

@@ -103,6 +103,8 @@ def test_more_blocks_than_compute_units(dtype, D, splits):
     run_case(dtype, 5, 260, 200, 20, 4, D, causal=True, lens=[200, 0, 77, 130, 199])
     run_case(dtype, 4, 290, 290, 24, 8, D, causal=True)
     run_case(dtype, 5, 150, 300, 20, 20, D, causal=True, lens=[300, 300, 0, 1, 170])
+    run_case(dtype, 5, 260, 200, 20, 4, D, lens=[200, 0, 77, 130, 199])
+    run_case(dtype, 7, 300, 300, 28, 7, D, causal=True)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
