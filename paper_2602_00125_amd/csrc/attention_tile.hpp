@@ -176,8 +176,13 @@ struct Loader {
       const __amdgpu_buffer_rsrc_t r =
           __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(uniform_ptr(base)), (short)0, 0x7fffffff, kRsrcWord3);
       const uint32_t lds0 = lds_byte_addr(tile);
+      if (left >= ROWS) {  // the test of the rows would be two vector instructions a load
 #pragma unroll
-      for (int j = 0; j < JB; ++j) dma16(r, row(j) < left ? off[j] : kOOB, lds0 + 1024 * (wave + NW * j));
+        for (int j = 0; j < JB; ++j) dma16(r, off[j], lds0 + 1024 * (wave + NW * j));
+      } else {
+#pragma unroll
+        for (int j = 0; j < JB; ++j) dma16(r, row(j) < left ? off[j] : kOOB, lds0 + 1024 * (wave + NW * j));
+      }
     } else {
       for (int j = 0; j < JB; ++j) {
         const int rr = row(j), d = col(j);
