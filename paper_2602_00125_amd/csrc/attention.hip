@@ -175,41 +175,63 @@ __device__ __forceinline__ float row_dot(const char* a, const char* b, bool ok, 
   return s;
 }
 
-// Stream tokens into a tile of ROWS rows by NW waves. bf16: straight into LDS by
-// fetch (see Loader). fp32: fetch reads into registers, commit splits them and
-// writes the planes, ROWS rows each. Rows from `left` on and columns from D on
-// are zero.
+// Stream tokens into a tile of ROWS rows by NW waves; rows from `left` on and
+// columns from D on are zero. bf16: straight into LDS by fetch (see Loader).
+// fp32: fetch reads into registers, part(e) for e in 0 .. PARTS - 1 splits a pair
+// of values a thread and writes finished chunks, each plane ROWS rows.
 template <int PL, int DP, int ROWS, int NW, bool VEC>
 struct Stream {
   using T = Tile<true, DP>;
-  static constexpr int CHUNKS = T::RB / 16, JB = ROWS * CHUNKS / (64 * NW);
+  static constexpr int CHUNKS = T::RB / 16, JB = ROWS * CHUNKS / (64 * NW), PARTS = 4 * JB;
   static_assert(ROWS * CHUNKS % (64 * NW) == 0, "whole chunks for every thread");
-  float v[JB][8];
+  f32x4 v[JB][2];
+  Frag<PL> f;
+  uint32_t off[JB];  // bytes from the tile's first token; columns past D: out of range
   int tid, D;
   int64_t st;
+  __device__ __forceinline__ int row(int j) const { return (tid + 64 * NW * j) / CHUNKS; }
+  __device__ __forceinline__ int chunk(int j) const { return (tid + 64 * NW * j) % CHUNKS; }
   __device__ __forceinline__ void init(int wave, int lane, int64_t st_, int D_) {
     tid = 64 * wave + lane;
     st = st_;
     D = D_;
+#pragma unroll
+    for (int j = 0; j < JB; ++j) off[j] = 8 * chunk(j) < D ? (row(j) * (uint32_t)st + 8 * chunk(j)) * 4u : kOOB;
   }
   __device__ __forceinline__ void fetch(const char* base, int left, char*) {
+    if constexpr (VEC) {
+      const __amdgpu_buffer_rsrc_t r =
+          __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(uniform_ptr(base)), (short)0, 0x7fffffff, kRsrcWord3);
 #pragma unroll
-    for (int j = 0; j < JB; ++j) {
-      const int c = tid + 64 * NW * j, r = c / CHUNKS;
-      row8<PL, VEC>(base + r * st * 4, c % CHUNKS * 8, r < left ? D : 0, v[j]);
+      for (int j = 0; j < JB; ++j) {
+        const uint32_t o = row(j) < left ? off[j] : kOOB;
+        v[j][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0));
+        // the chunk's second half may lie past D on its own
+        v[j][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                r, 8 * chunk(j) + 4 < D ? o + 16 : kOOB, 0, 0));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < JB; ++j) {
+        float x[8];
+        row8<PL, VEC>(base + row(j) * st * 4, 8 * chunk(j), row(j) < left ? D : 0, x);
+        v[j][0] = f32x4{x[0], x[1], x[2], x[3]};
+        v[j][1] = f32x4{x[4], x[5], x[6], x[7]};
+      }
     }
   }
-  __device__ __forceinline__ void commit(char* tile) const {
+  __device__ __forceinline__ void part(int e, char* tile) {
+    const int j = e >> 2, w = e & 3;
+    put<PL>(f, w, v[j][w >> 1][2 * (w & 1)], v[j][w >> 1][2 * (w & 1) + 1]);
+    if (w < 3) return;
 #pragma unroll
-    for (int j = 0; j < JB; ++j) {
-      const int c = tid + 64 * NW * j, r = c / CHUNKS;
-      Frag<PL> f;
+    for (int i = 0; i < PL; ++i)
+      *(u32x4*)(tile + i * ROWS * T::RB + row(j) * T::RB + ((chunk(j) ^ T::swz(row(j))) * 16)) = f.p[i];
+  }
+  // parts of share i of n
+  __device__ __forceinline__ void share(int i, int n, char* tile) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) put<PL>(f, e, v[j][2 * e], v[j][2 * e + 1]);
-#pragma unroll
-      for (int i = 0; i < PL; ++i)
-        *(u32x4*)(tile + i * ROWS * T::RB + r * T::RB + ((c % CHUNKS ^ T::swz(r)) * 16)) = f.p[i];
-    }
+    for (int e = i * PARTS / n; e < (i + 1) * PARTS / n; ++e) part(e, tile);
   }
 };
 template <int DP, int ROWS, int NW, bool VEC>
@@ -217,7 +239,7 @@ struct Stream<1, DP, ROWS, NW, VEC> {
   Loader<true, DP, ROWS, NW, VEC> l;
   __device__ __forceinline__ void init(int wave, int lane, int64_t st, int D) { l.init(wave, lane, st, D); }
   __device__ __forceinline__ void fetch(const char* base, int left, char* tile) { l.load(base, left, tile); }
-  __device__ __forceinline__ void commit(char*) const {}
+  __device__ __forceinline__ void share(int, int, char*) {}
 };
 
 // A step's left operand: every plane's.
@@ -316,7 +338,8 @@ struct QSet {
 // ---------------------------------------------------------------- forward
 // Two tiles are worked on at a time: the product for tile t + 1's scores runs
 // over tile t's exponentials, and the product of tile t's P and values over
-// tile t + 1's maximum. Keys are fetched two tiles ahead, values one.
+// tile t + 1's maximum. Keys are fetched two tiles ahead, values one; in fp32
+// three and two, into registers, and split under the products a tile later.
 template <int PL, int DP, bool VEC, int KS>
 __device__ __forceinline__ void fwd_set(const AttnParams& p, char (&lds)[2][2][QGeom<PL, DP, KS>::BYTES],  // keys, values
                                         const QBlocks& at, int qb) {
@@ -370,10 +393,10 @@ __device__ __forceinline__ void fwd_set(const AttnParams& p, char (&lds)[2][2][Q
   // X, masked or not; or there is none.
   auto tile = [&](auto next, auto masked, const f32x16 (&S)[N], f32x16 (&X)[N], int k0) {
     const int buf = k0 / BT & 1;
-    wait_all_barrier();
-    const bool more_v = k0 + BT < kend, more_k = k0 + 2 * BT < kend;
-    if (more_k) fetch_k(k0 + 2 * BT, buf);
-    if (more_v) fetch_v(k0 + BT, buf ^ 1);
+    if constexpr (PL == 1) wait_all_barrier();
+    else wait_lds_barrier();  // fp32 loads in flight end in registers
+    if (PL == 1 && k0 + 2 * BT < kend) fetch_k(k0 + 2 * BT, buf);
+    if (PL == 1 && k0 + BT < kend) fetch_v(k0 + BT, buf ^ 1);
     constexpr int NS = next ? N * NF : 0, NV = N * 2 * ND, PAIRS = 8 * N;
     const uint32_t K = lds_byte_addr(lds[0][buf ^ 1]) + ks * BK * RB, V = lds_byte_addr(lds[1][buf]) + ks * BK * RB;
     Frag<PL> P[N][2], ring[Gm::AHEAD];
@@ -414,19 +437,22 @@ __device__ __forceinline__ void fwd_set(const AttnParams& p, char (&lds)[2][2][Q
           t = fmaxf(t, X[e >> 4][e & 15]);
         }
       }
+      // (past the last tile: what is there, into buffers that are not read)
+      lk.share(i, NS + NV, lds[0][buf]);
+      lv.share(i, NS + NV, lds[1][buf ^ 1]);
       __builtin_amdgcn_sched_barrier(0);
     });
     if constexpr (next) follow(t);
-    if (more_k) lk.commit(lds[0][buf]);
-    if (more_v) lv.commit(lds[1][buf ^ 1]);
+    if (PL == 3 && k0 + 3 * BT < kend) fetch_k(k0 + 3 * BT, 0);
+    if (PL == 3 && k0 + 2 * BT < kend) fetch_v(k0 + 2 * BT, 0);
   };
 
   if (kend > 0) {
     using std::false_type;
     using std::true_type;
     fetch_k(0, 0);
-    lk.commit(lds[0][0]);
     fetch_v(0, 0);
+    lk.share(0, 1, lds[0][0]);
     if (BT < kend) fetch_k(BT, 1);
     wait_all_barrier();
     f32x16 S[N], X[N];
@@ -445,8 +471,10 @@ __device__ __forceinline__ void fwd_set(const AttnParams& p, char (&lds)[2][2][Q
       }
       follow(t);
     }
-    lv.commit(lds[1][0]);
-    if (BT < kend) lk.commit(lds[0][1]);
+    lv.share(0, 1, lds[1][0]);
+    lk.share(0, 1, lds[0][1]);
+    if (PL == 3 && 2 * BT < kend) fetch_k(2 * BT, 0);
+    if (PL == 3 && BT < kend) fetch_v(BT, 0);
     int k0 = 0;
     // two at a time: the scores change places without a copy
     for (; k0 + 3 * BT <= kall; k0 += 2 * BT) {
@@ -520,10 +548,6 @@ __device__ __forceinline__ void dq_set(const AttnParams& p, char (&lds)[2][2][QG
     lk.fetch(kbase + (int64_t)k0 * p.k.st * ES, set.sp.len - k0, lds[buf][0]);
     lv.fetch(vbase + (int64_t)k0 * p.v.st * ES, set.sp.len - k0, lds[buf][1]);
   };
-  auto commit = [&](int buf) {
-    lk.commit(lds[buf][0]);
-    lv.commit(lds[buf][1]);
-  };
   if (kend > 0) fetch(0, 0);
   const char* gorow = row_of(p.dout, at.b, set.qi, at.hq, ES);
   const int64_t stat = ((int64_t)at.b * p.HQ + at.hq) * p.TQ + set.qi;
@@ -539,15 +563,19 @@ __device__ __forceinline__ void dq_set(const AttnParams& p, char (&lds)[2][2][QG
   Own32<PL, DP> q, go;
   q.template load<VEC>(row_of(p.q, at.b, set.qi, at.hq, ES), set.ok, p.D, lane);
   go.template load<VEC>(gorow, set.ok, p.D, lane);
-  if (kend > 0) commit(0);
+  if (kend > 0) {
+    lk.share(0, 1, lds[0][0]);
+    lv.share(0, 1, lds[0][1]);
+    if (PL == 3 && BT < kend) fetch(BT, 0);
+  }
   const Planes<PL, DP, Gm::PLANE> left(lane);
   const float c = p.scale_log2;
   f32x16 acc[ND] = {};
   auto tile = [&](auto masked, int k0) {
     const int buf = k0 / BT & 1;
-    wait_all_barrier();
-    const bool more = k0 + BT < kend;
-    if (more) fetch(k0 + BT, buf ^ 1);
+    if constexpr (PL == 1) wait_all_barrier();
+    else wait_lds_barrier();  // fp32 loads in flight end in registers
+    if (PL == 1 && k0 + BT < kend) fetch(k0 + BT, buf ^ 1);
     constexpr int NS = N * 2 * NF, NA = N * 2 * ND;
     const uint32_t K = lds_byte_addr(lds[buf][0]) + ks * BK * RB;
     auto load = [&](auto i) {
@@ -597,9 +625,11 @@ __device__ __forceinline__ void dq_set(const AttnParams& p, char (&lds)[2][2][QG
 #pragma unroll
         for (int e = j * 8 / (2 * ND); e < (j + 1) * 8 / (2 * ND); ++e) gradient(N - 1, e);
       }
+      lk.share(i, NS + NA, lds[buf ^ 1][0]);
+      lv.share(i, NS + NA, lds[buf ^ 1][1]);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if (more) commit(buf ^ 1);
+    if (PL == 3 && k0 + 2 * BT < kend) fetch(k0 + 2 * BT, 0);
   };
   int k0 = 0;
   for (; k0 < kall; k0 += BT) tile(std::false_type{}, k0);
@@ -699,10 +729,14 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
   Stream<PL, DP, BQ, NW, VEC> lq, lo;
   lq.init(wave, lane, p.q.st, p.D);
   lo.init(wave, lane, p.dout.st, p.D);
-  auto fetch = [&](int it, int buf) {
+  const int iters = tiles * p.G;
+  auto fetch = [&](int it, int buf) {  // past the last: zeros, without a read
+    const int hq = hk * p.G + it / tiles, t0 = q_first + (tiles - 1 - it % tiles) * BQ, n = it < iters ? p.TQ - t0 : 0;
+    lq.fetch(row_of(p.q, b, t0, hq, ES), n, lds[buf][0]);
+    lo.fetch(row_of(p.dout, b, t0, hq, ES), n, lds[buf][1]);
+  };
+  auto fetch_stats = [&](int it, int buf) {
     const int hq = hk * p.G + it / tiles, t0 = q_first + (tiles - 1 - it % tiles) * BQ;
-    lq.fetch(row_of(p.q, b, t0, hq, ES), p.TQ - t0, lds[buf][0]);
-    lo.fetch(row_of(p.dout, b, t0, hq, ES), p.TQ - t0, lds[buf][1]);
     if (wave < 2 * ((BQ + 63) / 64)) {  // a 4-byte statistic a lane
       const int which = wave & 1, q = 64 * (wave >> 1) + lane;
       const float* s = p.delta + ((int64_t)which * p.B * p.HQ + (int64_t)b * p.HQ + hq) * p.TQ + t0;
@@ -711,12 +745,10 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
       dma4(r, q < BQ && q < p.TQ - t0 ? 4u * q : kOOB, lds_byte_addr(stats[buf][which]) + 256 * (wave >> 1));
     }
   };
-  auto commit = [&](int buf) {
-    lq.commit(lds[buf][0]);
-    lo.commit(lds[buf][1]);
-  };
-  const int iters = tiles * p.G;
-  if (iters > 0) fetch(0, 0);
+  if (iters > 0) {
+    fetch(0, 0);
+    fetch_stats(0, 0);
+  }
   Own32<PL, DP> k;
   k.template load<VEC>(row_of(p.k, b, krow, hk, ES), ok, p.D, lane);
   auto v = [&] {
@@ -725,7 +757,7 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
       l.init(wave, lane, p.v.st, p.D);
       if (iters > 0) {
         l.fetch(row_of(p.v, b, kb * BKV, hk, ES), sp.len - kb * BKV, vlds);
-        l.commit(vlds);
+        l.share(0, 1, vlds);
       }
       return OwnRows<PL, DP, Gm::VPLANE>(vlds, 32 * kg, lane);
     } else {
@@ -734,16 +766,24 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
       return o;
     }
   }();
-  if (iters > 0) commit(0);
+  if (iters > 0) {
+    lq.share(0, 1, lds[0][0]);
+    lo.share(0, 1, lds[0][1]);
+    if (PL == 3) fetch(1, 1);
+  }
   const Planes<PL, DP, Gm::PLANE> left(lane);
   f32x16 ak[ND] = {}, av[ND] = {};
   int it = 0, buf = 0;
   auto tile = [&](auto masked, int t0) {
-    wait_all_barrier();
+    // in fp32 the statistics go to LDS before the last tile's loads, which may
+    // be in flight still
+    if constexpr (PL == 1 || !VEC) wait_all_barrier();
+    else wait_barrier<2 * decltype(lq)::JB + 2 * decltype(lo)::JB>();
     const int now = buf;
-    const bool more = it + 1 < iters;
-    if (more) fetch(it + 1, now ^ 1);
-    ++it;
+    if (it + 1 < iters) {
+      if constexpr (PL == 1) fetch(it + 1, now ^ 1);
+      fetch_stats(it + 1, now ^ 1);
+    }
     buf ^= 1;
     const int r0 = 32 * qs;
     if (wave_on && !(masked && t0 + r0 + 32 <= wfirst)) {
@@ -806,10 +846,17 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
           for (int e = (i - 2 * NF) * 8 / NA; e < (i - 2 * NF + 1) * 8 / NA; ++e)
             put<PL>(dS[e >> 2], e & 3, dP[2 * e] * S[2 * e], dP[2 * e + 1] * S[2 * e + 1]);
         }
+        // (past the last tile: what is there, into a buffer that is not read)
+        lq.share(i, STEPS, lds[now ^ 1][0]);
+        lo.share(i, STEPS, lds[now ^ 1][1]);
         __builtin_amdgcn_sched_barrier(0);
       });
+    } else {
+      lq.share(0, 1, lds[now ^ 1][0]);
+      lo.share(0, 1, lds[now ^ 1][1]);
     }
-    if (more) commit(now ^ 1);
+    if (PL == 3) fetch(it + 2, now);
+    ++it;
   };
   // from the last query on, so that the blocks of a head read the same tiles at
   // a time whatever their first query is

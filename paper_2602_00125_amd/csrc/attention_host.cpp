@@ -173,7 +173,7 @@ mt_status check_lse(const mt_tensor* lse, const mt_tensor* q) {
 bool attn_vector_ok(const mt_tensor* const* ts, int n) {
   if (g_force_vec1) return false;
   for (int i = 0; i < n; ++i)
-    if (ts[i] && (!vector_ok(ts[i], 16) || (ts[i]->shape[1] > 1 && ts[i]->stride[1] > (1 << 22)))) return false;
+    if (ts[i] && (!vector_ok(ts[i], 16) || (ts[i]->shape[1] > 1 && ts[i]->stride[1] > (1 << 21)))) return false;
   return true;
 }
 

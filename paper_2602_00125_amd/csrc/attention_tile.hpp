@@ -56,6 +56,14 @@ __device__ __forceinline__ void wait_all_barrier() {
   __asm__ __volatile__("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+// The wave's LDS accesses and all its loads but the last N done, then every wave's.
+template <int N>
+__device__ __forceinline__ void wait_barrier() {
+  __asm__ __volatile__("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// The same with no regard to loads.
+__device__ __forceinline__ void wait_lds_barrier() { __asm__ __volatile__("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // The stream row a lane hands to the MFMA as row lane & 31 (see the top).
 __device__ __forceinline__ int tile_row(int lane) {
   const int m = lane & 31;
