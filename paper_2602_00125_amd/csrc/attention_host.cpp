@@ -135,8 +135,10 @@ mt_status check_attention(const AttnArgs& a, float scale, mt::AttnParams* p) {
   if (!(scale > 0.f) || !std::isfinite(scale)) return fail(MT_ERR_INVALID, "scale must be positive and finite");
   if (a.kv_len && (s = check_index(a.kv_len, "kv_len", B))) return s;
   if (a.q_start && (s = check_index(a.q_start, "q_start", B))) return s;
-  if (B * HQ > INT32_MAX / 2 || B * HQ * cdiv(TQ, mt::kAttnRows) > INT32_MAX / 2 ||
-      B * HK * cdiv(TK, mt::kAttnRows) > INT32_MAX / 2 || B * HQ * TQ > INT32_MAX / 64)
+  // a launch has fewer than 2^32 threads, blocks up to 512
+  const int64_t most = (1 << 23) - 8;
+  if (B * HQ > most || B * HK > most || B * HQ * cdiv(TQ, mt::kAttnRows) > most ||
+      B * HK * cdiv(TK, mt::kAttnRows) > most || B * HQ * TQ > INT32_MAX / 64)
     return fail(MT_ERR_SHAPE, "too many blocks of tokens and heads");
   *p = mt::AttnParams{};
   p->q = view(a.q);

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(256) void kernel(const DropoutParams p) {
 template <bool XB, bool YB, bool RES>
 hipError_t launch(const DropoutParams& p, bool vec, hipStream_t stream) {
   const int64_t groups = (p.M * p.N + 7) / 8, blocks = (groups + 255) / 256;
-  const dim3 grid((unsigned)(blocks < (1 << 30) ? blocks : 1 << 30));
+  const dim3 grid((unsigned)(blocks < (1 << 23) ? blocks : 1 << 23));  // a launch has fewer than 2^32 threads
   if (vec) kernel<XB, YB, RES, true><<<grid, 256, 0, stream>>>(p);
   else kernel<XB, YB, RES, false><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();

@@ -183,12 +183,16 @@ struct Lanes {
   }
 };
 
+// A launch has fewer than 2^32 threads along x: more blocks go along y.
+constexpr int64_t kMaxX = 1 << 23;
+__device__ __forceinline__ int64_t block_index() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 template <bool XB, bool YB, int VEC, int HPG>
 __global__ __launch_bounds__(256) void fwd_kernel(const HeadNormParams p) {
   Lanes ln;
   ln.init<VEC>(p);
   const int heads = p.HQ + p.HK, chunks = (heads + HPG - 1) / HPG;
-  const int64_t unit = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> p.L_shift;
+  const int64_t unit = (block_index() * 256 + threadIdx.x) >> p.L_shift;
   const int64_t tok = unit / chunks;
   if (tok >= (int64_t)p.B * p.T) return;  // whole groups leave together
   const int h0 = (int)(unit - tok * chunks) * HPG;
@@ -362,7 +366,7 @@ __device__ __forceinline__ Row<XB, YB> elem_row(const HeadNormParams& p, int64_t
 template <bool XB, bool YB>
 __global__ __launch_bounds__(256) void fwd_elem_kernel(const HeadNormParams p) {
   const int lane = threadIdx.x & 63, heads = p.HQ + p.HK;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t unit = block_index() * 4 + (threadIdx.x >> 6);
   if (unit >= (int64_t)p.B * p.T * heads) return;
   const int64_t tok = unit / heads, b = tok / p.T, t = tok - b * p.T;
   const int head = (int)(unit - tok * heads);
@@ -455,7 +459,8 @@ hipError_t head_norm_fwd(const HeadNormParams& p, bool x_bf16, bool y_bf16, int 
     const int64_t tokens = (int64_t)p.B * p.T, heads = p.HQ + p.HK;
     const int64_t units = vec ? tokens * ((heads + hpg - 1) / hpg) : tokens * heads;
     const int64_t per = vec ? 256 >> p.L_shift : 4;
-    const dim3 grid((unsigned)((units + per - 1) / per));
+    const int64_t blocks = (units + per - 1) / per, x = blocks < headnorm::kMaxX ? blocks : headnorm::kMaxX;
+    const dim3 grid((unsigned)x, (unsigned)((blocks + x - 1) / x));
     if (vec == 8 && hpg == 4) headnorm::fwd_kernel<XB, YB, 8, 4><<<grid, 256, 0, stream>>>(p);
     else if (vec == 8) headnorm::fwd_kernel<XB, YB, 8, 1><<<grid, 256, 0, stream>>>(p);
     else if (vec == 4 && hpg == 4) headnorm::fwd_kernel<XB, YB, 4, 4><<<grid, 256, 0, stream>>>(p);

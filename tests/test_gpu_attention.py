@@ -339,3 +339,29 @@ def test_replays_from_a_graph():
         torch.cuda.synchronize()
         for got, want in zip((o, lse, *grads), eager):
             assert torch.equal(got, want)
+
+
+# pitch of a token's row in elements: vectors at the longest pitch that they serve, and
+# by element past it; 1300 rows reach past 2^31 elements and 2^32 bytes
+@pytest.mark.parametrize("dtype,pitch", [("bf16", 1 << 21), ("bf16", (1 << 21) + 3), ("f32", 1 << 20), ("f32", (1 << 21) + 8)])
+def test_offsets_past_32_bits(dtype, pitch):
+    T, H, D = 1300, 2, 32
+    W = H * D
+    x = torch.empty(T * pitch, dtype=DT[dtype], device=DEV)
+    assert x.numel() * x.element_size() > 1 << 32
+    q, k, v, o, dout, dq, dk, dv = (x.as_strided((1, T, H, D), (T * pitch, pitch, D, 1), W * i) for i in range(8))
+    close = [draw((1, T, H, D), dtype, i) for i in range(4)]
+    for far, near in zip((q, k, v, dout), close):
+        far.copy_(near)
+    want_o, want_lse = forward(*close[:3], causal=True)
+    want = backward(*close[:3], want_o, want_lse, close[3], causal=True)
+    _, lse = forward(q, k, v, o, causal=True)
+    backward(q, k, v, o, lse, dout, (dq, dk, dv), causal=True)
+    few, few_lse = forward(q[:, -3:], k, v, causal=True)  # the last tokens against a long cache
+    torch.cuda.synchronize()
+    assert torch.equal(lse, want_lse) and torch.equal(o, want_o)
+    for got, near in zip((dq, dk, dv), want):
+        assert torch.equal(got, near)
+    ref = reference(close[0][:, -3:], *close[1:3], D ** -0.5, causal=True)
+    check("o", few, *ref["o"])
+    check("lse", few_lse, *ref["lse"])

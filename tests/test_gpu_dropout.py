@@ -157,3 +157,16 @@ def test_replays_from_a_graph():
         call()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
+
+
+def test_indices_past_32_bits():
+    N, tail, p = (1 << 32) + 4099, 9000, 0.4  # elements; bf16: 8.6 GB
+    at = (N - tail) // 8 * 8
+    x = torch.empty((1, N), dtype=torch.bfloat16, device=DEV)
+    y = torch.empty_like(x)
+    x[:, at:].copy_(torch.randn((1, N - at), generator=torch.Generator("cpu").manual_seed(1)))
+    b.dropout_fwd(x, None, p, 9, 3, y)
+    part = torch.empty((1, N - at), dtype=torch.bfloat16, device=DEV)
+    b.dropout_fwd(x[:, at:], None, p, 9, 3 + at // 8, part)
+    torch.cuda.synchronize()
+    assert torch.equal(y[:, at:], part)

@@ -224,3 +224,12 @@ def test_same_bits_every_time():
         b.qk_norm_rope_bwd(q, None, w, None, cos, sin, dy, None, dq, None, dw, workspace=ws)
         outs.append((dq, dw))
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+def test_more_rows_than_threads_along_a_grid():
+    T = (1 << 26) + 5  # a wave a row: 2^32 threads and some
+    x = torch.empty((1, T, 1, 1), dtype=torch.bfloat16, device=DEV).fill_(3.0)
+    y = torch.full_like(x, math.nan)
+    b.qk_norm_rope_fwd(x, None, None, None, None, None, y, None, eps=0.0)
+    torch.cuda.synchronize()
+    assert (y == 1).all()
