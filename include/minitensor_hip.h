@@ -362,14 +362,16 @@ mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt
  *   (clamped to 0 .. TK). Keys and values past it are never used, whatever
  *   they hold.
  *   q_start [B] i32 or NULL (TK - TQ, the last positions): the key position
- *   of query 0.
+ *   of query 0, any value; used with MT_CAUSAL only.
  *   scale: positive and finite, usually D^(-1/2).
  * flags: MT_CAUSAL: query i sees key j for j <= q_start + i only.
  * A query that sees no key gets o = 0 and lse = -inf, and its gradients are 0.
  * A key that some queries see should hold finite values: its infinities and
  * NaN may reach the queries near them that do not see it.
- * fp32: products and sums in fp32. bf16: products exact, sums and softmax in
- * fp32, P rounded to bf16 for its product with v. lse is from fp32 sums.
+ * Sums, softmax and lse are fp32. fp32 inputs: the products from an exact split
+ * into three bf16 parts, terms below 2^-24 of a product left out (an infinity
+ * gives NaN), or on the fp32 matrix instructions where the keys are split.
+ * bf16 inputs: products exact, P rounded to bf16 for its product with v.
  * ws: optional (mt_attention_fwd_workspace): a few queries against many keys
  * are split along the keys, the parts joined in a fixed order.
  */
@@ -391,8 +393,9 @@ mt_status mt_attention_fwd_workspace(const mt_tensor* q, const mt_tensor* k, con
  *   dv the shape and dtype of q, k, v, NULL to skip. Outputs may be views of
  *   one packed buffer. kv_len, q_start, scale and MT_CAUSAL as in the forward;
  *   dk and dv of keys past kv_len are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
- *   bf16: P and dS are rounded to bf16 for the products.
- *   ws: REQUIRED (mt_attention_bwd_workspace): delta, and partial sums.
+ *   fp32: products by the split of the forward. bf16: P and dS are rounded to
+ *   bf16 for the products. Reruns give the same bits.
+ *   ws: REQUIRED (mt_attention_bwd_workspace): two values a query and head.
  */
 mt_status mt_attention_bwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
                            const mt_tensor* kv_len, const mt_tensor* q_start, const mt_tensor* o,
