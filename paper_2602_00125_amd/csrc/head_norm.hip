@@ -12,10 +12,13 @@
 //   dx = r (e - n mean(n e))
 //
 // x is read, y (dx) written; r is computed anew in the backward, nothing is
-// kept. Bound: HBM. A row is held by L lanes (a power of two), VEC values
-// each, its sums taken across them; a group of lanes takes several heads of
-// one token, whose row of the tables and weights it reads once. Rows that do
-// not allow vectors go to a kernel of a wave a row, by element.
+// kept. Bound: HBM (4 x 4096 tokens, 40 heads of 128, bf16, 0.34 GB from HBM: 77 us
+// = 4.4 TB/s; the gradient of 8 x 1021, 32 heads of 64, fp32, 0.20 GB: 36 us and 4
+// for dw = 5.0). A row is held by L lanes (a power of two), VEC values each, its
+// sums taken across them; a group of lanes takes several heads of one token,
+// whose row of the tables and weights it reads once. Rows that do not allow
+// vectors go to a kernel of a wave a row, by element. A token a sequence costs
+// the launch (64 x 40 heads of 128: 4 us of kernel, 6 a call).
 //
 // dw: each lane keeps the sums of its columns over the rows it meets, a block
 // adds its groups' in order, and a second launch the blocks' in order.
