@@ -676,15 +676,16 @@ __global__ __launch_bounds__((256 * KS), (QGeom<PL, DP, KS>::OCC)) void dq_kerne
 // keys a block or blocks of four waves). Grids that leave CUs without a block
 // hold 64 keys a block in bf16 (6 x 777 ragged, 4 heads of 96: 41 us against 59
 // with 128). Two accumulators leave no room for both keys and values in 256
-// registers, so the values stay in LDS, but for narrow bf16 heads, which have
-// the room; wide fp32 heads take all registers of a SIMD for one wave, their LDS
+// registers, so the values stay in LDS, but for bf16 heads of up to 96, which
+// have the room (2 x 4096, 16 heads over 4 of 96, causal, gradient: 490 us against
+// 503); wide fp32 heads take all registers of a SIMD for one wave, their LDS
 // being full.
 template <int PL, int DP, int KG>
 struct KvGeom {
   using T = Tile<true, DP>;
   static constexpr int OCC = PL == 1 || DP <= 64 ? 2 : 1, QS = 4 * OCC / KG;
   static constexpr int NW = KG * QS, BQ = 32 * QS, BKV = 32 * KG;
-  static constexpr bool VLDS = PL == 1 ? DP > 64 : DP <= 64;
+  static constexpr bool VLDS = PL == 1 ? DP > 96 : DP <= 64;
   static constexpr int PLANE = BQ * T::RB, BYTES = PL * PLANE, VPLANE = BKV * T::RB;
   static constexpr int AHEAD = PL == 1 ? 4 : 2, VAHEAD = PL == 1 ? 3 : 1;
 };
