@@ -395,7 +395,8 @@ mt_status mt_attention_fwd_workspace(const mt_tensor* q, const mt_tensor* k, con
  *   dk and dv of keys past kv_len are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
  *   fp32: products by the split of the forward. bf16: P and dS are rounded to
  *   bf16 for the products. Reruns give the same bits.
- *   ws: REQUIRED (mt_attention_bwd_workspace): two values a query and head.
+ *   ws: REQUIRED (mt_attention_bwd_workspace): two values a query and head, and,
+ *   for few keys, partial sums of dk and dv.
  */
 mt_status mt_attention_bwd(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v,
                            const mt_tensor* kv_len, const mt_tensor* q_start, const mt_tensor* o,

@@ -31,11 +31,18 @@ hipError_t attn_fwd(const AttnParams& p, bool bf16, bool vec, hipStream_t stream
 // head) meet in p.part unless there is one.
 hipError_t attn_fwd_split(const AttnParams& p, bool bf16, bool vec, hipStream_t stream);
 // The dq pass (which also writes p.delta; with_dq = 0: nothing else) and the
-// dk / dv pass.
+// dk / dv pass: p.splits shares of the query tiles a block of keys, which meet in
+// p.part (2 B HK TK D floats each) unless there is one.
 hipError_t attn_bwd_dq(const AttnParams& p, bool bf16, bool vec, hipStream_t stream);
 hipError_t attn_bwd_dkv(const AttnParams& p, bool bf16, bool vec, hipStream_t stream);
 
 constexpr int kAttnRows = 128;  // queries (forward, dq) or keys (dk, dv) a block holds
 constexpr int kAttnMaxD = 128;
+
+// Keys a block of the dk / dv pass holds: in bf16 half as many where there
+// would be fewer blocks than CUs.
+inline int attn_kv_block(const AttnParams& p, bool bf16) {
+  return bf16 && (int64_t)p.B * p.HK * ((p.TK + 127) / 128) < 256 ? 64 : 128;
+}
 
 }  // namespace mt

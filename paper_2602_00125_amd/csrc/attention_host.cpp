@@ -217,6 +217,32 @@ int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
   return splits;
 }
 
+// Shares of the query tiles (of all heads of a key head) for the dk / dv pass,
+// where its blocks are fewer than the CUs: whatever is estimated shortest, in us
+// a tile and for the join. Gradients with one share and with those chosen:
+//   1 x 2048, 8 heads over 1 of 128, bf16: 251 us against 86 (8 shares), fp32: 2327
+//   against 365 (16); 1 x 512, 16 over 4 of 64, fp32: 158 against 62 (16); 1 x 71,
+//   8 over 1 of 96, fp32: 98 against 33 (24); 4 x 512, 12 over 4 of 96, bf16: 42.5
+//   against 43.1 (2), where the estimates meet.
+int choose_dkv_splits(const mt::AttnParams& p, bool bf16) {
+  const int keys = mt::attn_kv_block(p, bf16);
+  const int64_t items = (int64_t)p.B * p.HK * cdiv(p.TK, keys);
+  const int64_t tiles = p.G * cdiv(p.TQ, bf16 ? (keys == 64 ? 128 : 64) : p.D > 64 ? 32 : 64);
+  const double tile = bf16 ? 1.8 : 3.5;
+  // what a share of every key writes and the join reads, at 4 TB/s
+  const double bytes = 16.0 * p.B * p.HK * p.TK * p.D / 4e6;
+  double best = tiles * tile;
+  int splits = 1;
+  for (int64_t s = 2; s <= tiles && s * items <= 256; ++s) {
+    const double t = cdiv(tiles, s) * tile + 4.0 + (0.1 + bytes) * s;
+    if (t < best) {
+      best = t;
+      splits = (int)s;
+    }
+  }
+  return splits;
+}
+
 }  // namespace
 
 mt_status attention_fwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_tensor* v, const mt_tensor* kv_len,
@@ -278,7 +304,9 @@ mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
       return fail(MT_ERR_ALIAS, std::string(names[i]) + " overlaps kv_len or q_start");
   }
   if ((s = check_apart(outs, names, 3, ins, 6, any_overlap))) return s;
-  const size_t need = 2 * (size_t)p.B * p.HQ * p.TQ * sizeof(float);
+  const size_t stats = (2 * (size_t)p.B * p.HQ * p.TQ * sizeof(float) + 255) / 256 * 256;
+  const int splits = (dk || dv) && p.TK > 0 && stats > 0 ? choose_dkv_splits(p, q->dtype == MT_BF16) : 1;
+  const size_t need = stats + (splits > 1 ? 2 * (size_t)splits * p.B * p.HK * p.TK * p.D * sizeof(float) : 0);
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
@@ -299,6 +327,8 @@ mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
   const bool bf = q->dtype == MT_BF16, vec = attn_vector_ok(all, 8);
   (void)hipGetLastError();
   if (p.TQ > 0 && (s = hip_status(mt::attn_bwd_dq(p, bf, vec, stream)))) return s;
+  p.splits = splits;
+  p.part = (float*)((char*)ws + stats);
   if ((dk || dv) && p.TK > 0) return hip_status(mt::attn_bwd_dkv(p, bf, vec, stream));
   return MT_OK;
 }

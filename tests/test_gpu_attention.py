@@ -365,3 +365,13 @@ def test_offsets_past_32_bits(dtype, pitch):
     ref = reference(close[0][:, -3:], *close[1:3], D ** -0.5, causal=True)
     check("o", few, *ref["o"])
     check("lse", few_lse, *ref["lse"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [(1, 71, 71, 8, 1, 96), (1, 600, 600, 8, 1, 128), (2, 257, 190, 6, 2, 50), (1, 1100, 40, 3, 1, 64)])
+def test_gradients_of_few_key_blocks(dtype, case):
+    """Blocks of keys fewer than the compute units: the query tiles are shared out, some shares without a tile."""
+    B, TK = case[0], case[2]
+    run_case(dtype, *case, causal=True)
+    run_case(dtype, *case, lens=[TK // 3] * B)
+    run_case(dtype, *case, causal=True, start=[TK - 5] * B)
