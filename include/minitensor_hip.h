@@ -366,8 +366,9 @@ mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt
  *   scale: positive and finite, usually D^(-1/2).
  * flags: MT_CAUSAL: query i sees key j for j <= q_start + i only.
  * A query that sees no key gets o = 0 and lse = -inf, and its gradients are 0.
- * A key that some queries see should hold finite values: its infinities and
- * NaN may reach the queries near them that do not see it.
+ * Keys that no query of the call sees are never used either. A key that some
+ * queries see should hold finite values: its infinities and NaN may reach the
+ * queries near them that do not see it.
  * Sums, softmax and lse are fp32. fp32 inputs: the products from an exact split
  * into three bf16 parts, terms below 2^-24 of a product left out (an infinity
  * gives NaN), or on the fp32 matrix instructions where the keys are split.
@@ -392,7 +393,7 @@ mt_status mt_attention_fwd_workspace(const mt_tensor* q, const mt_tensor* k, con
  *   o and lse as the forward wrote them; dout the shape and dtype of q; dq, dk,
  *   dv the shape and dtype of q, k, v, NULL to skip. Outputs may be views of
  *   one packed buffer. kv_len, q_start, scale and MT_CAUSAL as in the forward;
- *   dk and dv of keys past kv_len are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
+ *   dk and dv of keys that no query sees are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
  *   fp32: products by the split of the forward. bf16: P and dS are rounded to
  *   bf16 for the products. Reruns give the same bits.
  *   ws: REQUIRED (mt_attention_bwd_workspace): two values a query and head, and,

@@ -912,7 +912,7 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
     store_rows<false, DP, VEC>(row(1), in, p.D, av, 1.f, !ok, false, lane);
     return;
   }
-  // keys past the batch element's length take no part: zero
+  // keys past the batch element's length or the last query's take no part: zero
   const bool write = in && (ok || !p.accumulate);
   if (p.dk.p) store_rows<PL == 1, DP, VEC>(row_of(p.dk, b, krow, hk, ES), write, p.D, ak, p.scale, !ok, p.accumulate, lane);
   if (p.dv.p) store_rows<PL == 1, DP, VEC>(row_of(p.dv, b, krow, hk, ES), write, p.D, av, 1.f, !ok, p.accumulate, lane);

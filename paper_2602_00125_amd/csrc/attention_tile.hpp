@@ -275,7 +275,9 @@ __device__ __forceinline__ int work_item(int total) {
   return (int)(blockIdx.x >> 3) < per && w < total ? w : -1;
 }
 
-// Keys of a batch element, and the key position of its query 0.
+// Keys of a batch element that any query of the call sees (what the last one
+// does: keys past them are not read, as those past the length), and the key
+// position of its query 0.
 struct Span {
   int len;
   int64_t start;
@@ -288,6 +290,10 @@ __device__ __forceinline__ Span span_of(const AttnParams& p, int b) {
     s.len = n < 0 ? 0 : n < p.TK ? n : p.TK;
   }
   s.start = p.q_start ? (int64_t)p.q_start[b] : (int64_t)p.TK - p.TQ;
+  if (p.causal) {
+    const int64_t n = s.start + p.TQ;
+    s.len = n <= 0 ? 0 : n < s.len ? (int)n : s.len;
+  }
   return s;
 }
 // How many keys query i sees (the first ones).
