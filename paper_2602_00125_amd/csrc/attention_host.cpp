@@ -314,7 +314,7 @@ mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
   if (ws && ((uintptr_t)ws & 255)) return fail(MT_ERR_WORKSPACE, "workspace must be 256-byte aligned");
   if (need > 0 && (!ws || ws_bytes < need))
     return fail(MT_ERR_WORKSPACE, "mt_attention_bwd needs the workspace that mt_attention_bwd_workspace reports");
-  if (p.B == 0 || p.HQ == 0) return MT_OK;
+  if (p.B == 0) return MT_OK;
   p.dout = view(dout);
   p.dq = view(dq);
   p.dk = view(dk);
@@ -326,10 +326,11 @@ mt_status attention_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt_te
   const mt_tensor* all[] = {q, k, v, o, dout, dq, dk, dv};
   const bool bf = q->dtype == MT_BF16, vec = attn_vector_ok(all, 8);
   (void)hipGetLastError();
-  if (p.TQ > 0 && (s = hip_status(mt::attn_bwd_dq(p, bf, vec, stream)))) return s;
+  if (p.TQ > 0 && p.HQ > 0 && (s = hip_status(mt::attn_bwd_dq(p, bf, vec, stream)))) return s;
   p.splits = splits;
   p.part = (float*)((char*)ws + stats);
-  if ((dk || dv) && p.TK > 0) return hip_status(mt::attn_bwd_dkv(p, bf, vec, stream));
+  // without queries too: dk and dv are empty sums then
+  if ((dk || dv) && p.TK > 0 && p.HK > 0) return hip_status(mt::attn_bwd_dkv(p, bf, vec, stream));
   return MT_OK;
 }
 
