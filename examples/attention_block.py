@@ -5,7 +5,8 @@
 with grouped key heads and causal attention over ragged sequences. ``AttentionBlock`` holds the parameters, every
 buffer and workspace of a training step; ``step`` runs forward, mean squared error, backward and Adam, ``decode`` one
 token of each sequence against a cache. fp32 throughout, or with bf16 products and attention (fp32 parameters, residual
-stream and statistics).
+stream and statistics): the projections' bf16 copies are made anew by every ``forward`` and after every update, and by
+``refresh`` for a program that changes the parameters by itself and goes on with ``decode``.
 
     python examples/attention_block.py [--dtype bf16] [--steps 20] [--batch 4] [--tokens 1024] ...
 """
@@ -71,6 +72,7 @@ class AttentionBlock:
         if dtype != torch.float32:
             self.x16 = torch.empty(M, C, **act)
             self.w16 = {n: torch.empty_like(self.params[n], dtype=dtype) for n in ("wqkv", "wo")}
+        self.refresh()
         kw = dict(causal=True, kv_len=torch.zeros(B, dtype=torch.int32, device=DEV))
         q32, k32, _ = self._heads(self.qkv)
         dq, dk, dv = self._heads(self.dqkv)
@@ -108,14 +110,18 @@ class AttentionBlock:
     def _cast(src, dst):
         mt.dropout_fwd(src, None, 0.0, 0, 0, dst)  # p = 0: a copy, rounded to dst's type
 
+    def refresh(self):
+        """The bf16 copies of the projections from the parameters (nothing to do in fp32)."""
+        for n, w in self.w16.items():
+            self._cast(self.params[n], w)
+
     # ---------------------------------------------------------------------- training
     def forward(self, x, kv_len):
         """x [B T, C] fp32 -> h [B T, C]; tokens from kv_len on are padding."""
         P, M = self.params, self.B * self.T
         if self.dtype != torch.float32:
             self._cast(x, self.x16)
-            for n in self.w16:
-                self._cast(P[n], self.w16[n])
+        self.refresh()
         mt.linear_fwd(self._operand("x", x), self._weight("wqkv"), P["bqkv"], self.qkv)
         q, k, _ = self._heads(self.qkv)
         mt.qk_norm_rope_fwd(q, k, P["gq"], P["gk"], self.cos, self.sin, self.q, self.k, eps=EPS)
@@ -155,6 +161,7 @@ class AttentionBlock:
         self.t += 1
         mt.adam_step(list(self.params.values()), list(self.grads.values()), list(self.m.values()), list(self.v.values()),
                      self.lr, 0.9, 0.999, 1e-8, self.t)
+        self.refresh()
 
     # ----------------------------------------------------------------------- serving
     def decode(self, x, k_cache, v_cache, lens):
