@@ -365,7 +365,8 @@ mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt
  *   of query 0, any value; used with MT_CAUSAL only.
  *   scale: positive and finite, usually D^(-1/2).
  * flags: MT_CAUSAL: query i sees key j for j <= q_start + i only.
- * A query that sees no key gets o = 0 and lse = -inf, and its gradients are 0.
+ * A query that sees no key gets o = 0 and lse = -inf, and its gradients are 0,
+ * whatever it and its dout hold; it adds nothing to the keys' gradients.
  * Keys that no query of the call sees are never used either. A key that some
  * queries see should hold finite values: its infinities and NaN may reach the
  * queries near them that do not see it.

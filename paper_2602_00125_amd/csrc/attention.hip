@@ -326,13 +326,14 @@ inline dim3 qblock_grid(const AttnParams& p) {
 // The lane's query of a set, and the keys the set sees.
 struct QSet {
   int qi, lim, kend, kall;
-  bool ok;
+  bool ok, sees;  // the query exists; and sees a key
   Span sp;
   __device__ __forceinline__ QSet(const AttnParams& p, int b, int qb, int qg, int lane, int BT) {
     sp = span_of(p, b);
     qi = qb * 128 + qg * 32 + (lane & 31);
     ok = qi < p.TQ;
     lim = ok ? visible(p, sp, qi) : 0;
+    sees = lim > 0;
     kend = __builtin_amdgcn_readfirstlane(visible(p, sp, qb * 128 + 127 < p.TQ ? qb * 128 + 127 : p.TQ - 1));
     // tiles that every query sees whole
     kall = __builtin_amdgcn_readfirstlane(visible(p, sp, qb * 128)) / BT * BT;
@@ -556,8 +557,9 @@ __device__ __forceinline__ void dq_set(const AttnParams& p, char (&lds)[2][2][QG
   if (kend > 0) fetch(0, 0);
   const char* gorow = row_of(p.dout, at.b, set.qi, at.hq, ES);
   const int64_t stat = ((int64_t)at.b * p.HQ + at.hq) * p.TQ + set.qi;
-  const float delta = sum_halves(row_dot<PL, DP, VEC>(gorow, row_of(p.o, at.b, set.qi, at.hq, ES), set.ok, p.D, lane));
-  // P = exp2(c S - lse2). A query that sees nothing has lse = -inf; all its
+  // A query that sees nothing counts as zeros, whatever it holds
+  const float delta = sum_halves(row_dot<PL, DP, VEC>(gorow, row_of(p.o, at.b, set.qi, at.hq, ES), set.sees, p.D, lane));
+  // P = exp2(c S - lse2); where a query sees nothing lse = -inf, and all its
   // keys are masked.
   const float lse = set.ok ? p.lse[stat] : 0.f, lse2 = lse * kLog2e;
   if (set.ok && lane < 32 && ks == 0) {
@@ -566,8 +568,8 @@ __device__ __forceinline__ void dq_set(const AttnParams& p, char (&lds)[2][2][QG
   }
   if (!p.with_dq) return;
   Own32<PL, DP> q, go;
-  q.template load<VEC>(row_of(p.q, at.b, set.qi, at.hq, ES), set.ok, p.D, lane);
-  go.template load<VEC>(gorow, set.ok, p.D, lane);
+  q.template load<VEC>(row_of(p.q, at.b, set.qi, at.hq, ES), set.sees, p.D, lane);
+  go.template load<VEC>(gorow, set.sees, p.D, lane);
   if (kend > 0) {
     lk.share(0, 1, lds[0][0]);
     lv.share(0, 1, lds[0][1]);
@@ -727,14 +729,16 @@ __global__ __launch_bounds__((64 * KvGeom<PL, DP, KG>::NW), (KvGeom<PL, DP, KG>:
   const int k0 = kb * BKV + kg * 32, kj = k0 + (lane & 31);
   const bool in = kj < p.TK, ok = kj < sp.len;
   const int krow = in ? kj : 0;
-  // query tiles from the first that sees a key of the block; from q_all on
-  // every query sees all of them, before wfirst none sees a key of the wave
+  // query tiles from the first that sees a key of the block, counted from the
+  // first that sees a key at all (the ones before it are not read: P = 0 would
+  // not keep their infinities and NaN out of the sums); from q_all on every
+  // query sees all of them, before wfirst none sees a key of the wave
   const bool any = kb * BKV < sp.len;
   auto first_for = [&](int key) {
     const int64_t i = p.causal ? (int64_t)key - sp.start : 0;
     return i < 0 ? 0 : i < p.TQ ? (int)i : p.TQ;
   };
-  const int q_first = any ? first_for(kb * BKV) / BQ * BQ : p.TQ;
+  const int q0 = first_for(0), q_first = any ? q0 + (first_for(kb * BKV) - q0) / BQ * BQ : p.TQ;
   const int tiles = (p.TQ - q_first + BQ - 1) / BQ;
   const int q_all = first_for(kb * BKV + BKV - 1), wfirst = first_for(k0);
   const bool wave_on = k0 < sp.len;

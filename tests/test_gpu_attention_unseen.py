@@ -1,5 +1,5 @@
 """Attention with infinities and NaN in places that take no part: keys that no query of the call sees, wherever the
-causal edge lies in a tile."""
+causal edge lies in a tile, and queries that see no key."""
 import math
 
 import pytest
@@ -42,3 +42,24 @@ def test_keys_that_no_query_sees_may_hold_anything(dtype, D, n, splits):
         for t in grads[1:]:
             for i, s in enumerate(starts):
                 assert (t[i, s + TQ:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 96, 128, 50])
+@pytest.mark.parametrize("what", ["q", "dout"])
+def test_queries_that_see_no_key_may_hold_anything(dtype, D, what):
+    """Queries before every key: o = 0, lse = -inf, no gradient, and nothing of theirs in the keys' gradients."""
+    TQ, TK = 150, 130
+    starts = (-37, -149, -150, -64, 0)
+    B = len(starts)
+    q, k, v, dout = (draw((B, t, h, D), dtype, i) for i, (t, h) in enumerate(((TQ, 4), (TK, 2), (TK, 2), (TQ, 4))))
+    kw = dict(causal=True, q_start=torch.tensor(starts, dtype=torch.int32, device=DEV))
+    ref = reference(q, k, v, D ** -0.5, dout=dout, **kw)
+    bad = q if what == "q" else dout
+    for i, s in enumerate(starts):
+        bad[i, :-s, ::2], bad[i, :-s, 1::2] = math.nan, math.inf
+    o, lse = forward(q, k, v, **kw)
+    grads = backward(q, k, v, o, lse, dout, **kw)
+    compare((o, lse, *grads), ref)
+    for i, s in enumerate(starts):
+        assert (o[i, :-s] == 0).all() and (lse[i, :, :-s] == -math.inf).all() and (grads[0][i, :-s] == 0).all()
