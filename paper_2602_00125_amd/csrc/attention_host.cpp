@@ -496,6 +496,7 @@ mt_status qk_norm_rope_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt
   p.dyk = view(dyk);
   p.yq = view(dq);
   p.yk = view(dk);
+  p.with_dx = dq != nullptr;
   p.accumulate = (flags & MT_ACCUMULATE) != 0;
   p.part = weights ? (float*)ws : nullptr;
   (void)hipGetLastError();

@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256) void bwd_kernel(const HeadNormParams p) {
         else sk[e] += gn;
         x[i][e] = r * (g[i][e] * (isq ? wq[e] : wk[e]) - n * mean);
       }
-      if (p.yq.p && ln.on && head < heads) {
+      if (p.with_dx && ln.on && head < heads) {
         char* dst = row_of(p.yq, p.yk, p.HQ, b, t, head, YE) + ln.d0 * YE;
         if (p.accumulate) {
           float old[VEC];
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(256) void bwd_elem_kernel(const HeadNormParams p) {
     }
     const float r = rsqrtf(group_sum(ss, 64) * p.inv_D + p.eps);
     const float mean = group_sum(xe, 64) * r * p.inv_D;
-    char* dst = p.yq.p ? row_of(p.yq, p.yk, p.HQ, b, t, head, YB ? 2 : 4) : nullptr;
+    char* dst = p.with_dx ? row_of(p.yq, p.yk, p.HQ, b, t, head, YB ? 2 : 4) : nullptr;
     for (int d = lane; d < p.D; d += 64) {
       const float n = load1<XB>(row.x, d) * r, g = row.g(p, d);
       sums[wave][head >= p.HQ][d] += g * n;

@@ -186,12 +186,12 @@ struct HeadView {
 constexpr int kHeadNormMaxD = 1024;
 struct HeadNormParams {
   HeadView q, k;      // x
-  HeadView yq, yk;    // forward: y; backward: dx (p == NULL: skipped)
+  HeadView yq, yk;    // forward: y; backward: dx
   HeadView dyq, dyk;  // backward
   const float *wq, *wk, *cos, *sin;  // weights may be NULL (ones)
   int64_t cos_sb, cos_st, sin_sb, sin_st;
   int32_t B, T, HQ, HK, D, R;
-  int32_t interleaved, accumulate;
+  int32_t interleaved, accumulate, with_dx;  // with_dx: the backward writes yq and yk
   int32_t L, L_shift;  // lanes a row (a power of two)
   float eps, inv_D;    // 1 / D
   float* part;  // backward: [blocks][2][D] column sums of dw, or NULL

@@ -1,9 +1,12 @@
 """Corners of attention and the head norms."""
+import math
+
 import pytest
 import torch
 
 pytestmark = pytest.mark.gpu
 
+from paper_2602_00125_amd import binding as b  # noqa: E402  (a missing library fails the module)
 from test_gpu_attention import DEV, backward, draw, forward  # noqa: E402
 
 
@@ -22,3 +25,23 @@ def test_keys_without_query_heads_have_no_gradient(dtype, causal, B, TQ, TK, HK,
         outs = (dq, *(t.clone() for t in was))
         backward(q, k, v, o, lse, dout, outs=outs, accumulate=True, causal=causal, kv_len=kv_len)
         assert torch.equal(outs[1], was[0]) and torch.equal(outs[2], was[1])
+
+
+@pytest.mark.parametrize("D", [64, 50])  # by vectors and by element
+@pytest.mark.parametrize("none", ["q", "k"])
+def test_norm_gradients_with_no_heads_on_one_side(D, none):
+    """Queries or keys of no heads, whose empty tensors have no memory: the others' gradient is what it is alone."""
+    B, T, H = 2, 21, 3
+    x, dy, w = draw((B, T, H, D), "f32", 0), draw((B, T, H, D), "f32", 1), draw((D,), "f32", 2)
+    a = 6.3 * torch.rand((B, T, D // 2), generator=torch.Generator("cpu").manual_seed(3))
+    cos, sin = a.cos().to(DEV), a.sin().to(DEV)
+    want = torch.empty_like(x)
+    b.qk_norm_rope_bwd(x, None, w, None, cos, sin, dy, None, want)
+    empty = torch.empty(B, T, 0, D, device=DEV)
+    assert empty.data_ptr() == 0
+    dx = torch.full_like(x, math.nan)
+    ins, outs = [(empty, empty), (x, dy)], [empty, dx]
+    (q, dyq), (k, dyk) = ins if none == "q" else ins[::-1]
+    dq, dk = outs if none == "q" else outs[::-1]
+    b.qk_norm_rope_bwd(q, k, w, w, cos, sin, dyq, dyk, dq, dk)
+    assert torch.equal(dx, want)
