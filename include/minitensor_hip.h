@@ -363,7 +363,7 @@ mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt
  *   they hold.
  *   q_start [B] i32 or NULL (TK - TQ, the last positions): the key position
  *   of query 0, any value; used with MT_CAUSAL only.
- *   scale: positive and finite, usually D^(-1/2).
+ *   scale: 2^-100 to 2^100, usually D^(-1/2). Scaled scores are finite floats.
  * flags: MT_CAUSAL: query i sees key j for j <= q_start + i only.
  * A query that sees no key gets o = 0 and lse = -inf, and its gradients are 0,
  * whatever it and its dout hold; it adds nothing to the keys' gradients.

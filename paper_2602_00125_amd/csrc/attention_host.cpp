@@ -132,7 +132,9 @@ mt_status check_attention(const AttnArgs& a, float scale, mt::AttnParams* p) {
   if ((s = same_heads(a.v, "v", a.k, "k"))) return s;
   if (D < 1 || D > mt::kAttnMaxD) return fail(MT_ERR_SHAPE, "the head width must be 1 to 128");
   if (HK > 0 ? HQ % HK != 0 : HQ != 0) return fail(MT_ERR_SHAPE, "the query heads must be a multiple of the key heads");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(MT_ERR_INVALID, "scale must be positive and finite");
+  // Past these lse / scale (what the dk / dv pass starts its sums from; lse is 22
+  // at most more than the largest score) or scale log2(e) might not be finite
+  if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return fail(MT_ERR_INVALID, "scale must lie in 2^-100 .. 2^100");
   if (a.kv_len && (s = check_index(a.kv_len, "kv_len", B))) return s;
   if (a.q_start && (s = check_index(a.q_start, "q_start", B))) return s;
   // a launch has fewer than 2^32 threads, blocks up to 512

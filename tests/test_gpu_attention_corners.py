@@ -45,3 +45,20 @@ def test_norm_gradients_with_no_heads_on_one_side(D, none):
     dq, dk = outs if none == "q" else outs[::-1]
     b.qk_norm_rope_bwd(q, k, w, w, cos, sin, dyq, dyk, dq, dk)
     assert torch.equal(dx, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [100, -100])
+def test_the_ends_of_the_range_of_scales(dtype, n):
+    """A scale of 2^-100 (2^100) with queries and keys of as much larger (smaller) values: powers of two change no
+    rounding, so o, lse and dv are the bits of scale 1/8, dq and dk those times the powers."""
+    B, T, HQ, HK, D = 2, 200, 4, 2, 64
+    q, k, v, dout = (draw((B, T, h, D), dtype, i) for i, h in enumerate((HQ, HK, HK, HQ)))
+    fq, fk = 2.0 ** (n // 2 - 2), 2.0 ** (n // 2 - 1)  # 2^-100 fq fk = 1 / 8
+    outs = []
+    for x, y, scale in ((q, k, 0.125), (q * fq, k * fk, 2.0 ** -n)):
+        o, lse = forward(x, y, v, scale=scale, causal=True)
+        outs.append([o, lse, *backward(x, y, v, o, lse, dout, scale=scale, causal=True)])
+    (o, lse, dq, dk, dv), (o2, lse2, dq2, dk2, dv2) = outs
+    assert torch.equal(o2, o) and torch.equal(lse2, lse) and torch.equal(dv2, dv)
+    assert torch.equal(dq2 * fq, dq) and torch.equal(dk2 * fk, dk)
