@@ -356,7 +356,9 @@ mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt
  *   q, o [B, TQ, HQ, D]; k, v [B, TK, HK, D], one dtype (f32 or bf16), any
  *   strides with each vector contiguous (memory order [B, H, T, D], packed
  *   projections and caches are views); o addresses each element once. D is 1
- *   to 128.
+ *   to 128. No size passes 2^30 - 1, and the blocks of 128 tokens of all heads
+ *   and batch elements (B HQ ceil(TQ / 128), B HK ceil(TK / 128)) are fewer than
+ *   2^23 - 7.
  *   lse [B, HQ, TQ] f32, contiguous, or NULL (the backward needs it).
  *   kv_len [B] i32 or NULL (TK): key j of batch b exists for j < kv_len[b]
  *   (clamped to 0 .. TK). Keys and values past it are never used, whatever
@@ -421,7 +423,7 @@ mt_status mt_attention_bwd_workspace(const mt_tensor* q, const mt_tensor* k, con
  * D - R values pass.
  *   q, yq [B, T, HQ, D]; k, yk [B, T, HK, D], or both NULL. q and k share a
  *   dtype, yq and yk one of their own (f32 or bf16). Strides as for attention;
- *   D is 1 to 1024.
+ *   D is 1 to 1024; B T (HQ + HK) is less than 2^30.
  *   wq, wk [D] f32 or NULL (ones).
  *   cos, sin [B, T, R / 2] f32, rows contiguous, any other strides (0: shared
  *   by the batch, or by the tokens), or both NULL (R = 0).
@@ -544,8 +546,8 @@ mt_status mt_matmul_shape(int32_t na, const int64_t* a, int32_t nb, const int64_
  * 0 a launch per sub-pixel phase, 1 = the default: one grid when large,
  * 2 always one grid); "attn_splits" (forward attention: -1 = the default,
  * automatic; 0 = blocks of 128 queries; 1..64 = 32 queries a block and so many
- * shares of the keys). Results stay within the documented accuracy for
- * every setting. */
+ * shares of the keys, fewer where a launch does not hold them). Results stay
+ * within the documented accuracy for every setting. */
 int mt_debug_set(const char* key, int64_t value);
 
 /* Static description of a status code. */

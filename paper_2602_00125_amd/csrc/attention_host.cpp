@@ -118,6 +118,9 @@ bool vector_ok(const mt_tensor* t, int bytes) {
 }
 
 // ---------------------------------------------------------------- attention
+// A launch has fewer than 2^32 threads, blocks up to 512.
+constexpr int64_t kMostBlocks = (1 << 23) - 8;
+
 struct AttnArgs {
   const mt_tensor *q, *k, *v, *kv_len, *q_start, *o, *lse;
 };
@@ -137,10 +140,8 @@ mt_status check_attention(const AttnArgs& a, float scale, mt::AttnParams* p) {
   if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) return fail(MT_ERR_INVALID, "scale must lie in 2^-100 .. 2^100");
   if (a.kv_len && (s = check_index(a.kv_len, "kv_len", B))) return s;
   if (a.q_start && (s = check_index(a.q_start, "q_start", B))) return s;
-  // a launch has fewer than 2^32 threads, blocks up to 512
-  const int64_t most = (1 << 23) - 8;
-  if (B * HQ > most || B * HK > most || B * HQ * cdiv(TQ, mt::kAttnRows) > most ||
-      B * HK * cdiv(TK, mt::kAttnRows) > most || B * HQ * TQ > INT32_MAX / 64)
+  if (B * HQ > kMostBlocks || B * HK > kMostBlocks || B * HQ * cdiv(TQ, mt::kAttnRows) > kMostBlocks ||
+      B * HK * cdiv(TK, mt::kAttnRows) > kMostBlocks)
     return fail(MT_ERR_SHAPE, "too many blocks of tokens and heads");
   *p = mt::AttnParams{};
   p->q = view(a.q);
@@ -181,6 +182,15 @@ bool attn_vector_ok(const mt_tensor* const* ts, int n) {
   return true;
 }
 
+// The most shares of the keys that the split forward can launch (0: not even
+// one): its blocks hold 32 queries, and more than one meet in a join of a block
+// of 256 threads a query and head.
+int most_attn_splits(const mt::AttnParams& p) {
+  const int64_t blocks = (int64_t)p.B * p.HK * cdiv((int64_t)p.G * p.TQ, 32);
+  if (blocks > kMostBlocks) return 0;
+  return (int64_t)p.B * p.HQ * p.TQ < 1 << 24 ? (int)std::min<int64_t>(64, kMostBlocks / blocks) : 1;
+}
+
 // Shares of the keys for the split forward, 0 for the forward by blocks of 128
 // queries: whichever is estimated shorter, in us a key from what was measured
 // (bf16 / fp32, heads of up to 64 / 128; one block a CU, then two):
@@ -190,7 +200,8 @@ bool attn_vector_ok(const mt_tensor* const* ts, int n) {
 //   16 x 1 query, 32 over 8 heads, 4096 keys, fp32: 110 us (2 shares) against
 //   757; 1 x 2000, 8 heads, fp32: 131 (1 share) against 163.
 int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
-  if (const int fs = g_attn_splits; fs >= 0) return fs;
+  const int most = most_attn_splits(p);
+  if (const int fs = g_attn_splits; fs >= 0) return std::min(fs, most);
   const int64_t whole = (int64_t)p.B * p.HQ * cdiv(p.TQ, mt::kAttnRows);
   if (whole > 512 && p.TQ > 32) return 0;
   const int64_t blocks = (int64_t)p.B * p.HK * cdiv((int64_t)p.G * p.TQ, 32);
@@ -207,7 +218,7 @@ int choose_attn_splits(const mt::AttnParams& p, bool bf16) {
   // what the shares of every row write and the join reads, at 4 TB/s
   const double bytes = 8.0 * p.B * p.HQ * p.TQ * (p.D + 2) / 4e6;
   // a share holds a tile of 32 keys a wave
-  for (int s = 1; s <= 64 && (s == 1 || s * 128 <= p.TK); ++s) {
+  for (int s = 1; s <= most && (s == 1 || s * 128 <= p.TK); ++s) {
     const double join = s > 1 ? 3.0 + (0.12 + bytes) * s : 0.0;
     const int64_t rounds = cdiv(blocks * s, slots);
     const double t = rounds * (5.0 + p.TK * round / s) * (rounds > 1 ? later : 1.0) + join;

@@ -1,10 +1,11 @@
-"""Which scales attention's validation lets through, seen from the refusal that comes next: no case passes validation, so
+"""Which sizes and scales attention's validation lets through, seen from the refusal that comes next: no case passes validation, so
 nothing is launched and no GPU is needed."""
 from helpers import load_binding
 
 b = load_binding()
 
-from test_abi_host_attention import INVALID, WS, bwd, fwd  # noqa: E402
+from test_abi_host import BF16, D, F32  # noqa: E402
+from test_abi_host_attention import ALIAS, INVALID, SHAPE, WS, bwd, fwd  # noqa: E402
 
 
 def test_scales():
@@ -14,3 +15,21 @@ def test_scales():
             assert call(scale=bad) == INVALID
     for good in (2.0 ** -100, 0.125, 1.0, 2.0 ** 100):
         assert bwd(scale=good, ws=None, ws_bytes=0) == WS
+
+
+def many(TQ, HQ, HK, TK=64, B=1, W=8):
+    """A call of many rows whose first output lies on its queries."""
+    q = D([B, TQ, HQ, W], BF16, 0x100000000000)
+    k, v = (D([B, TK, HK, W], BF16, 0x200000000000 * i) for i in (1, 2))
+    stats = D([B, HQ, TQ], F32, 0x300000000000)
+    kw = dict(q=q, k=k, v=v, o=q, lse=stats)
+    return [fwd(**kw), bwd(**kw, dout=D([B, TQ, HQ, W], BF16, 0x500000000000), dq=q, dk=None, dv=None)]
+
+
+def test_rows():
+    """Blocks of 128 tokens and heads, fewer than 2^23, are what bounds a call; its rows are not."""
+    for size in ((1 << 20, 32, 1), (1 << 24, 8, 8), ((1 << 23) * 127, 1, 1)):
+        assert many(*size) == [ALIAS, ALIAS], size
+    for size in ((1 << 30, 1, 1), (1 << 25, 32, 1), (1, 1 << 23, 1)):
+        assert many(*size) == [SHAPE, SHAPE], size
+    assert many(1, 1, 1, TK=1 << 30) == [SHAPE, SHAPE] and many(1, 1, 1, TK=(1 << 23) * 127) == [ALIAS, ALIAS]

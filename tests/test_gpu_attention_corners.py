@@ -4,10 +4,12 @@ import math
 import pytest
 import torch
 
+from attention_reference import check, reference
+
 pytestmark = pytest.mark.gpu
 
 from paper_2602_00125_amd import binding as b  # noqa: E402  (a missing library fails the module)
-from test_gpu_attention import DEV, backward, draw, forward  # noqa: E402
+from test_gpu_attention import DEV, backward, draw, forward, splits  # noqa: E402,F401
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -62,3 +64,25 @@ def test_the_ends_of_the_range_of_scales(dtype, n):
     (o, lse, dq, dk, dv), (o2, lse2, dq2, dk2, dv2) = outs
     assert torch.equal(o2, o) and torch.equal(lse2, lse) and torch.equal(dv2, dv)
     assert torch.equal(dq2 * fq, dq) and torch.equal(dk2 * fk, dk)
+
+
+@pytest.mark.parametrize("n", [-1, 3])
+def test_more_rows_than_a_launch_of_a_block_a_row_has(n, splits):
+    """32 heads of 2^20 queries: 2^25 rows, which only the join of shared-out keys could not take."""
+    splits(n)
+    TQ, TK, HQ, D = 1 << 20, 64, 32, 8
+    q, dout = (torch.randn((1, TQ, HQ, D), generator=torch.Generator(DEV).manual_seed(i), device=DEV).bfloat16() for i in range(2))
+    k, v = draw((1, TK, 1, D), "bf16", 2), draw((1, TK, 1, D), "bf16", 3)
+    o, lse = forward(q, k, v)
+    dq, dk, dv = backward(q, k, v, o, lse, dout)
+    sums = {"dk": [0.0, 0.0], "dv": [0.0, 0.0]}
+    step = 1 << 16
+    for t in range(0, TQ, step):
+        cut = slice(t, t + step)
+        ref = reference(q[:, cut], k, v, D ** -0.5, dout=dout[:, cut])
+        for name, got in (("o", o[:, cut]), ("lse", lse[:, :, cut]), ("dq", dq[:, cut])):
+            check(name, got, *ref[name])
+        for name, s in sums.items():
+            s[0], s[1] = s[0] + ref[name][0], s[1] + ref[name][1]
+    for name, got in (("dk", dk), ("dv", dv)):
+        check(name, got, *sums[name])
