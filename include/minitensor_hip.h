@@ -395,8 +395,9 @@ mt_status mt_attention_fwd_workspace(const mt_tensor* q, const mt_tensor* k, con
  *   (dk, dv summed over a key head's query heads)
  *   o and lse as the forward wrote them; dout the shape and dtype of q; dq, dk,
  *   dv the shape and dtype of q, k, v, NULL to skip. Outputs may be views of
- *   one packed buffer. kv_len, q_start, scale and MT_CAUSAL as in the forward;
- *   dk and dv of keys that no query sees are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
+ *   one packed buffer, side by side in each token's row or for each head.
+ *   kv_len, q_start, scale and MT_CAUSAL as in the forward; dk and dv of keys
+ *   that no query sees are 0. flags: MT_CAUSAL, MT_ACCUMULATE.
  *   fp32: products by the split of the forward. bf16: P and dS are rounded to
  *   bf16 for the products. Reruns give the same bits.
  *   ws: REQUIRED (mt_attention_bwd_workspace): two values a query and head, and,

@@ -47,26 +47,29 @@ mt_status check_out_heads(const mt_tensor* t, const char* name) {
 }
 
 // Whether two [B, T, H, D] views may share an element. Views of one packed
-// buffer (queries, keys and values side by side in each token's row) have
-// overlapping ranges but no common element: with equal pitches, the larger a
-// multiple of the smaller and rows that fit in it, only the places within that
-// pitch count.
-bool heads_overlap(const mt_tensor* a, const mt_tensor* b) {
-  if (!overlaps(a, b)) return false;
-  auto row_bytes = [](const mt_tensor* t) {  // what one token's heads span
-    return ((t->shape[2] - 1) * t->stride[2] + t->shape[3]) * (int64_t)elem_size(t->dtype);
+// buffer have overlapping ranges but no common element. Over the first `dims`
+// dims, with equal sizes and pitches, the larger pitches multiples of the
+// smallest, only the places within that one count: 2 dims for queries, keys and
+// values side by side in each token's row, 3 for those of each head.
+bool apart_within_pitch(const mt_tensor* a, const mt_tensor* b, int dims) {
+  auto inner_bytes = [&](const mt_tensor* t) {  // what the other dims span
+    return ((dims < 3 ? (t->shape[2] - 1) * t->stride[2] : 0) + t->shape[3]) * (int64_t)elem_size(t->dtype);
   };
   auto pitch = [](const mt_tensor* t, int d) { return t->stride[d] * (int64_t)elem_size(t->dtype); };
-  if (a->shape[0] != b->shape[0] || a->shape[1] != b->shape[1]) return true;
-  int64_t p = 0;  // the smaller pitch of batch and token
-  for (int d = 0; d < 2; ++d)
+  int64_t p = 0;
+  for (int d = 0; d < dims; ++d) {
+    if (a->shape[d] != b->shape[d]) return false;
     if (a->shape[d] > 1 && (p == 0 || pitch(a, d) < p)) p = pitch(a, d);
-  if (p == 0) return true;
-  for (int d = 0; d < 2; ++d)
-    if (a->shape[d] > 1 && (pitch(a, d) != pitch(b, d) || pitch(a, d) % p)) return true;
+  }
+  if (p == 0) return false;
+  for (int d = 0; d < dims; ++d)
+    if (a->shape[d] > 1 && (pitch(a, d) != pitch(b, d) || pitch(a, d) % p)) return false;
   int64_t at = ((int64_t)((uintptr_t)b->data - (uintptr_t)a->data)) % p;  // b's place within a's pitch
   if (at < 0) at += p;
-  return row_bytes(a) > at || at + row_bytes(b) > p;
+  return inner_bytes(a) <= at && at + inner_bytes(b) <= p;
+}
+bool heads_overlap(const mt_tensor* a, const mt_tensor* b) {
+  return overlaps(a, b) && !apart_within_pitch(a, b, 2) && !apart_within_pitch(a, b, 3);
 }
 
 // The outputs against the inputs and one another (nulls are skipped).

@@ -1,4 +1,4 @@
-"""Which sizes and scales attention's validation lets through, seen from the refusal that comes next: no case passes validation, so
+"""Which sizes, scales and packings attention's validation lets through, seen from the refusal that comes next: no case passes validation, so
 nothing is launched and no GPU is needed."""
 from helpers import load_binding
 
@@ -33,3 +33,19 @@ def test_rows():
     for size in ((1 << 30, 1, 1), (1 << 25, 32, 1), (1, 1 << 23, 1)):
         assert many(*size) == [SHAPE, SHAPE], size
     assert many(1, 1, 1, TK=1 << 30) == [SHAPE, SHAPE] and many(1, 1, 1, TK=(1 << 23) * 127) == [ALIAS, ALIAS]
+
+
+def test_heads_side_by_side_are_apart():
+    """Each head's gradients next to one another in one buffer ([B, T, H, 3, W]) pass the overlap check; views that
+    share a value, or reach into the next head, do not."""
+    B, T, H, W = 2, 6, 4, 16
+    view = lambda at, w=W, pitch=3 * W: D([B, T, H, w], F32, 0x700000 + 4 * at, [T * H * pitch, H * pitch, pitch, 1])
+    q, k, v, o, dout = (D([B, T, H, W], F32, 0x100000 * (i + 1)) for i in range(5))
+    call = lambda dq, dk, dv: bwd(q=q, k=k, v=v, o=o, dout=dout, lse=D([B, H, T], ptr=0x600000), dq=dq, dk=dk, dv=dv,
+                                  ws=None)
+    assert call(view(0), view(W), view(2 * W)) == WS
+    assert call(view(2 * W), view(0), view(W)) == WS
+    assert call(view(0), view(W - 1), view(2 * W)) == ALIAS
+    assert call(view(0), view(W), view(2 * W + 1)) == ALIAS
+    assert call(view(0), view(W, pitch=4 * W), view(2 * W)) == ALIAS
+    assert call(view(0), view(W), view(3 * W)) == ALIAS  # the next head's dq

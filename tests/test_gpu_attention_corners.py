@@ -86,3 +86,17 @@ def test_more_rows_than_a_launch_of_a_block_a_row_has(n, splits):
             s[0], s[1] = s[0] + ref[name][0], s[1] + ref[name][1]
     for name, got in (("dk", dk), ("dv", dv)):
         check(name, got, *sums[name])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_heads_of_a_packed_buffer_side_by_side(dtype):
+    """Each head's query, key and value next to one another ([B, T, H, 3, D]), the gradients laid out the same."""
+    B, T, H, D = 2, 77, 3, 64
+    qkv, dout = draw((B, T, H, 3, D), dtype, 0), draw((B, T, H, D), dtype, 1)
+    grads = torch.full_like(qkv, math.nan)
+    q, k, v = qkv.unbind(3)
+    o, lse = forward(q, k, v, causal=True)
+    backward(q, k, v, o, lse, dout, outs=grads.unbind(3), causal=True)
+    ref = reference(q, k, v, D ** -0.5, causal=True, dout=dout)
+    for name, got in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, *grads.unbind(3))):
+        check(name, got, *ref[name])
