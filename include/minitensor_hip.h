@@ -372,9 +372,11 @@ mt_status mt_reduce_broadcast_grad_workspace(const mt_tensor* grad_out, const mt
  * Keys that no query of the call sees are never used either. A key that some
  * queries see should hold finite values: its infinities and NaN may reach the
  * queries near them that do not see it.
- * Sums, softmax and lse are fp32. fp32 inputs: the products from an exact split
- * into three bf16 parts, terms below 2^-24 of a product left out (an infinity
- * gives NaN), or on the fp32 matrix instructions where the keys are split.
+ * Sums, softmax and lse are fp32. fp32 inputs: the products from a split into
+ * three bf16 parts, terms of together 2^-24 of a product left out (exact for
+ * values of 2^-110 and more, to 2^-133 below; an infinity, or a value from
+ * 3.39e38 on, gives NaN), or on the fp32 matrix instructions where the keys are
+ * split.
  * bf16 inputs: products exact, P rounded to bf16 for its product with v.
  * ws: optional (mt_attention_fwd_workspace): a few queries against many keys
  * are split along the keys, the parts joined in a fixed order.
