@@ -14,16 +14,28 @@
 // so that softmax statistics are one value a lane and P goes into the second
 // product from the registers it is in.
 //
-// Bound: the matrix cores, and beside them the softmax's vector instructions
-// (about 70 for 32 MFMAs, which take 1024 cycles of a SIMD; an exponential
-// takes 16). A wave's MFMAs are written down in order, each step's left operand
-// read from LDS a few steps before it and a share of the softmax between them;
-// left to itself the compiler reads each operand right before its MFMA once
-// registers are short. Measured on causal 4 x 4096 tokens, 32 heads over 8 of
-// 128, bf16: forward 529 us (1.04 PFLOP/s, matrix cores busy 54% of the cycles
-// at a clock of 1.9 GHz), dq 724 us (1.14, 62%), dk / dv 1031 us (1.07, 48%); no
-// LDS bank conflicts; a third buffer for the tiles changes nothing. 1 x 16384,
-// 16 heads over 4: forward 974 us (1.13).
+// Bound: the matrix cores and the softmax's vector instructions, one after the
+// other. A tile that every query sees whole takes, in bf16 at a width of 128,
+//   forward: 32 MFMAs (32 cycles of a SIMD each), 136 vector instructions (4
+//   cycles; the 32 exponentials among them 16): 1024 + 928 cycles;
+//   dq: 48 and 167 (32 exponentials): 1536 + 1052; dk / dv: 32 and 95 (16): 1024 + 572.
+// A wave's MFMAs are written down in order, each step's left operand read from
+// LDS a few steps before it and a share of the softmax between them; left to
+// itself the compiler reads each operand right before its MFMA once registers
+// are short. Measured on causal 4 x 4096 tokens, 32 heads over 8 of 128, bf16,
+// at a clock of 1.9 GHz: forward 529 to 567 us on different cards (1.04 PFLOP/s,
+// matrix cores busy 54% of the cycles), dq 726 us (1.13, 62%), dk / dv 1062 us
+// (1.04, 47%). So forward and dq take what their products and their vector
+// instructions take in turn (a tile 1900 and 2470 cycles): the two waves of a
+// SIMD hardly overlap them. dk / dv (2200 for 1596) is bound by neither. No LDS
+// bank conflicts; a third buffer for the tiles changes nothing. 1 x 16384, 16
+// heads over 4: forward 977 us (1.13).
+//
+// Registers: bf16 by vectors spills none. In fp32 dk / dv spills 6 vector
+// registers at a width of 64 and 14 at 128, where it and dq also move 80 to 150
+// registers a tile to and from accumulation registers, beside 192 and 144 MFMAs
+// (2 x 1024, 16 heads over 4 of 128, causal: matrix cores busy 27 to 28%).
+// The variants by element spill up to 97.
 //
 // fp32 values are split into three bf16 parts (PL planes: each what the ones
 // before left, rounded to nearest even), tiles on their way into LDS, P and dS in
@@ -41,10 +53,11 @@
 // operand type, an error of 2^-8 of a term where the output is rounded to bf16
 // as well. The row sum of P is taken before the rounding.
 //
-// Each result is summed by one block in a fixed order: no atomics. dq and
-// dk / dv take a pass each, and both compute S and dP (7 products in place of
-// 5): adding dq across the blocks of one pass would take atomics, or partial
-// sums of 4 bytes a d for every 128 keys, which cost more than the products.
+// Each result is summed in a fixed order, by one block or by several whose shares
+// another launch joins in order: no atomics. dq and dk / dv take a pass each, and
+// both compute S and dP (7 products in place of 5): adding dq across the blocks
+// of one pass would take atomics, or partial sums of 4 bytes a d for every 128
+// keys, which cost more than the products.
 #include <hip/hip_runtime.h>
 
 #include "attention.hpp"

@@ -8,7 +8,7 @@
 // joined in LDS, the blocks' by join_kernel, in order. Bound: HBM (16 tokens
 // against 8192 keys, 32 over 8 heads of 128: 107 us bf16 = 5.0 TB/s; against
 // 4096 keys in fp32 110 us = 4.9 TB/s, on the fp32 matrix instructions; against
-// ragged caches of 8192 keys at most, 0.34 GB in use, bf16: 73 to 78 us = 4.3 to
+// ragged caches of 8192 keys at most, 0.34 GB in use, bf16: 73 to 79 us = 4.3 to
 // 4.6 TB/s, 4 of them the join).
 #include <hip/hip_runtime.h>
 
