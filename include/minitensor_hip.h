@@ -21,8 +21,9 @@
  *     memory; its required size comes from the matching *_workspace call.
  *     A NULL workspace (or one that is too small) selects a slower variant
  *     that needs none, so workspace only ever buys speed. The exceptions need
- *     theirs: the convolution (its unfolded input), mt_attention_bwd and the
- *     weight gradients of mt_qk_norm_rope_bwd.
+ *     theirs: the convolution (its unfolded input), mt_attention_bwd, the
+ *     weight gradients of mt_qk_norm_rope_bwd and mt_layer_norm_bwd,
+ *     mt_embedding_bwd, mt_cross_entropy and mt_clip_grad_norm.
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *     All device work is enqueued on it asynchronously; results are visible
  *     after the caller synchronises that stream.
@@ -61,7 +62,7 @@ extern "C" {
 typedef enum {
   MT_F32 = 0,
   MT_BF16 = 1,
-  MT_I32 = 2  /* lengths and positions, where an entry point asks for them */
+  MT_I32 = 2  /* lengths, positions, tokens and classes, where an entry point asks for them */
 } mt_dtype;
 
 typedef enum {
@@ -479,6 +480,97 @@ mt_status mt_dropout_fwd(const mt_tensor* x, const mt_tensor* residual, float p,
  */
 mt_status mt_dropout_bwd(const mt_tensor* dy, float p, uint64_t seed, uint64_t offset,
                          const mt_tensor* dx, uint32_t flags, void* stream);
+
+/* ------------------------------------------------------------- embedding
+ * mt_embedding_fwd: y[m] = scale table[ids[m]], for tokens in row-major order.
+ *   ids    [M] or [B, T] (M = B T) i32, any strides; fewer than 2^30 tokens
+ *   table  [V, D], y [M, D]  f32 or bf16 each; any row pitch, rows contiguous;
+ *          D up to 2^20
+ * A token outside 0 .. V-1 (padding) gets a row of zeros. The product is fp32,
+ * rounded to y's type once. scale is finite.
+ */
+mt_status mt_embedding_fwd(const mt_tensor* ids, const mt_tensor* table, float scale,
+                           const mt_tensor* y, void* stream);
+
+/* mt_embedding_bwd: the table's gradient from dy (the add pullback through
+ * the lookup):
+ *   dtable[v] = scale sum of dy[m] over the m with ids[m] = v
+ *   dy [M, D] f32 or bf16; dtable [V, D] f32. Rows without a token become 0,
+ *   or with MT_ACCUMULATE stay as they are and the others are added to. Rows
+ *   of dy whose token is outside 0 .. V-1 are not read.
+ *   Up to 2^26 tokens, V up to 2^24. Sums are fp32, in one order for given ids.
+ *   ws: REQUIRED (mt_embedding_bwd_workspace): the tokens sorted by id, and the
+ *   partial sums of ids that many tokens share.
+ */
+mt_status mt_embedding_bwd(const mt_tensor* ids, const mt_tensor* dy, float scale,
+                           const mt_tensor* dtable, uint32_t flags, void* ws, size_t ws_bytes,
+                           void* stream);
+mt_status mt_embedding_bwd_workspace(const mt_tensor* ids, const mt_tensor* dy,
+                                     const mt_tensor* dtable, size_t* bytes);
+
+/* ------------------------------------------------------------ layer norm
+ * mt_layer_norm_fwd: each row x of C values
+ *   y = n w + b,   n = (x - mean x) / sqrt(var x + eps),
+ * var the mean of (x - mean x)^2.
+ *   x, y [M, C] f32 or bf16 each, any row pitch, rows contiguous; C is 1 to 16384
+ *   w, b [C] f32, or NULL (ones, zeros); eps >= 0
+ * Arithmetic is fp32; y is rounded once.
+ */
+mt_status mt_layer_norm_fwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* b, float eps,
+                            const mt_tensor* y, void* stream);
+
+/* mt_layer_norm_bwd: its gradients from dy, the statistics computed again from
+ * x. With r = 1 / sqrt(var x + eps), n as above and g = dy w:
+ *   dx = r (g - mean g - n mean(g n));   dw = sum over rows of dy n;
+ *   db = sum over rows of dy
+ *   dy [M, C] f32 or bf16; dx [M, C] of dy's type; dw, db [C] f32; outputs may
+ *   be NULL (not all). flags: MT_ACCUMULATE, for all three.
+ *   ws: required for dw and db (mt_layer_norm_bwd_workspace): partial sums.
+ */
+mt_status mt_layer_norm_bwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy, float eps,
+                            const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db,
+                            uint32_t flags, void* ws, size_t ws_bytes, void* stream);
+mt_status mt_layer_norm_bwd_workspace(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy,
+                                      const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db,
+                                      size_t* bytes);
+
+/* --------------------------------------------------------- cross-entropy
+ * mt_cross_entropy: the cross-entropy of each row's softmax against its class
+ * (Sec. 3.3 Eq. (8)) and its gradient. Over the rows m whose class t is one of
+ * 0 .. V-1 (they count; n is their number):
+ *   losses[m] = log sum_v exp z[m][v] - z[m][t];   loss = their sum / n
+ *   dlogits[m][v] = (softmax(z[m])[v] - [v = t]) / n
+ * Rows whose class is outside 0 .. V-1 (padding) are not read; their loss and
+ * gradient are 0. With no row that counts, loss is 0.
+ *   logits [M, V], dlogits [M, V] f32 or bf16 each, any row pitch, rows
+ *   contiguous; V is 1 to 2^24
+ *   targets [M] or [B, T] (M = B T) i32, any strides
+ *   loss: f32, one element; losses [M] f32. Outputs may be NULL (not all).
+ * A logit of -infinity has probability 0 (a class that is -infinity itself has
+ * loss +infinity). A row whose logits are all -infinity, or hold +infinity or
+ * NaN, has NaN as its loss and gradient. Arithmetic is fp32.
+ * ws: REQUIRED (mt_cross_entropy_workspace): n, and the rows' losses.
+ */
+mt_status mt_cross_entropy(const mt_tensor* logits, const mt_tensor* targets, const mt_tensor* loss,
+                           const mt_tensor* losses, const mt_tensor* dlogits, void* ws,
+                           size_t ws_bytes, void* stream);
+mt_status mt_cross_entropy_workspace(const mt_tensor* logits, const mt_tensor* targets,
+                                     size_t* bytes);
+
+/* -------------------------------------------------------------- clipping
+ * mt_clip_grad_norm: the norm over n gradients together, and all of them
+ * scaled where it passes max_norm (>= 0; infinity: the norm alone):
+ *   norm = sqrt(sum over all tensors of g^2);   out = g min(1, max_norm / norm)
+ * grads: n tensors, f32 or bf16 each, contiguous, any rank. out: n tensors of
+ * their shapes, f32 or bf16 each, contiguous, overlapping nothing; or NULL: the
+ * gradients are scaled in place (and not written where nothing is clipped).
+ * norm: f32, one element, or NULL. Squares are formed and added in 64 bits. A
+ * norm that is not finite clips nothing: the caller reads it from norm.
+ * ws: REQUIRED (mt_clip_grad_norm_workspace): partial sums.
+ */
+mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+                            const mt_tensor* norm, void* ws, size_t ws_bytes, void* stream);
+mt_status mt_clip_grad_norm_workspace(int32_t n, const mt_tensor* grads, size_t* bytes);
 
 /* ------------------------------------------------------- workspace query
  * mt_workspace_bytes: the workspace size of one call, by operation, with the

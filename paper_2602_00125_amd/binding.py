@@ -45,7 +45,9 @@ EXPORTS = ["mt_linear_fwd", "mt_linear_bwd", "mt_linear_bwd_workspace", "mt_matm
            "mt_conv2d_fwd", "mt_conv2d_fwd_workspace", "mt_conv2d_bwd", "mt_conv2d_bwd_workspace",
            "mt_workspace_bytes", "mt_linear_bwd_noalloc", "mt_attention_fwd", "mt_attention_fwd_workspace",
            "mt_attention_bwd", "mt_attention_bwd_workspace", "mt_qk_norm_rope_fwd", "mt_qk_norm_rope_bwd",
-           "mt_qk_norm_rope_bwd_workspace", "mt_dropout_fwd", "mt_dropout_bwd"]
+           "mt_qk_norm_rope_bwd_workspace", "mt_dropout_fwd", "mt_dropout_bwd", "mt_embedding_fwd", "mt_embedding_bwd",
+           "mt_embedding_bwd_workspace", "mt_layer_norm_fwd", "mt_layer_norm_bwd", "mt_layer_norm_bwd_workspace",
+           "mt_cross_entropy", "mt_cross_entropy_workspace", "mt_clip_grad_norm", "mt_clip_grad_norm_workspace"]
 NOALLOC_SCRATCH_BYTES = 32 << 20  # MT_NOALLOC_SCRATCH_BYTES
 NUM_GEMM_CFG = 19  # tile configurations mt_debug_set("cfg", i) accepts
 ACT = {"none": 0, "relu": 1, "sigmoid": 2, "tanh": 3, "gelu": 4}
@@ -95,6 +97,16 @@ lib.mt_qk_norm_rope_bwd_workspace.argtypes = [_P] * 12 + [ctypes.POINTER(_sz)]
 _u64 = ctypes.c_uint64
 lib.mt_dropout_fwd.argtypes = [_P, _P, _f, _u64, _u64, _P, _vp]
 lib.mt_dropout_bwd.argtypes = [_P, _f, _u64, _u64, _P, _u32, _vp]
+lib.mt_embedding_fwd.argtypes = [_P, _P, _f, _P, _vp]
+lib.mt_embedding_bwd.argtypes = [_P, _P, _f, _P, _u32, _vp, _sz, _vp]
+lib.mt_embedding_bwd_workspace.argtypes = [_P, _P, _P, ctypes.POINTER(_sz)]
+lib.mt_layer_norm_fwd.argtypes = [_P, _P, _P, _f, _P, _vp]
+lib.mt_layer_norm_bwd.argtypes = [_P, _P, _P, _f, _P, _P, _P, _u32, _vp, _sz, _vp]
+lib.mt_layer_norm_bwd_workspace.argtypes = [_P] * 6 + [ctypes.POINTER(_sz)]
+lib.mt_cross_entropy.argtypes = [_P] * 5 + [_vp, _sz, _vp]
+lib.mt_cross_entropy_workspace.argtypes = [_P, _P, ctypes.POINTER(_sz)]
+lib.mt_clip_grad_norm.argtypes = [_i32, _P, _f, _P, _P, _vp, _sz, _vp]
+lib.mt_clip_grad_norm_workspace.argtypes = [_i32, _P, ctypes.POINTER(_sz)]
 lib.mt_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.POINTER(_P), ctypes.c_int32]
 lib.mt_debug_set.argtypes = [ctypes.c_char_p, ctypes.c_int64]
 lib.mt_status_str.argtypes = [ctypes.c_int]
@@ -135,14 +147,14 @@ def raw_desc(ptr: int, dtype: int, shape, stride) -> MtTensor:
 
 
 def desc(t: torch.Tensor | None, index: bool = False):
-    """The descriptor of a tensor (index: one of int32 lengths or positions)."""
+    """The descriptor of a tensor (index: one of int32 lengths, positions, tokens or classes)."""
     if t is None:
         return None
     if not t.is_cuda:
         raise ValueError("libminitensor_hip works on device tensors (got a CPU tensor)")
     if index:
         if t.dtype != torch.int32:
-            raise TypeError(f"lengths and positions are int32 (got {t.dtype})")
+            raise TypeError(f"lengths, positions, tokens and classes are int32 (got {t.dtype})")
         dt = I32
     elif t.dtype == torch.float32:
         dt = F32
@@ -404,6 +416,70 @@ def dropout_fwd(x, residual, p, seed, offset, y, stream=None) -> None:
 def dropout_bwd(dy, p, seed, offset, dx, accumulate=False, stream=None) -> None:
     """dx = dy with the forward's mask and scale."""
     _check(_m.dropout_bwd(dy, p, seed, offset, dx, ACCUMULATE if accumulate else 0, stream), "mt_dropout_bwd")
+
+
+def embedding_fwd(ids, table, y, scale=1.0, stream=None) -> None:
+    """y [M, D] = scale table[ids] for int32 tokens ids [M] or [B, T] (M = B T); tokens that are no row of table
+    [V, D] (padding, such as -1) get zeros."""
+    _check(_m.embedding_fwd(ids, table, scale, y, stream), "mt_embedding_fwd")
+
+
+def embedding_bwd_workspace(ids, dy, dtable) -> int:
+    n = _sz(0)
+    _check(lib.mt_embedding_bwd_workspace(_ref(desc(ids, True)), _ref(desc(dy)), _ref(desc(dtable)), ctypes.byref(n)),
+           "mt_embedding_bwd_workspace")
+    return int(n.value)
+
+
+def embedding_bwd(ids, dy, dtable, scale=1.0, accumulate=False, workspace=None, stream=None) -> None:
+    """dtable[v] (fp32) = scale times the sum of dy's rows whose token is v; needs the workspace."""
+    _check(_m.embedding_bwd(ids, dy, scale, dtable, ACCUMULATE if accumulate else 0, workspace, stream),
+           "mt_embedding_bwd")
+
+
+def layer_norm_fwd(x, w, b, y, eps=1e-5, stream=None) -> None:
+    """y = (x - mean) / sqrt(var + eps) w + b over the rows of x [M, C] (w, b fp32 [C] or None)."""
+    _check(_m.layer_norm_fwd(x, w, b, eps, y, stream), "mt_layer_norm_fwd")
+
+
+def layer_norm_bwd_workspace(x, w, dy, dx=None, dw=None, db=None) -> int:
+    n = _sz(0)
+    _check(lib.mt_layer_norm_bwd_workspace(*[_ref(desc(t)) for t in (x, w, dy, dx, dw, db)], ctypes.byref(n)),
+           "mt_layer_norm_bwd_workspace")
+    return int(n.value)
+
+
+def layer_norm_bwd(x, w, dy, dx=None, dw=None, db=None, eps=1e-5, accumulate=False, workspace=None,
+                   stream=None) -> None:
+    """The gradients of layer_norm_fwd (None skips one); dw and db need the workspace."""
+    _check(_m.layer_norm_bwd(x, w, dy, eps, dx, dw, db, ACCUMULATE if accumulate else 0, workspace, stream),
+           "mt_layer_norm_bwd")
+
+
+def cross_entropy_workspace(logits, targets) -> int:
+    n = _sz(0)
+    _check(lib.mt_cross_entropy_workspace(_ref(desc(logits)), _ref(desc(targets, True)), ctypes.byref(n)),
+           "mt_cross_entropy_workspace")
+    return int(n.value)
+
+
+def cross_entropy(logits, targets, loss=None, losses=None, dlogits=None, workspace=None, stream=None) -> None:
+    """The mean cross-entropy of logits [M, V] against int32 classes (loss, one element), each row's (losses [M]) and
+    the mean's gradient (dlogits); rows whose class is none of 0 .. V-1 do not count. Needs the workspace."""
+    _check(_m.cross_entropy(logits, targets, loss, losses, dlogits, workspace, stream), "mt_cross_entropy")
+
+
+def clip_grad_norm_workspace(grads) -> int:
+    n = _sz(0)
+    ds = (MtTensor * max(1, len(grads)))(*[desc(t) for t in grads])
+    _check(lib.mt_clip_grad_norm_workspace(len(grads), ds, ctypes.byref(n)), "mt_clip_grad_norm_workspace")
+    return int(n.value)
+
+
+def clip_grad_norm(grads, max_norm, norm=None, out=None, workspace=None, stream=None) -> None:
+    """The norm over a list of gradients together (norm, one element), and the gradients times min(1, max_norm / norm)
+    in the tensors of out, or in place where out is None. Needs the workspace."""
+    _check(_m.clip_grad_norm(grads, out, max_norm, norm, workspace, stream), "mt_clip_grad_norm")
 
 
 def _shape_call(fn, a, b, where):

@@ -1,7 +1,8 @@
 // C-ABI of libminitensor_hip: argument validation, shape planning and kernel
 // dispatch (the convolution's lives in conv_host.cpp; that of attention, the
-// head norms and dropout in attention_host.cpp). Declarations and their
-// contracts: include/minitensor_hip.h.
+// head norms and dropout in attention_host.cpp; that of the embedding, the
+// layer norm, the cross-entropy loss and clipping in language_host.cpp).
+// Declarations and their contracts: include/minitensor_hip.h.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -1377,6 +1378,97 @@ mt_status mt_dropout_bwd(const mt_tensor* dy, float p, uint64_t seed, uint64_t o
   }
 }
 
+mt_status mt_embedding_fwd(const mt_tensor* ids, const mt_tensor* table, float scale, const mt_tensor* y, void* stream) {
+  try {
+    return embedding_fwd_impl(ids, table, scale, y, (hipStream_t)stream);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_embedding_bwd(const mt_tensor* ids, const mt_tensor* dy, float scale, const mt_tensor* dtable,
+                           uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    return embedding_bwd_impl(ids, dy, scale, dtable, flags, ws, ws_bytes, (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_embedding_bwd_workspace(const mt_tensor* ids, const mt_tensor* dy, const mt_tensor* dtable, size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return embedding_bwd_impl(ids, dy, 1.f, dtable, 0, nullptr, 0, nullptr, bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_layer_norm_fwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* b, float eps, const mt_tensor* y,
+                            void* stream) {
+  try {
+    return layer_norm_fwd_impl(x, w, b, eps, y, (hipStream_t)stream);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_layer_norm_bwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy, float eps, const mt_tensor* dx,
+                            const mt_tensor* dw, const mt_tensor* db, uint32_t flags, void* ws, size_t ws_bytes,
+                            void* stream) {
+  try {
+    return layer_norm_bwd_impl(x, w, dy, eps, dx, dw, db, flags, ws, ws_bytes, (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_layer_norm_bwd_workspace(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy, const mt_tensor* dx,
+                                      const mt_tensor* dw, const mt_tensor* db, size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return layer_norm_bwd_impl(x, w, dy, 0.f, dx, dw, db, 0, nullptr, 0, nullptr, bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_cross_entropy(const mt_tensor* logits, const mt_tensor* targets, const mt_tensor* loss,
+                           const mt_tensor* losses, const mt_tensor* dlogits, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    return cross_entropy_impl(logits, targets, loss, losses, dlogits, ws, ws_bytes, (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_cross_entropy_workspace(const mt_tensor* logits, const mt_tensor* targets, size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return cross_entropy_impl(logits, targets, nullptr, nullptr, nullptr, nullptr, 0, nullptr, bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+                            const mt_tensor* norm, void* ws, size_t ws_bytes, void* stream) {
+  try {
+    return clip_grad_norm_impl(n, grads, max_norm, out, norm, ws, ws_bytes, (hipStream_t)stream, nullptr);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
+mt_status mt_clip_grad_norm_workspace(int32_t n, const mt_tensor* grads, size_t* bytes) {
+  try {
+    if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
+    return clip_grad_norm_impl(n, grads, 0.f, nullptr, nullptr, nullptr, 0, nullptr, bytes);
+  } catch (...) {
+    return fail(MT_ERR_INVALID, "internal error");
+  }
+}
+
 mt_status mt_linear_bwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy,
                         const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db,
                         uint32_t flags, void* ws, size_t ws_bytes, void* stream) {
@@ -1613,4 +1705,5 @@ int mt_debug_set(const char* key, int64_t value) {
 #ifndef MT_SEPARATE_UNITS
 // one object for the host code: a build that does not compile this on its own
 #include "attention_host.cpp"
+#include "language_host.cpp"
 #endif

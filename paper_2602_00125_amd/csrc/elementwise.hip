@@ -399,6 +399,10 @@ hipError_t rmsprop_step(const OptBatch& b, float lr, float alpha, float eps, hip
 // one object for these kernels: a build that does not compile them on their own
 #include "attention.hip"
 #include "attention_split.hip"
+#include "cross_entropy.hip"
 #include "dropout.hip"
+#include "embedding.hip"
+#include "grad_clip.hip"
 #include "head_norm.hip"
+#include "layer_norm.hip"
 #endif

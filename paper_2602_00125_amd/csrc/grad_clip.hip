@@ -1,0 +1,117 @@
+// The norm over the gradients of all parameters and their clipping, gfx950:
+//
+//   N = (sum over tensors of g^2)^(1/2),   out = g min(1, max_norm / N)
+//
+// Squares are formed and added in 64 bits: no finite gradient overflows or
+// vanishes in them, and the sum of hundreds of millions of values keeps its
+// digits. Bound: HBM (the conversions and products of 64 bits are a tenth of the
+// time that the loads take).
+//
+// Two launches for each 120 tensors. norm_kernel: blocks take the chunks of the
+// tensors in turn and write a partial sum each. scale_kernel: every block adds
+// all partial sums in one order, so that all find the same factor, and takes the
+// chunks again, the last first: those are in the caches. In place and with
+// nothing to clip it ends there.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "language.hpp"
+
+namespace mt {
+namespace clip {
+
+using namespace vio;
+
+// The tensor that chunk c belongs to; the same in every lane.
+__device__ __forceinline__ int tensor_of(const ClipBatch& b, int c) {
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kClipTensors; i += 64) n += __popcll(__ballot(i + lane < b.n && b.start[i + lane] <= c));
+  return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+// The 256 threads' values added by a fixed tree.
+__device__ __forceinline__ double block_sum(double v, double* red) {
+  red[threadIdx.x] = v;
+  __syncthreads();
+  for (int w = 128; w > 0; w >>= 1) {
+    if ((int)threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
+    __syncthreads();
+  }
+  return red[0];
+}
+
+constexpr int kPer = kClipChunk / 256;  // values a thread of a chunk
+
+// f(i, n, values): the thread's values of a chunk by eights, the first n of which
+// exist.
+template <bool BF, typename F>
+__device__ __forceinline__ void chunk(const void* src, int64_t c0, int64_t numel, F f) {
+  float v[kPer / 8][8];
+  const int n = (int)min(numel - c0, (int64_t)kClipChunk), at = (int)threadIdx.x * 8;
+#pragma unroll
+  for (int j = 0; j < kPer / 8; ++j) load_some<BF, 8>(src, c0 + at + j * 2048, n - at - j * 2048, 0.f, v[j]);
+#pragma unroll
+  for (int j = 0; j < kPer / 8; ++j) f(c0 + at + j * 2048, n - at - j * 2048, v[j]);
+}
+
+__global__ __launch_bounds__(256) void norm_kernel(const ClipBatch b, double* part) {
+  __shared__ double red[256];
+  double sum = 0.0;
+  auto add = [&](int64_t, int, const float (&v)[8]) {
+    for (float x : v) sum = fma((double)x, (double)x, sum);
+  };
+  for (int c = blockIdx.x; c < b.start[b.n]; c += gridDim.x) {
+    const int t = tensor_of(b, c);
+    const int64_t c0 = (int64_t)(c - b.start[t]) * kClipChunk;
+    if (b.kind[t] & 1) chunk<true>(b.src[t], c0, b.numel[t], add);
+    else chunk<false>(b.src[t], c0, b.numel[t], add);
+  }
+  sum = block_sum(sum, red);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(256) void scale_kernel(const ClipBatch b, const double* part, int parts, float max_norm, float* out_norm) {
+  __shared__ double red[256];
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
+  const double norm = sqrt(block_sum(sum, red));
+  if (out_norm && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = (float)norm;
+  // a norm that is not finite clips nothing
+  const bool clips = norm > (double)max_norm && norm < (double)INFINITY;
+  const float f = clips ? (float)((double)max_norm / norm) : 1.f;
+  for (int c = b.start[b.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+    const int t = tensor_of(b, c);
+    if (!clips && b.src[t] == b.dst[t]) continue;
+    const int64_t c0 = (int64_t)(c - b.start[t]) * kClipChunk;
+    void* dst = b.dst[t];
+    const bool to_bf = b.kind[t] & 2;
+    auto put = [&](int64_t i, int n, float (&v)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= f;
+      if (to_bf) store_some<true, 8>(dst, i, n, v);
+      else store_some<false, 8>(dst, i, n, v);
+    };
+    if (b.kind[t] & 1) chunk<true>(b.src[t], c0, b.numel[t], put);
+    else chunk<false>(b.src[t], c0, b.numel[t], put);
+  }
+}
+
+}  // namespace clip
+
+int clip_blocks(int64_t chunks) { return (int)std::min<int64_t>(chunks, 2048); }
+
+hipError_t clip_norm(const ClipBatch& b, double* part, int blocks, hipStream_t stream) {
+  clip::norm_kernel<<<dim3((unsigned)blocks), 256, 0, stream>>>(b, part);
+  return hipGetLastError();
+}
+
+hipError_t clip_scale(const ClipBatch& b, const double* part, int parts, float max_norm, float* norm, int blocks,
+                      hipStream_t stream) {
+  clip::scale_kernel<<<dim3((unsigned)blocks), 256, 0, stream>>>(b, part, parts, max_norm, norm);
+  return hipGetLastError();
+}
+
+}  // namespace mt

@@ -84,4 +84,21 @@ mt_status qk_norm_rope_bwd_impl(const mt_tensor* q, const mt_tensor* k, const mt
 mt_status dropout_impl(const mt_tensor* x, const mt_tensor* residual, float p, uint64_t seed, uint64_t offset,
                        const mt_tensor* y, uint32_t flags, bool backward, hipStream_t stream);
 
+// the bodies of the embedding, the layer norm, the cross-entropy loss and
+// clipping (language_host.cpp); ws_query as above
+mt_status embedding_fwd_impl(const mt_tensor* ids, const mt_tensor* table, float scale, const mt_tensor* y,
+                             hipStream_t stream);
+mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float scale, const mt_tensor* dtable,
+                             uint32_t flags, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query);
+mt_status layer_norm_fwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_tensor* b, float eps,
+                              const mt_tensor* y, hipStream_t stream);
+mt_status layer_norm_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy, float eps,
+                              const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db, uint32_t flags, void* ws,
+                              size_t ws_bytes, hipStream_t stream, size_t* ws_query);
+mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, const mt_tensor* loss,
+                             const mt_tensor* losses, const mt_tensor* dlogits, void* ws, size_t ws_bytes,
+                             hipStream_t stream, size_t* ws_query);
+mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+                              const mt_tensor* norm, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query);
+
 }  // namespace mt::host

@@ -1,0 +1,98 @@
+// Kernels of the embedding, the layer norm, the cross-entropy loss and the
+// clipping of gradients (embedding.hip, layer_norm.hip, cross_entropy.hip,
+// grad_clip.hip), as their host code (language_host.cpp) launches them.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "vector_io.hpp"
+
+namespace mt {
+
+// y[m] = scale table[ids[m]], rows of zeros for ids outside 0 .. V-1.
+struct EmbeddingParams {
+  vio::Index ids;
+  const void* table;
+  void* y;
+  int64_t M, V, D, ldt, ldy;
+  float scale;
+};
+hipError_t embedding_fwd(const EmbeddingParams& p, bool t_bf16, bool y_bf16, hipStream_t stream);
+
+// Its gradient. ws holds the tokens grouped by id and the sums of runs that
+// chunks cut.
+struct EmbeddingGradParams {
+  vio::Index ids;
+  const void* dy;
+  float* dtable;
+  int64_t M, V, D, ldy, ldt;
+  float scale;
+  int accumulate;
+  int32_t chunk, chunks;       // tokens of a chunk, chunks of M tokens
+  int32_t bucket_shift;        // 2^bucket_shift buckets: the low bits of an id
+  int32_t* total;              // tokens with an id in range
+  int32_t *id, *pos;           // [M]: ids grouped, and the tokens they come from
+  float *head, *tail;          // [chunks][D]: a run that began before the chunk; one that ends after it
+};
+constexpr int kEmbedBucketIds = 1024;  // ids of a bucket, at most
+hipError_t embedding_bwd(const EmbeddingGradParams& p, bool bf16, hipStream_t stream);
+
+constexpr int kLayerNormMaxC = 16384;
+struct LayerNormParams {
+  const void *x, *dy;
+  const float *w, *b;
+  void* out;  // y, or dx (NULL: none)
+  float* part;  // backward: [blocks][2][C] sums of dw and db, or NULL
+  int64_t M, ldx, ldd, ldo;
+  int32_t C, L, L_shift;  // L lanes a row (a power of two)
+  int32_t accumulate;
+  float eps, C_f;  // C as a float: means are quotients, so that rows of one value have exact ones
+};
+// nv: groups of values (8 where a side is bf16, else 4) a lane holds, 16 values
+// at most; threads of a block, blocks.
+hipError_t layer_norm_fwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, int nv, int threads, int blocks,
+                          hipStream_t stream);
+hipError_t layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, int nv, int threads, int blocks,
+                          hipStream_t stream);
+hipError_t layer_norm_finish(const float* part, int parts, int C, float* dw, float* db, bool add, hipStream_t stream);
+
+// Cross-entropy: row_loss[m] = lse_m - z[m][t], dz = (softmax - onehot) / n.
+struct CrossEntropyParams {
+  const void* z;
+  void* dz;  // or NULL
+  vio::Index targets;
+  float* row_loss;
+  const int32_t* counted;  // n, or NULL where nothing needs it
+  int64_t M, ldz, ldd;
+  int32_t V;
+};
+// How a row is held (cross_entropy.hip).
+struct CrossEntropyForm {
+  int32_t threads, values;  // values a thread holds; 0: none, the row is read twice
+  int32_t L, L_shift;            // lanes a row where a wave holds several, else 0
+};
+hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, int32_t* counted, hipStream_t stream);
+hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16,
+                              hipStream_t stream);
+hipError_t cross_entropy_mean(const float* row_loss, int64_t M, const int32_t* counted, float* loss, hipStream_t stream);
+
+// Up to kClipTensors tensors of a launch, cut into chunks of kClipChunk values.
+constexpr int kClipTensors = 120;
+constexpr int kClipChunk = 4096;
+struct ClipBatch {
+  const void* src[kClipTensors];
+  void* dst[kClipTensors];
+  int64_t numel[kClipTensors];
+  int32_t start[kClipTensors + 1];  // chunks before tensor i
+  int8_t kind[kClipTensors];        // 1: src is bf16, 2: dst is bf16
+  int32_t n;
+};
+// part[block] = the block's sum of squares; blocks <= clip_blocks(chunks).
+int clip_blocks(int64_t chunks);
+hipError_t clip_norm(const ClipBatch& b, double* part, int blocks, hipStream_t stream);
+// norm = sqrt of the parts' sum (where not NULL); dst = src min(1, max_norm / norm).
+hipError_t clip_scale(const ClipBatch& b, const double* part, int parts, float max_norm, float* norm, int blocks,
+                      hipStream_t stream);
+
+}  // namespace mt

@@ -1,0 +1,421 @@
+// Argument validation and dispatch of the embedding, the layer norm, the
+// cross-entropy loss and the clipping of gradients. Contracts:
+// include/minitensor_hip.h.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+#include <vector>
+
+#include "host.hpp"
+#include "language.hpp"
+
+namespace mt::host {
+namespace {
+
+constexpr int64_t kMostRows = (int64_t)1 << 30;
+
+// Rank 1 or 2, any strides: tokens or classes.
+mt_status check_ids(const mt_tensor* t, const char* name, mt::vio::Index* out, int64_t* count) {
+  if (!t) return fail(MT_ERR_NULL, std::string(name) + ": null tensor descriptor");
+  if (t->ndim < 1 || t->ndim > 2) return fail(MT_ERR_NDIM, std::string(name) + ": must have rank 1 or 2");
+  if (t->dtype != MT_I32) return fail(MT_ERR_DTYPE, std::string(name) + ": must be i32");
+  for (int i = 0; i < t->ndim; ++i) {
+    if (t->shape[i] < 0) return fail(MT_ERR_SHAPE, std::string(name) + ": negative size");
+    if (t->shape[i] > kMostRows) return fail(MT_ERR_SHAPE, std::string(name) + ": size beyond 2^30");
+    if (t->stride[i] < 0) return fail(MT_ERR_LAYOUT, std::string(name) + ": negative stride");
+  }
+  const int64_t n = numel(t);
+  if (n > kMostRows) return fail(MT_ERR_SHAPE, std::string(name) + ": more than 2^30 values");
+  if (n > 0 && !t->data) return fail(MT_ERR_NULL, std::string(name) + ": null data pointer");
+  *count = n;
+  const int64_t inner = t->shape[t->ndim - 1], s1 = t->stride[t->ndim - 1], s0 = t->ndim > 1 ? t->stride[0] : 0;
+  const bool rows = t->ndim > 1 && t->shape[0] > 1, flat = (inner <= 1 || s1 == 1) && (!rows || s0 == inner);
+  *out = mt::vio::Index{(const int32_t*)t->data, flat ? 0 : inner, s0, s1};
+  return MT_OK;
+}
+
+// [rows, columns], the columns contiguous; `out`: rows apart.
+mt_status check_rows(const mt_tensor* t, const char* name, bool out) {
+  mt_status s = check_tensor(t, name, 2, 2);
+  if (s) return s;
+  if (t->shape[1] > 1 && t->stride[1] != 1)
+    return fail(MT_ERR_LAYOUT, std::string(name) + ": inner dimension must be contiguous");
+  if (t->shape[0] > kMostRows) return fail(MT_ERR_SHAPE, std::string(name) + ": more than 2^30 rows");
+  if (out && t->shape[0] > 1 && t->stride[0] < t->shape[1])
+    return fail(MT_ERR_LAYOUT, std::string(name) + ": rows overlap (row pitch < columns)");
+  return MT_OK;
+}
+int64_t row_pitch(const mt_tensor* t) { return t->shape[0] > 1 ? t->stride[0] : t->shape[1]; }
+
+// Byte ranges; tokens and classes have four bytes an element too.
+bool apart(const mt_tensor* a, const mt_tensor* b) {
+  if (!a || !b) return true;
+  mt_tensor x = *a, y = *b;
+  if (x.dtype == MT_I32) x.dtype = MT_F32;
+  if (y.dtype == MT_I32) y.dtype = MT_F32;
+  return !overlaps(&x, &y);
+}
+mt_status check_apart(std::initializer_list<const mt_tensor*> outs, std::initializer_list<const mt_tensor*> ins) {
+  for (auto o = outs.begin(); o != outs.end(); ++o) {
+    for (const mt_tensor* i : ins)
+      if (!apart(*o, i)) return fail(MT_ERR_ALIAS, "an output overlaps an input");
+    for (auto q = outs.begin(); q != o; ++q)
+      if (!apart(*o, *q)) return fail(MT_ERR_ALIAS, "two outputs overlap");
+  }
+  return MT_OK;
+}
+
+mt_status check_workspace(const void* ws, size_t ws_bytes, size_t need, const char* who) {
+  if (ws && ((uintptr_t)ws & 255)) return fail(MT_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (need > 0 && (!ws || ws_bytes < need))
+    return fail(MT_ERR_WORKSPACE, std::string(who) + " needs the workspace that its _workspace call reports");
+  return MT_OK;
+}
+
+// Values of a lane's group: 16 bytes of the narrower type.
+int vector_of(std::initializer_list<const mt_tensor*> ts) {
+  for (const mt_tensor* t : ts)
+    if (t && t->dtype == MT_BF16) return 8;
+  return 4;
+}
+
+size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// ---------------------------------------------------------------- embedding
+mt_status embedding_fwd_impl(const mt_tensor* ids, const mt_tensor* table, float scale, const mt_tensor* y,
+                             hipStream_t stream) {
+  mt::EmbeddingParams p{};
+  mt_status s;
+  if ((s = check_ids(ids, "ids", &p.ids, &p.M)) || (s = check_rows(table, "table", false)) ||
+      (s = check_rows(y, "y", true)))
+    return s;
+  p.V = table->shape[0];
+  p.D = table->shape[1];
+  if (y->shape[0] != p.M || y->shape[1] != p.D) return fail(MT_ERR_SHAPE, "y must be [tokens, D] with table [V, D]");
+  if (p.D > (1 << 20)) return fail(MT_ERR_SHAPE, "rows of more than 2^20 values");
+  if (!std::isfinite(scale)) return fail(MT_ERR_INVALID, "scale must be finite");
+  if ((s = check_apart({y}, {ids, table}))) return s;
+  if (p.M == 0 || p.D == 0) return MT_OK;
+  p.table = table->data;
+  p.y = y->data;
+  p.ldt = row_pitch(table);
+  p.ldy = row_pitch(y);
+  p.scale = scale;
+  (void)hipGetLastError();
+  return hip_status(mt::embedding_fwd(p, table->dtype == MT_BF16, y->dtype == MT_BF16, stream));
+}
+
+namespace {
+// Tokens of a chunk: two blocks a CU of 256 lanes, at least 16 tokens.
+int embedding_chunk(int64_t M, int64_t D, int vec) {
+  int64_t lanes = 1;
+  while (lanes < 256 && lanes * vec < D) lanes *= 2;
+  const int64_t tiles = cdiv(D, lanes * vec), rows = 256 / lanes;  // a block takes `rows` chunks of a tile
+  int chunk = 16;
+  while (chunk < 256 && cdiv(cdiv(M, chunk), rows) * tiles > 2048) chunk *= 2;
+  return chunk;
+}
+}  // namespace
+
+mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float scale, const mt_tensor* dtable,
+                             uint32_t flags, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
+  if (flags & ~MT_ACCUMULATE) return fail(MT_ERR_INVALID, "mt_embedding_bwd: unknown flags");
+  mt::EmbeddingGradParams p{};
+  mt_status s;
+  if ((s = check_ids(ids, "ids", &p.ids, &p.M)) || (s = check_rows(dy, "dy", false)) ||
+      (s = check_rows(dtable, "dtable", true)))
+    return s;
+  if (dtable->dtype != MT_F32) return fail(MT_ERR_DTYPE, "dtable must be f32");
+  p.V = dtable->shape[0];
+  p.D = dtable->shape[1];
+  if (dy->shape[0] != p.M || dy->shape[1] != p.D)
+    return fail(MT_ERR_SHAPE, "dy must be [tokens, D] with dtable [V, D]");
+  if (p.D > (1 << 20)) return fail(MT_ERR_SHAPE, "rows of more than 2^20 values");
+  if (p.V > (1 << 24)) return fail(MT_ERR_SHAPE, "more than 2^24 rows of dtable");
+  if (p.M > (1 << 26)) return fail(MT_ERR_SHAPE, "more than 2^26 tokens");
+  if (!std::isfinite(scale)) return fail(MT_ERR_INVALID, "scale must be finite");
+  if ((s = check_apart({dtable}, {ids, dy}))) return s;
+  p.chunk = embedding_chunk(p.M, p.D, vector_of({dy}));
+  p.chunks = (int32_t)cdiv(p.M, p.chunk);
+  const size_t list = round256(p.M * sizeof(int32_t)), sums = round256((size_t)p.chunks * p.D * sizeof(float));
+  const size_t need = p.V && p.D ? 256 + 2 * list + 2 * sums : 0;
+  if (ws_query) {
+    *ws_query = need;
+    return MT_OK;
+  }
+  if ((s = check_workspace(ws, ws_bytes, need, "mt_embedding_bwd"))) return s;
+  if (p.V == 0 || p.D == 0) return MT_OK;
+  char* at = (char*)ws;
+  p.total = (int32_t*)at;
+  p.id = (int32_t*)(at += 256);
+  p.pos = (int32_t*)(at += list);
+  p.head = (float*)(at += list);
+  p.tail = (float*)(at += sums);
+  p.dy = dy->data;
+  p.dtable = (float*)dtable->data;
+  p.ldy = row_pitch(dy);
+  p.ldt = row_pitch(dtable);
+  p.scale = scale;
+  p.accumulate = (flags & MT_ACCUMULATE) != 0;
+  // buckets of 256 blocks, or as many as leave a bucket no more ids than it has counters for
+  while (p.bucket_shift < 8 && (int64_t)1 << p.bucket_shift < p.V) ++p.bucket_shift;
+  while (p.V > (int64_t)mt::kEmbedBucketIds << p.bucket_shift) ++p.bucket_shift;
+  (void)hipGetLastError();
+  return hip_status(mt::embedding_bwd(p, dy->dtype == MT_BF16, stream));
+}
+
+// --------------------------------------------------------------- layer norm
+namespace {
+
+mt_status check_norm(const mt_tensor* x, const mt_tensor* w, float eps, mt::LayerNormParams* p) {
+  mt_status s = check_rows(x, "x", false);
+  if (s) return s;
+  const int64_t C = x->shape[1];
+  if (C < 1 || C > mt::kLayerNormMaxC) return fail(MT_ERR_SHAPE, "a row must have 1 to 16384 values");
+  if (w && (s = check_vector(w, "w", C))) return s;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(MT_ERR_INVALID, "eps must be finite and not negative");
+  *p = mt::LayerNormParams{};
+  p->x = x->data;
+  p->w = w ? (const float*)w->data : nullptr;
+  p->M = x->shape[0];
+  p->C = (int32_t)C;
+  p->ldx = row_pitch(x);
+  p->eps = eps;
+  p->C_f = (float)C;
+  return MT_OK;
+}
+
+mt_status like(const mt_tensor* t, const char* name, const mt_tensor* x, bool out) {
+  mt_status s = check_rows(t, name, out);
+  if (s) return s;
+  if (t->shape[0] != x->shape[0] || t->shape[1] != x->shape[1])
+    return fail(MT_ERR_SHAPE, std::string(name) + " must have the shape of x");
+  return MT_OK;
+}
+
+// How a row is held: L lanes with nv groups of vec values, blocks of `threads`.
+struct NormForm {
+  int nv, threads, blocks;
+};
+NormForm norm_form(mt::LayerNormParams* p, int vec, int threads, int most_blocks) {
+  NormForm f{1, threads, 1};
+  const int most = 16 / vec;  // groups a lane
+  for (p->L = 1, p->L_shift = 0; p->L < 64 && p->L * vec * most < p->C; p->L *= 2) ++p->L_shift;
+  while (p->L * vec * most < p->C) p->L *= 2, ++p->L_shift;
+  f.nv = (int)cdiv(p->C, (int64_t)p->L * vec);
+  f.threads = std::max(threads, p->L);
+  f.blocks = (int)std::min<int64_t>(most_blocks, std::max<int64_t>(1, cdiv(p->M, f.threads / p->L)));
+  return f;
+}
+
+}  // namespace
+
+mt_status layer_norm_fwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_tensor* b, float eps,
+                              const mt_tensor* y, hipStream_t stream) {
+  mt::LayerNormParams p;
+  mt_status s;
+  if ((s = check_norm(x, w, eps, &p)) || (b && (s = check_vector(b, "b", p.C))) || (s = like(y, "y", x, true)) ||
+      (s = check_apart({y}, {x, w, b})))
+    return s;
+  if (p.M == 0) return MT_OK;
+  p.b = b ? (const float*)b->data : nullptr;
+  p.out = y->data;
+  p.ldo = row_pitch(y);
+  const NormForm f = norm_form(&p, vector_of({x, y}), 256, 2048);
+  (void)hipGetLastError();
+  return hip_status(mt::layer_norm_fwd(p, x->dtype == MT_BF16, y->dtype == MT_BF16, f.nv, f.threads, f.blocks, stream));
+}
+
+mt_status layer_norm_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy, float eps,
+                              const mt_tensor* dx, const mt_tensor* dw, const mt_tensor* db, uint32_t flags, void* ws,
+                              size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
+  if (flags & ~MT_ACCUMULATE) return fail(MT_ERR_INVALID, "mt_layer_norm_bwd: unknown flags");
+  mt::LayerNormParams p;
+  mt_status s;
+  if ((s = check_norm(x, w, eps, &p)) || (s = like(dy, "dy", x, false))) return s;
+  if (!dx && !dw && !db) return fail(MT_ERR_NULL, "no output requested");
+  if (dx) {
+    if ((s = like(dx, "dx", x, true))) return s;
+    if (dx->dtype != dy->dtype) return fail(MT_ERR_DTYPE, "dx must have dy's dtype");
+  }
+  if ((dw && (s = check_vector(dw, "dw", p.C))) || (db && (s = check_vector(db, "db", p.C))) ||
+      (s = check_apart({dx, dw, db}, {x, w, dy})))
+    return s;
+  const NormForm f = norm_form(&p, vector_of({x, dy}), 1024, 256);
+  const bool weights = dw || db;
+  const size_t need = weights ? (size_t)f.blocks * 2 * p.C * sizeof(float) : 0;
+  if (ws_query) {
+    *ws_query = need;
+    return MT_OK;
+  }
+  if ((s = check_workspace(ws, ws_bytes, need, "mt_layer_norm_bwd"))) return s;
+  p.dy = dy->data;
+  p.ldd = row_pitch(dy);
+  p.out = dx ? dx->data : nullptr;
+  p.ldo = dx ? row_pitch(dx) : 0;
+  p.accumulate = (flags & MT_ACCUMULATE) != 0;
+  p.part = weights ? (float*)ws : nullptr;
+  (void)hipGetLastError();
+  // without rows too: dw and db are empty sums then
+  if (p.M > 0 || weights) {
+    s = hip_status(mt::layer_norm_bwd(p, x->dtype == MT_BF16, dy->dtype == MT_BF16, f.nv, f.threads, f.blocks, stream));
+    if (s) return s;
+  }
+  if (!weights) return MT_OK;
+  return hip_status(mt::layer_norm_finish(p.part, f.blocks, p.C, dw ? (float*)dw->data : nullptr,
+                                          db ? (float*)db->data : nullptr, p.accumulate, stream));
+}
+
+// ------------------------------------------------------------ cross-entropy
+mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, const mt_tensor* loss,
+                             const mt_tensor* losses, const mt_tensor* dlogits, void* ws, size_t ws_bytes,
+                             hipStream_t stream, size_t* ws_query) {
+  mt::CrossEntropyParams p{};
+  mt_status s;
+  int64_t n = 0;
+  if ((s = check_rows(logits, "logits", false)) || (s = check_ids(targets, "targets", &p.targets, &n))) return s;
+  p.M = logits->shape[0];
+  const int64_t V = logits->shape[1];
+  if (n != p.M) return fail(MT_ERR_SHAPE, "targets must hold one class for each row of logits");
+  if (V < 1 || V > (1 << 24)) return fail(MT_ERR_SHAPE, "a row must have 1 to 2^24 logits");
+  const size_t need = 256 + round256(p.M * sizeof(float));
+  if (ws_query) {
+    *ws_query = need;
+    return MT_OK;
+  }
+  if (!loss && !losses && !dlogits) return fail(MT_ERR_NULL, "mt_cross_entropy: no output requested");
+  if (loss) {
+    if ((s = check_tensor(loss, "loss", 0, MT_MAX_DIMS))) return s;
+    if (loss->dtype != MT_F32) return fail(MT_ERR_DTYPE, "loss must be f32");
+    if (numel(loss) != 1) return fail(MT_ERR_SHAPE, "loss must hold exactly one element");
+  }
+  if (losses && (s = check_vector(losses, "losses", p.M))) return s;
+  if (dlogits) {
+    if ((s = check_rows(dlogits, "dlogits", true))) return s;
+    if (dlogits->shape[0] != p.M || dlogits->shape[1] != V)
+      return fail(MT_ERR_SHAPE, "dlogits must have the shape of logits");
+  }
+  if ((s = check_apart({loss, losses, dlogits}, {logits, targets})) ||
+      (s = check_workspace(ws, ws_bytes, need, "mt_cross_entropy")))
+    return s;
+  int32_t* counted = (int32_t*)ws;
+  p.V = (int32_t)V;
+  p.counted = counted;
+  p.row_loss = losses && p.M ? (float*)losses->data : (float*)((char*)ws + 256);
+  p.z = logits->data;
+  p.ldz = row_pitch(logits);
+  const bool zb = logits->dtype == MT_BF16, db = dlogits ? dlogits->dtype == MT_BF16 : zb;
+  if (dlogits) {
+    p.dz = dlogits->data;
+    p.ldd = row_pitch(dlogits);
+  }
+  mt::CrossEntropyForm f{256, 0, 0, 0};
+  if (V <= 512) {
+    for (f.L = 1; f.L < 64 && f.L * 8 < V; f.L *= 2) ++f.L_shift;
+  } else {
+    while (f.threads < 1024 && (int64_t)f.threads * 64 < V) f.threads *= 2;
+    if ((int64_t)f.threads * 64 >= V) f.values = (int32_t)cdiv(V, f.threads);
+  }
+  (void)hipGetLastError();
+  const hipStream_t st = stream;
+  if ((s = hip_status(mt::cross_entropy_count(p.targets, p.M, V, counted, st)))) return s;
+  if (p.M > 0 && (s = hip_status(mt::cross_entropy_rows(p, f, zb, db, st)))) return s;
+  if (!loss) return MT_OK;
+  return hip_status(mt::cross_entropy_mean(p.row_loss, p.M, counted, (float*)loss->data, st));
+}
+
+// ----------------------------------------------------------------- clipping
+mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+                              const mt_tensor* norm, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
+  const std::string who = "mt_clip_grad_norm: ";
+  if (n < 0) return fail(MT_ERR_INVALID, who + "negative tensor count");
+  if (n > 0 && !grads) return fail(MT_ERR_NULL, who + "null array");
+  mt_status s;
+  struct Range {
+    uintptr_t lo, hi;
+    bool out;
+  };
+  std::vector<Range> ranges;
+  std::vector<mt::ClipBatch> batches;
+  size_t parts = 0;
+  int64_t chunks = 0;
+  auto close = [&] {
+    batches.back().start[batches.back().n] = (int32_t)chunks;
+    parts += mt::clip_blocks(chunks);
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    const mt_tensor* ts[2] = {&grads[i], out ? &out[i] : &grads[i]};
+    for (int j = 0; j < (out ? 2 : 1); ++j) {
+      const std::string name = who + (j ? "out " : "grad ") + std::to_string(i);
+      if ((s = check_tensor(ts[j], name.c_str(), 0, MT_MAX_DIMS))) return s;
+      if (!is_row_major(ts[j])) return fail(MT_ERR_LAYOUT, name + ": must be contiguous");
+      if (ts[j]->ndim != ts[0]->ndim || !std::equal(ts[j]->shape, ts[j]->shape + ts[j]->ndim, ts[0]->shape))
+        return fail(MT_ERR_SHAPE, name + " must have the shape of its gradient");
+      const uintptr_t lo = (uintptr_t)ts[j]->data;
+      if (numel(ts[j]) > 0) ranges.push_back({lo, lo + numel(ts[j]) * elem_size(ts[j]->dtype), j > 0});
+    }
+    const int64_t count = numel(ts[0]), pieces = cdiv(count, mt::kClipChunk);
+    if (count == 0) continue;
+    if (pieces > (1 << 28)) return fail(MT_ERR_SHAPE, who + "tensor " + std::to_string(i) + " is too large");
+    if (batches.empty() || batches.back().n == mt::kClipTensors || chunks + pieces > (1 << 29)) {
+      if (!batches.empty()) close();
+      batches.emplace_back();
+      chunks = 0;
+    }
+    mt::ClipBatch& b = batches.back();
+    const int k = b.n++;
+    b.src[k] = ts[0]->data;
+    b.dst[k] = ts[1]->data;
+    b.numel[k] = count;
+    b.start[k] = (int32_t)chunks;
+    b.kind[k] = (int8_t)((ts[0]->dtype == MT_BF16 ? 1 : 0) | (ts[1]->dtype == MT_BF16 ? 2 : 0));
+    chunks += pieces;
+  }
+  if (!batches.empty()) close();
+  const size_t need = round256(std::max<size_t>(1, parts) * sizeof(double));
+  if (ws_query) {
+    *ws_query = need;
+    return MT_OK;
+  }
+  if (!(max_norm >= 0.f)) return fail(MT_ERR_INVALID, who + "max_norm must not be negative");
+  if (norm) {
+    if ((s = check_tensor(norm, "norm", 0, MT_MAX_DIMS))) return s;
+    if (norm->dtype != MT_F32) return fail(MT_ERR_DTYPE, "norm must be f32");
+    if (numel(norm) != 1) return fail(MT_ERR_SHAPE, "norm must hold exactly one element");
+    ranges.push_back({(uintptr_t)norm->data, (uintptr_t)norm->data + 4, true});
+  }
+  // what is written overlaps nothing else
+  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  uintptr_t far = 0, far_out = 0;  // ends of what came before: of all, of what is written
+  for (const Range& r : ranges) {
+    const bool written = !out || r.out;
+    if (r.lo < far_out || (written && r.lo < far)) return fail(MT_ERR_ALIAS, who + "a tensor that is written overlaps another");
+    far = std::max(far, r.hi);
+    if (written) far_out = std::max(far_out, r.hi);
+  }
+  if ((s = check_workspace(ws, ws_bytes, need, "mt_clip_grad_norm"))) return s;
+  double* part = (double*)ws;
+  float* to = norm ? (float*)norm->data : nullptr;
+  (void)hipGetLastError();
+  size_t at = 0;
+  for (const mt::ClipBatch& b : batches) {
+    const int blocks = mt::clip_blocks(b.start[b.n]);
+    if ((s = hip_status(mt::clip_norm(b, part + at, blocks, stream)))) return s;
+    at += blocks;
+  }
+  if (batches.empty()) {
+    if (!to) return MT_OK;
+    return hip_status(mt::clip_scale(mt::ClipBatch{}, part, 0, max_norm, to, 1, stream));
+  }
+  for (const mt::ClipBatch& b : batches) {
+    if ((s = hip_status(mt::clip_scale(b, part, (int)parts, max_norm, to, mt::clip_blocks(b.start[b.n]), stream)))) return s;
+    to = nullptr;  // written once
+  }
+  return MT_OK;
+}
+
+}  // namespace mt::host

@@ -1,0 +1,272 @@
+// Layer norm and its gradient, gfx950. For a row x of C values:
+//
+//   mu = mean x,  r = (mean (x - mu)^2 + eps)^(-1/2),  n = (x - mu) r,  y = n w + b
+//   g = dy w,  dx = r (g - mean g - n mean(g n)),  dw = sum over rows of dy n,  db = of dy
+//
+// A row is read once and held in registers by L lanes (a power of two, up to a
+// block), so that the variance is a mean of squared deviations and not a
+// difference of large numbers, and the gradient needs no saved statistics: it
+// takes them again from the row that it reads anyway. Bound: HBM.
+//
+// dw, db: a lane keeps the sums of its columns over the rows that it meets, a
+// block adds its groups' in order, a second launch the blocks' in order.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "language.hpp"
+
+namespace mt {
+namespace layernorm {
+
+using namespace vio;
+
+// Sums over a row's lanes; rows of more than a wave (WIDE) meet in LDS, one
+// buffer a sum, used again only after another sum's barrier.
+template <bool WIDE, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], int L, float (*red)[16]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], WIDE ? 64 : L);
+  if constexpr (WIDE) {
+    const int wave = threadIdx.x >> 6, W = L >> 6, first = wave & ~(W - 1);
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[i][wave] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = 0.f;
+      for (int w = 0; w < W; ++w) s += red[i][first + w];
+      v[i] = s;
+    }
+  }
+}
+
+// Column of value e of group k of a lane's: (l + k L) VEC + e.
+template <bool XB, bool YB, int VEC, int NV, bool WIDE>
+__global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
+  __shared__ float red[2][16];
+  const int l = threadIdx.x & (p.L - 1), rows = blockDim.x >> p.L_shift;
+  float w[NV][VEC], b[NV][VEC];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      w[k][e] = 1.f;
+      b[k][e] = 0.f;
+    }
+    if (p.w) load_some<false, VEC>(p.w, c, p.C - c, 0.f, w[k]);
+    if (p.b) load_some<false, VEC>(p.b, c, p.C - c, 0.f, b[k]);
+  }
+  // all rows of a block go through the loop the same number of times
+  for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
+    const int64_t m = m0 + (threadIdx.x >> p.L_shift);
+    const bool on = m < p.M;
+    float x[NV][VEC], s[1] = {0.f}, q[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+      load_some<XB, VEC>(p.x, m * p.ldx + c, on ? p.C - c : 0, 0.f, x[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[0] += x[k][e];
+    row_sums<WIDE, 1>(s, p.L, red);
+    const float mu = s[0] / p.C_f;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        x[k][e] = c + e < p.C ? x[k][e] - mu : 0.f;
+        q[0] = fmaf(x[k][e], x[k][e], q[0]);
+      }
+    }
+    row_sums<WIDE, 1>(q, p.L, red + 1);
+    const float r = 1.f / sqrtf(q[0] / p.C_f + p.eps);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[k][e] = fmaf(x[k][e] * r, w[k][e], b[k][e]);
+      store_some<YB, VEC>(p.out, m * p.ldo + c, on ? p.C - c : 0, x[k]);
+    }
+  }
+}
+
+template <bool XB, bool YB, int VEC, int NV, bool WIDE>
+__global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
+  __shared__ float red[4][16];
+  __shared__ float cols[1024 * 16];  // [group][C], where a block has several groups
+  const int l = threadIdx.x & (p.L - 1), rows = blockDim.x >> p.L_shift, grp = threadIdx.x >> p.L_shift;
+  float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      w[k][e] = 1.f;
+      dw[k][e] = db[k][e] = 0.f;
+    }
+    if (p.w) load_some<false, VEC>(p.w, c, p.C - c, 0.f, w[k]);
+  }
+  for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
+    const int64_t m = m0 + grp;
+    const bool on = m < p.M;
+    float x[NV][VEC], g[NV][VEC], s[1] = {0.f}, t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+      load_some<XB, VEC>(p.x, m * p.ldx + c, on ? p.C - c : 0, 0.f, x[k]);
+      load_some<YB, VEC>(p.dy, m * p.ldd + c, on ? p.C - c : 0, 0.f, g[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[0] += x[k][e];
+    row_sums<WIDE, 1>(s, p.L, red);
+    const float mu = s[0] / p.C_f;
+    // squares of the deviations, sums of g and of g times the deviations
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        x[k][e] = c + e < p.C ? x[k][e] - mu : 0.f;
+        const float gw = g[k][e] * w[k][e];
+        t[0] = fmaf(x[k][e], x[k][e], t[0]);
+        t[1] += gw;
+        t[2] = fmaf(x[k][e], gw, t[2]);
+      }
+    }
+    row_sums<WIDE, 3>(t, p.L, red + 1);
+    const float r = 1.f / sqrtf(t[0] / p.C_f + p.eps);
+    const float mg = t[1] / p.C_f, mgn = t[2] * r / p.C_f;  // the means of g and of g n
+    if (!on) continue;  // no barrier below
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+      float o[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float n = x[k][e] * r;
+        dw[k][e] = fmaf(g[k][e], n, dw[k][e]);
+        db[k][e] += g[k][e];
+        o[e] = r * (fmaf(g[k][e], w[k][e], -mg) - n * mgn);
+      }
+      if (!p.out) continue;
+      if (p.accumulate) {
+        float old[VEC];
+        load_some<YB, VEC>(p.out, m * p.ldo + c, p.C - c, 0.f, old);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] += old[e];
+      }
+      store_some<YB, VEC>(p.out, m * p.ldo + c, p.C - c, o);
+    }
+  }
+  if (!p.part) return;
+  float* part = p.part + (int64_t)blockIdx.x * 2 * p.C;
+#pragma unroll
+  for (int which = 0; which < 2; ++which, part += p.C) {
+    if (rows == 1) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (c + e < p.C) part[c + e] = which ? db[k][e] : dw[k][e];
+      }
+      continue;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int c = (l + (k << p.L_shift)) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (c + e < p.C) cols[grp * p.C + c + e] = which ? db[k][e] : dw[k][e];
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
+      float s = 0.f;
+      for (int i = 0; i < rows; ++i) s += cols[i * p.C + c];
+      part[c] = s;
+    }
+  }
+}
+
+// dw, db (+)= the blocks' parts, in order within each of 64 interleaved shares,
+// then over the shares; a block covers 16 of the 2 C columns.
+__global__ __launch_bounds__(1024) void finish_kernel(const float* part, int parts, int C, float* dw, float* db, int add) {
+  __shared__ float sums[64][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
+  float s = 0.f;
+  if (c < 2 * C) {
+#pragma unroll 8
+    for (int i = share; i < parts; i += 64) s += part[(int64_t)i * 2 * C + c];
+  }
+  sums[share][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (share || c >= 2 * C) return;
+  s = 0.f;
+#pragma unroll 16
+  for (int i = 0; i < 64; ++i) s += sums[i][threadIdx.x];
+  float* out = c < C ? dw : db;
+  if (!out) return;
+  out += c < C ? c : c - C;
+  *out = add ? *out + s : s;
+}
+
+template <typename F>
+hipError_t by_types(bool x, bool y, F f) {
+  if (x) return y ? f(std::true_type{}, std::true_type{}) : f(std::true_type{}, std::false_type{});
+  return y ? f(std::false_type{}, std::true_type{}) : f(std::false_type{}, std::false_type{});
+}
+
+// f(groups of values a lane, lanes past a wave) for the forms that are built.
+template <int VEC, typename F>
+hipError_t by_form(int nv, bool wide, F f) {
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  using Most = std::integral_constant<int, 16 / VEC>;
+  if (nv == 1) return wide ? f(One{}, std::true_type{}) : f(One{}, std::false_type{});
+  if (nv == 2) return wide ? f(Two{}, std::true_type{}) : f(Two{}, std::false_type{});
+  return wide ? f(Most{}, std::true_type{}) : f(Most{}, std::false_type{});
+}
+
+}  // namespace layernorm
+
+hipError_t layer_norm_fwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, int nv, int threads, int blocks,
+                          hipStream_t stream) {
+  return layernorm::by_types(x_bf16, y_bf16, [&](auto xb, auto yb) {
+    constexpr bool XB = decltype(xb)::value, YB = decltype(yb)::value;
+    constexpr int VEC = XB || YB ? 8 : 4;
+    return layernorm::by_form<VEC>(nv, p.L > 64, [&](auto n, auto wide) {
+      layernorm::fwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value>
+          <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, int nv, int threads, int blocks,
+                          hipStream_t stream) {
+  return layernorm::by_types(x_bf16, y_bf16, [&](auto xb, auto yb) {
+    constexpr bool XB = decltype(xb)::value, YB = decltype(yb)::value;
+    constexpr int VEC = XB || YB ? 8 : 4;
+    return layernorm::by_form<VEC>(nv, p.L > 64, [&](auto n, auto wide) {
+      layernorm::bwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value>
+          <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t layer_norm_finish(const float* part, int parts, int C, float* dw, float* db, bool add, hipStream_t stream) {
+  layernorm::finish_kernel<<<dim3((unsigned)((2 * C + 15) / 16)), 1024, 0, stream>>>(part, parts, C, dw, db, add);
+  return hipGetLastError();
+}
+
+}  // namespace mt

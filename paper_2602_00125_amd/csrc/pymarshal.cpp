@@ -38,6 +38,12 @@ struct Lib {
   decltype(&mt_qk_norm_rope_bwd) qk_norm_rope_bwd;
   decltype(&mt_dropout_fwd) dropout_fwd;
   decltype(&mt_dropout_bwd) dropout_bwd;
+  decltype(&mt_embedding_fwd) embedding_fwd;
+  decltype(&mt_embedding_bwd) embedding_bwd;
+  decltype(&mt_layer_norm_fwd) layer_norm_fwd;
+  decltype(&mt_layer_norm_bwd) layer_norm_bwd;
+  decltype(&mt_cross_entropy) cross_entropy;
+  decltype(&mt_clip_grad_norm) clip_grad_norm;
 } L;
 
 bool as_i64(PyObject* o, int64_t* v) {
@@ -80,7 +86,7 @@ bool refuse(PyObject* t, bool index) {
   return false;
 }
 
-// index: a tensor of int32 lengths or positions, else one of the two dtypes.
+// index: a tensor of int32 lengths, positions, tokens or classes, else one of the two dtypes.
 bool describe(PyObject* t, mt_tensor* d, bool index = false) {
   PyObject* v = PyObject_GetAttr(t, s_is_cuda);
   if (!v) return false;
@@ -318,6 +324,49 @@ FN(dropout_bwd) {  // dy, p, seed, offset, dx, flags, stream
   void* st = g.stream(6);
   return call(g.ok, [&] { return L.dropout_bwd(dy, p, seed, offset, dx, flags, st); });
 }
+FN(embedding_fwd) {  // ids, table, scale, y, stream
+  Args g(a, n, 5);
+  const mt_tensor *ids = g.tensor(0, true), *t = g.tensor(1);
+  const float scale = g.f32(2);
+  const mt_tensor* y = g.tensor(3);
+  void* st = g.stream(4);
+  return call(g.ok, [&] { return L.embedding_fwd(ids, t, scale, y, st); });
+}
+FN(embedding_bwd) {  // ids, dy, scale, dtable, flags, ws, stream
+  Args g(a, n, 7);
+  const mt_tensor *ids = g.tensor(0, true), *dy = g.tensor(1);
+  const float scale = g.f32(2);
+  const mt_tensor* d = g.tensor(3);
+  const uint32_t flags = (uint32_t)g.i64(4);
+  const Args::Ws ws = g.ws(5);
+  void* st = g.stream(6);
+  return call(g.ok, [&] { return L.embedding_bwd(ids, dy, scale, d, flags, ws.p, ws.n, st); });
+}
+FN(layer_norm_fwd) {  // x, w, b, eps, y, stream
+  Args g(a, n, 6);
+  const mt_tensor *x = g.tensor(0), *w = g.tensor(1), *b = g.tensor(2);
+  const float eps = g.f32(3);
+  const mt_tensor* y = g.tensor(4);
+  void* st = g.stream(5);
+  return call(g.ok, [&] { return L.layer_norm_fwd(x, w, b, eps, y, st); });
+}
+FN(layer_norm_bwd) {  // x, w, dy, eps, dx, dw, db, flags, ws, stream
+  Args g(a, n, 10);
+  const mt_tensor *x = g.tensor(0), *w = g.tensor(1), *dy = g.tensor(2);
+  const float eps = g.f32(3);
+  const mt_tensor *dx = g.tensor(4), *dw = g.tensor(5), *db = g.tensor(6);
+  const uint32_t flags = (uint32_t)g.i64(7);
+  const Args::Ws ws = g.ws(8);
+  void* st = g.stream(9);
+  return call(g.ok, [&] { return L.layer_norm_bwd(x, w, dy, eps, dx, dw, db, flags, ws.p, ws.n, st); });
+}
+FN(cross_entropy) {  // logits, targets, loss, losses, dlogits, ws, stream
+  Args g(a, n, 7);
+  const mt_tensor *z = g.tensor(0), *t = g.tensor(1, true), *l = g.tensor(2), *ls = g.tensor(3), *d = g.tensor(4);
+  const Args::Ws ws = g.ws(5);
+  void* st = g.stream(6);
+  return call(g.ok, [&] { return L.cross_entropy(z, t, l, ls, d, ws.p, ws.n, st); });
+}
 
 // Descriptors of up to four lists of n tensors each, one list after another.
 // The lists' tensors are held until the call has returned: it runs without
@@ -381,6 +430,20 @@ FN(rmsprop_step) {  // params, grads, sq_avg, lr, alpha, eps, stream
   void* st = g.stream(6);
   return call(g.ok, [&] { return L.rmsprop_step((int32_t)t.n, t[0], t[1], t[2], lr, alpha, eps, st); });
 }
+FN(clip_grad_norm) {  // grads, out, max_norm, norm, ws, stream
+  Args g(a, n, 6);
+  if (!g.ok) return nullptr;
+  const bool in_place = a[1] == Py_None;
+  const Lists t(a, in_place ? 1 : 2);
+  if (!t.ok) return nullptr;
+  const float most = g.f32(2);
+  const mt_tensor* norm = g.tensor(3);
+  const Args::Ws ws = g.ws(4);
+  void* st = g.stream(5);
+  return call(g.ok, [&] {
+    return L.clip_grad_norm((int32_t)t.n, t[0], most, in_place ? nullptr : t[1], norm, ws.p, ws.n, st);
+  });
+}
 
 FN(init) {
   if (n != 7) {
@@ -400,7 +463,8 @@ FN(init) {
   SYM(linear_fwd) SYM(linear_act_fwd) SYM(linear_bwd) SYM(matmul) SYM(reduce_broadcast_grad) SYM(act_bwd)
   SYM(mse_loss) SYM(sgd_step) SYM(adam_step) SYM(rmsprop_step) SYM(conv2d_fwd) SYM(conv2d_bwd)
   SYM(attention_fwd) SYM(attention_bwd) SYM(qk_norm_rope_fwd) SYM(qk_norm_rope_bwd) SYM(dropout_fwd)
-  SYM(dropout_bwd)
+  SYM(dropout_bwd) SYM(embedding_fwd) SYM(embedding_bwd) SYM(layer_norm_fwd) SYM(layer_norm_bwd) SYM(cross_entropy)
+  SYM(clip_grad_norm)
 #undef SYM
   PyObject** to[] = {&g_f32, &g_bf16, &g_i32, &g_describe, &g_current, &g_stream_of};
   for (int i = 0; i < 6; ++i) {
@@ -416,6 +480,8 @@ PyMethodDef methods[] = {METHOD(init), METHOD(linear_fwd), METHOD(linear_act_fwd
                          METHOD(adam_step), METHOD(rmsprop_step), METHOD(conv2d_fwd), METHOD(conv2d_bwd),
                          METHOD(attention_fwd), METHOD(attention_bwd), METHOD(qk_norm_rope_fwd),
                          METHOD(qk_norm_rope_bwd), METHOD(dropout_fwd), METHOD(dropout_bwd),
+                         METHOD(embedding_fwd), METHOD(embedding_bwd), METHOD(layer_norm_fwd), METHOD(layer_norm_bwd),
+                         METHOD(cross_entropy), METHOD(clip_grad_norm),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "argument marshalling of the binding", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,114 @@
+"""mt_clip_grad_norm against the formulas in 64 bits; the bounds are derived in language_reference.py."""
+import pytest
+import torch
+
+from language_reference import DEV, DT, clip, close, draw
+
+pytestmark = pytest.mark.gpu
+
+from paper_2602_00125_amd import binding as b  # noqa: E402  (a missing library fails the module)
+
+INF = float("inf")
+
+
+def run(grads, max_norm, out=None, norm=True):
+    n = torch.full((1,), float("nan"), device=DEV) if norm else None
+    ws = torch.full((b.clip_grad_norm_workspace(grads),), 0xff, dtype=torch.uint8, device=DEV)
+    b.clip_grad_norm(grads, max_norm, n, out=out, workspace=ws)
+    return n
+
+
+def gradients(shapes, dtypes, seed=0, scale=1e-3):
+    return [draw(s, dtypes[i % len(dtypes)], seed + i, scale) for i, s in enumerate(shapes)]
+
+
+SHAPES = [[(1,)], [()], [(4096,)], [(4097,)], [(3, 5, 7), (0,), (64, 64), (2,)], [(1000, 1000)], [(33, 129), (8193,), (1, 1)],
+          [(37,)] * 119, [(50,)] * 120, [(3, 9)] * 121, [(125, 60), (125,)] * 200]
+
+
+@pytest.mark.parametrize("dtypes", [["f32"], ["bf16"], ["f32", "bf16"]], ids=str)
+@pytest.mark.parametrize("shapes", SHAPES, ids=lambda s: f"{len(s)}x{s[0]}")
+def test_sizes(shapes, dtypes):
+    grads = gradients(shapes, dtypes)
+    size = float(clip(grads, 1.0, DT.values())[0][0])
+    for part in (0.3, 3.0):
+        types = [g.dtype for g in grads]
+        (norm, bound), outs = clip(grads, part * size, types)
+        here = [g.clone() for g in grads]
+        close("norm", run(here, part * size), norm, bound)
+        for i, (g, o) in enumerate(zip(here, outs)):
+            close(f"grad {i}", g, *o)
+            assert part < 1 or torch.equal(g, grads[i])
+        for other in ("f32", "bf16"):
+            out = [torch.full(g.shape, float("nan"), dtype=DT[other], device=DEV) for g in grads]
+            run(grads, part * size, out, norm=False)
+            for i, (g, o) in enumerate(zip(out, clip(grads, part * size, [DT[other]] * len(grads))[1])):
+                close(f"out {i}", g, *o)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_odd_places(dtype):
+    """Views one element into a buffer, with others' values beside them."""
+    flat = torch.full((3 + 5000 + 7 + 4096 + 9,), 5.0, dtype=DT[dtype], device=DEV)
+    grads = [flat[3:5003], flat[5010:9106]]
+    for i, g in enumerate(grads):
+        g.copy_(draw(g.shape, dtype, i))
+    (norm, bound), outs = clip([g.clone() for g in grads], 0.5, [g.dtype for g in grads])
+    close("norm", run(grads, 0.5), norm, bound)
+    for g, o in zip(grads, outs):
+        close("grad", g, *o)
+    assert (flat[:3] == 5).all() and (flat[5003:5010] == 5).all() and (flat[9106:] == 5).all()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-42, 1e30])
+def test_squares_past_fp32(scale):
+    grads = gradients([(500,), (70, 70)], ["f32"], 3, scale)
+    (norm, bound), outs = clip(grads, 2 * scale, [torch.float32] * 2)
+    close("norm", run(grads, 2 * scale), norm, bound + 2.0 ** -149)
+    for g, o in zip(grads, outs):
+        close("grad", g, *o)
+
+
+def test_limits():
+    g = gradients([(300,)], ["f32"], 4)
+    keep = g[0].clone()
+    size = run(g, INF)
+    assert torch.equal(g[0], keep)
+    close("norm", size, *clip(g, INF, [torch.float32])[0])
+    assert run(g, 0.0) == size and not g[0].any()
+    assert run(g, 0.0) == 0 and not g[0].any()
+    assert run([], 1.0) == 0 and run([torch.empty(0, device=DEV)], 1.0) == 0
+    run([], 1.0, norm=False)
+
+
+@pytest.mark.parametrize("bad", [INF, -INF, float("nan")])
+def test_a_norm_that_is_not_finite_clips_nothing(bad):
+    g = gradients([(9000,), (5,)], ["f32", "bf16"], 5)
+    g[0][8500] = bad
+    keep = [t.clone() for t in g]
+    n = run(g, 1e-6)
+    assert n.isnan() if bad != bad else n == INF
+    assert all(torch.equal(a.nan_to_num(7.0), c.nan_to_num(7.0)) for a, c in zip(g, keep))
+    out = [torch.empty_like(t) for t in g]
+    run(g, 1e-6, out)
+    assert all(torch.equal(a.nan_to_num(7.0), c.nan_to_num(7.0)) for a, c in zip(out, keep))
+
+
+def test_large_tensors_and_reruns():
+    g = [torch.full((40_000_000,), 1e-3, device=DEV), draw((3_000_001,), "f32", 6)]
+    runs = []
+    for _ in range(2):
+        out = [torch.empty_like(t) for t in g]
+        runs.append([run(g, 1.0, out), *out])
+    assert all(torch.equal(a, c) for a, c in zip(*runs))
+    (norm, bound), outs = clip(g, 1.0, [torch.float32] * 2)
+    close("norm", runs[0][0], norm, bound)
+    for got, o in zip(runs[0][1:], outs):
+        close("out", got, *o)
+
+
+def test_past_2_31_values():
+    g = torch.zeros((1 << 31) + 5000, dtype=torch.bfloat16, device=DEV)
+    g[-1], g[0] = 3.0, 4.0
+    assert run([g], 2.5) == 5.0
+    assert g[-1] == 1.5 and g[0] == 2.0 and torch.count_nonzero(g[1 << 30:]) == 1
