@@ -25,10 +25,14 @@ using namespace vio;
 
 constexpr float kLog2E = 1.4426950408889634f, kLog2ELow = 1.9259629911266175e-8f, kLn2 = 0.6931471805599453f;
 
-// e^d for d <= 0: d log2(e) in two parts, so that its rounding does not grow with |d|.
+// e^d for d <= 0, the difference of two logits. fp32 logits' are rounded by up to
+// 2^-24 |d|, which the product with log2(e) would double: its rest is added back.
+// bf16 logits' are exact, or nearly so, and the product's rounding may stay.
+template <bool XB>
 __device__ __forceinline__ float exp_of(float d) {
   const float t = d * kLog2E;
   const float e = __builtin_amdgcn_exp2f(t);
+  if constexpr (XB) return e;
   const float low = fmaf(d, kLog2ELow, fmaf(d, kLog2E, -t));
   return d < -126.f ? e : fmaf(e, low * kLn2, e);  // past it e is 0 or tiny, and -inf - -inf none
 }
@@ -65,11 +69,27 @@ __device__ __forceinline__ void clear(void* dr, int step, int V) {
     for (int e0 = (int)threadIdx.x * VEC; e0 < V; e0 += step) store_some<YB, VEC>(dr, e0, V - e0, zero);
 }
 
-// A block a row, NV groups of VEC values a thread.
-template <bool XB, bool YB, int VEC, int NV>
-__global__ __launch_bounds__(1024) void row_kernel(const CrossEntropyParams p) {
-  __shared__ float red[2][16];
-  const int step = (int)blockDim.x * VEC;
+// dz = e c, and one less 1 / n at the class (of n values from e0 on).
+template <bool YB, int VEC>
+__device__ __forceinline__ void put(void* dr, int e0, int n, int32_t t, float c, float inv_n, float (&e)[VEC]) {
+  if ((uint32_t)(t - e0) < (uint32_t)VEC) {  // one group of the row
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) e[i] = e0 + i == t ? fmaf(e[i], c, -inv_n) : e[i] * c;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) e[i] *= c;
+  }
+  store_some<YB, VEC>(dr, e0, n, e);
+}
+
+// A block a row. A thread holds the first NV groups of VEC values it meets; of
+// the rest (REST: the held part is whole) it keeps the maximum and the sum so
+// far, raised together, and reads them again for the gradient, 16 values at a
+// time, from the caches.
+template <bool XB, bool YB, int VEC, int NV, bool REST>
+__global__ __launch_bounds__(512, REST ? 4 : 6) void row_kernel(const CrossEntropyParams p) {
+  __shared__ float red[2][8];
+  const int step = (int)blockDim.x * VEC, first = (int)threadIdx.x * VEC;
   for (int64_t m = blockIdx.x; m < p.M; m += gridDim.x) {
     const int32_t t = p.targets[m];
     const char* zr = row_at<XB>(p.z, m, p.ldz);
@@ -81,21 +101,44 @@ __global__ __launch_bounds__(1024) void row_kernel(const CrossEntropyParams p) {
     }
     float z[NV][VEC], top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int e0 = k * step + (int)threadIdx.x * VEC;
-      load_some<XB, VEC>(zr, e0, p.V - e0, -INFINITY, z[k]);
-    }
+    for (int k = 0; k < NV; ++k)
+      load_some<XB, VEC>(zr, first + k * step, REST ? VEC : p.V - first - k * step, -INFINITY, z[k]);
     const float zt = load_one<XB>(zr, t);
+    constexpr int U = 16 / VEC;  // groups of the rest in flight
+    if constexpr (REST) {
+      for (int e0 = first + NV * step; e0 < p.V; e0 += U * step) {
+        float v[U][VEC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_some<XB, VEC>(zr, e0 + u * step, p.V - e0 - u * step, -INFINITY, v[u]);
+        float most = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) most = fmaxf(most, v[u][e]);
+        if (most > top) {
+          sum *= exp_of<XB>(top - most);
+          top = most;
+        }
+        const float from = top == -INFINITY ? 0.f : top;  // nothing but -inf so far adds nothing
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) sum += exp_of<XB>(v[u][e] - from);
+      }
+    }
+    const float rest = top;  // of the rest
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) top = fmaxf(top, z[k][e]);
     top = block_max(top, red[0]);
+    // a rest of nothing but -inf adds nothing, unless there was a NaN
+    if (REST && rest > -INFINITY) sum *= exp_of<XB>(rest - top);
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        z[k][e] = exp_of(z[k][e] - top);
+        z[k][e] = exp_of<XB>(z[k][e] - top);
         sum += z[k][e];
       }
     sum = block_sum(sum, red[1]);
@@ -103,162 +146,184 @@ __global__ __launch_bounds__(1024) void row_kernel(const CrossEntropyParams p) {
     if (!dr) continue;
     const float inv_n = 1.f / (float)*p.counted, c = inv_n / sum;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int e0 = k * step + (int)threadIdx.x * VEC;
+    for (int k = 0; k < NV; ++k) put<YB, VEC>(dr, first + k * step, REST ? VEC : p.V - first - k * step, t, c, inv_n, z[k]);
+    if constexpr (REST) {
+      for (int e0 = first + NV * step; e0 < p.V; e0 += U * step) {
+        float v[U][VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) z[k][e] = e0 + e == t ? fmaf(z[k][e], c, -inv_n) : z[k][e] * c;
-      store_some<YB, VEC>(dr, e0, p.V - e0, z[k]);
+        for (int u = 0; u < U; ++u) load_some<XB, VEC>(zr, e0 + u * step, p.V - e0 - u * step, -INFINITY, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[u][e] = exp_of<XB>(v[u][e] - top);
+          put<YB, VEC>(dr, e0 + u * step, p.V - e0 - u * step, t, c, inv_n, v[u]);
+        }
+      }
     }
   }
 }
 
-// A block a row of any length, read twice: the maximum and the sum together,
-// raised where a thread meets a larger value.
+// A row by L lanes of a wave, l each one's place: up to 16 values a lane. The
+// row's loss, in every lane.
 template <bool XB, bool YB, int VEC>
-__global__ __launch_bounds__(1024) void long_kernel(const CrossEntropyParams p) {
-  __shared__ float red[2][16];
-  const int step = (int)blockDim.x * VEC;
-  for (int64_t m = blockIdx.x; m < p.M; m += gridDim.x) {
-    const int32_t t = p.targets[m];
-    const char* zr = row_at<XB>(p.z, m, p.ldz);
-    char* dr = p.dz ? (char*)row_at<YB>(p.dz, m, p.ldd) : nullptr;
-    if ((uint32_t)t >= (uint32_t)p.V) {
-      if (threadIdx.x == 0) p.row_loss[m] = 0.f;
-      clear<YB, VEC>(dr, step, p.V);
-      continue;
-    }
-    float top = -INFINITY, sum = 0.f;
-    const float zt = load_one<XB>(zr, t);
-    for (int e0 = (int)threadIdx.x * VEC; e0 < p.V; e0 += step) {
-      float z[VEC];
-      load_some<XB, VEC>(zr, e0, p.V - e0, -INFINITY, z);
-      float most = top;
+__device__ __forceinline__ float lanes_row(const CrossEntropyParams& p, int64_t m, int l, int L, int n) {
+  constexpr int NV = 16 / VEC;
+  const int32_t t = p.targets[m];
+  const bool counts = (uint32_t)t < (uint32_t)p.V;
+  const char* zr = row_at<XB>(p.z, m, p.ldz);
+  float z[NV][VEC], top = -INFINITY, sum = 0.f, zt = 0.f;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) most = fmaxf(most, z[e]);
-      if (most > top) {
-        sum *= exp_of(top - most);
-        top = most;
-      }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sum += z[e] == -INFINITY ? 0.f : exp_of(z[e] - top);
-    }
-    const float mine = top;
-    top = block_max(top, red[0]);
-    // a thread that met nothing but -inf adds nothing, unless it met a NaN or all did
-    if (mine > -INFINITY || top == -INFINITY) sum *= exp_of(mine - top);
-    sum = block_sum(sum, red[1]);
-    if (threadIdx.x == 0) p.row_loss[m] = (top - zt) + logf(sum);
-    if (!dr) continue;
-    const float inv_n = 1.f / (float)*p.counted, c = inv_n / sum;
-    for (int e0 = (int)threadIdx.x * VEC; e0 < p.V; e0 += step) {
-      float z[VEC];
-      load_some<XB, VEC>(zr, e0, p.V - e0, -INFINITY, z);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        z[e] = exp_of(z[e] - top);
-        z[e] = e0 + e == t ? fmaf(z[e], c, -inv_n) : z[e] * c;
-      }
-      store_some<YB, VEC>(dr, e0, p.V - e0, z);
-    }
+  for (int k = 0; k < NV; ++k) {
+    const int e0 = (l + k * L) * VEC;
+    load_some<XB, VEC>(zr, e0, counts ? p.V - e0 : 0, -INFINITY, z[k]);
   }
+  if (counts) zt = load_one<XB>(zr, t);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) top = fmaxf(top, z[k][e]);
+  top = lanes_max(top, L);
+#pragma unroll
+  for (int k = 0; k < NV; ++k)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      z[k][e] = exp_of<XB>(z[k][e] - top);
+      sum += z[k][e];
+    }
+  sum = lanes_sum(sum, L);
+  const float loss = counts ? (top - zt) + logf(sum) : 0.f;
+  if (l == 0) p.row_loss[m] = loss;
+  if (!p.dz) return loss;
+  char* dr = (char*)row_at<YB>(p.dz, m, p.ldd);
+  const float inv_n = 1.f / (float)n, c = inv_n / sum;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int e0 = (l + k * L) * VEC;
+    if (!counts)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) z[k][e] = 0.f;
+    put<YB, VEC>(dr, e0, p.V - e0, counts ? t : -1, counts ? c : 0.f, inv_n, z[k]);
+  }
+  return loss;
 }
 
-// L lanes a row, NV values a lane, one after another: short rows.
-template <bool XB, bool YB, int NV>
+// Short rows: 256 / L a block.
+template <bool XB, bool YB, int VEC>
 __global__ __launch_bounds__(256) void lanes_kernel(const CrossEntropyParams p, int L, int L_shift) {
-  const int l = threadIdx.x & (L - 1);
   const int64_t rows = 256 >> L_shift;
+  const int n = p.dz ? *p.counted : 1;
   // a row's lanes stay together
-  for (int64_t m = (int64_t)blockIdx.x * rows + (threadIdx.x >> L_shift); m < p.M; m += gridDim.x * rows) {
-    const int32_t t = p.targets[m];
-    const bool counts = (uint32_t)t < (uint32_t)p.V;
-    const char* zr = row_at<XB>(p.z, m, p.ldz);
-    float z[NV], top = -INFINITY, sum = 0.f, zt = 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int v = l + (k << L_shift);
-      z[k] = counts && v < p.V ? load_one<XB>(zr, v) : -INFINITY;
-    }
-    if (counts) zt = load_one<XB>(zr, t);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) top = fmaxf(top, z[k]);
-    top = lanes_max(top, L);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      z[k] = exp_of(z[k] - top);
-      sum += z[k];
-    }
-    sum = lanes_sum(sum, L);
-    if (l == 0) p.row_loss[m] = counts ? (top - zt) + logf(sum) : 0.f;
-    if (!p.dz) continue;
-    const float inv_n = counts ? 1.f / (float)*p.counted : 0.f, c = inv_n / sum;
-    char* dr = (char*)row_at<YB>(p.dz, m, p.ldd);
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int v = l + (k << L_shift);
-      if (v < p.V) store_one<YB>(dr, v, !counts ? 0.f : v == t ? fmaf(z[k], c, -inv_n) : z[k] * c);
-    }
-  }
+  for (int64_t m = (int64_t)blockIdx.x * rows + (threadIdx.x >> L_shift); m < p.M; m += gridDim.x * rows)
+    lanes_row<XB, YB, VEC>(p, m, threadIdx.x & (L - 1), L, n);
 }
 
-__global__ __launch_bounds__(1024) void count_kernel(const Index targets, int64_t M, int64_t V, int32_t* counted) {
-  __shared__ int32_t red[16];
-  int n = 0;
-#pragma unroll 8
-  for (int64_t m = threadIdx.x; m < M; m += 1024) n += (uint32_t)targets[m] < (uint64_t)V;
+__device__ __forceinline__ int block_count(int n, int* red) {
   for (int o = 32; o; o >>= 1) n += __shfl_xor(n, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = n;
   __syncthreads();
-  if (threadIdx.x) return;
   n = 0;
-  for (int w = 0; w < 16; ++w) n += red[w];
-  *counted = n;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) n += red[w];
+  return n;
 }
 
-// loss = sum of the rows' in a fixed order / n; 0 where no row counts
-__global__ __launch_bounds__(1024) void mean_kernel(const float* row_loss, int64_t M, const int32_t* counted, float* loss) {
+// A few short rows: the count, the rows and the mean by one block, one launch.
+template <bool XB, bool YB, int VEC>
+__global__ __launch_bounds__(1024) void few_kernel(const CrossEntropyParams p, int L, int L_shift, float* loss) {
   __shared__ float red[16];
+  __shared__ int counts[16];
+  int n = 0;
+  for (int64_t m = threadIdx.x; m < p.M; m += 1024) n += (uint32_t)p.targets[m] < (uint32_t)p.V;
+  n = block_count(n, counts);
+  float sum = 0.f;
+  for (int64_t m = threadIdx.x >> L_shift; m < p.M; m += 1024 >> L_shift) {
+    const float one = lanes_row<XB, YB, VEC>(p, m, threadIdx.x & (L - 1), L, n);
+    if ((threadIdx.x & (L - 1)) == 0) sum += one;
+  }
+  sum = block_sum(sum, red);
+  if (loss && threadIdx.x == 0) *loss = n > 0 ? sum / (float)n : 0.f;
+}
+
+// How many rows count; the mean of their losses, 0 where none does. Blocks take
+// shares of the rows, and one adds their results in order.
+__global__ __launch_bounds__(1024) void count_kernel(const Index targets, int64_t M, int64_t V, int32_t* out) {
+  __shared__ int red[16];
+  const int64_t share = (M + gridDim.x - 1) / gridDim.x, m0 = blockIdx.x * share, m1 = min(m0 + share, M);
+  int n = 0;
+#pragma unroll 8
+  for (int64_t m = m0 + threadIdx.x; m < m1; m += 1024) n += (uint32_t)targets[m] < (uint64_t)V;
+  n = block_count(n, red);
+  if (threadIdx.x == 0) out[blockIdx.x] = n;
+}
+__global__ __launch_bounds__(kCrossEntropyParts) void add_counts_kernel(const int32_t* part, int parts, int32_t* counted) {
+  __shared__ int red[16];
+  const int n = block_count((int)threadIdx.x < parts ? part[threadIdx.x] : 0, red);
+  if (threadIdx.x == 0) *counted = n;
+}
+// counted NULL: the sum, not the mean
+__global__ __launch_bounds__(1024) void mean_kernel(const float* row_loss, int64_t M, const int32_t* counted, float* out) {
+  __shared__ float red[16];
+  const int64_t share = (M + gridDim.x - 1) / gridDim.x, m0 = blockIdx.x * share, m1 = min(m0 + share, M);
   float s = 0.f;
 #pragma unroll 8
-  for (int64_t m = threadIdx.x; m < M; m += 1024) s += row_loss[m];
+  for (int64_t m = m0 + threadIdx.x; m < m1; m += 1024) s += row_loss[m];
   s = block_sum(s, red);
-  const int n = *counted;
-  if (threadIdx.x == 0) *loss = n > 0 ? s / (float)n : 0.f;
+  if (threadIdx.x) return;
+  if (!counted) {
+    out[blockIdx.x] = s;
+  } else {
+    const int n = *counted;
+    *out = n > 0 ? s / (float)n : 0.f;
+  }
 }
 
 constexpr int64_t kMostBlocks = 1 << 20;  // a launch has fewer than 2^32 threads
 
 template <bool XB, bool YB>
-hipError_t rows(const CrossEntropyParams& p, const CrossEntropyForm& f, hipStream_t stream) {
+hipError_t rows(const CrossEntropyParams& p, const CrossEntropyForm& f, float* loss, hipStream_t stream) {
   constexpr int VEC = XB ? 8 : 4;  // of the logits alone: a row's loss does not depend on what else is asked for
+  if (f.few) {
+    few_kernel<XB, YB, VEC><<<1, 1024, 0, stream>>>(p, f.L, f.L_shift, loss);
+    return hipGetLastError();
+  }
   if (f.L) {
     const int64_t per = 256 >> f.L_shift;
-    lanes_kernel<XB, YB, 8><<<dim3((unsigned)std::min((p.M + per - 1) / per, kMostBlocks)), 256, 0, stream>>>(p, f.L, f.L_shift);
+    lanes_kernel<XB, YB, VEC><<<dim3((unsigned)std::min((p.M + per - 1) / per, kMostBlocks)), 256, 0, stream>>>(p, f.L, f.L_shift);
     return hipGetLastError();
   }
   const dim3 grid((unsigned)std::min(p.M, kMostBlocks));
-  if (f.values == 0) long_kernel<XB, YB, VEC><<<grid, f.threads, 0, stream>>>(p);
-  else if (f.values <= 16) row_kernel<XB, YB, VEC, 16 / VEC><<<grid, f.threads, 0, stream>>>(p);
-  else if (f.values <= 32) row_kernel<XB, YB, VEC, 32 / VEC><<<grid, f.threads, 0, stream>>>(p);
-  else row_kernel<XB, YB, VEC, 64 / VEC><<<grid, f.threads, 0, stream>>>(p);
+  if (f.values <= 16) row_kernel<XB, YB, VEC, 16 / VEC, false><<<grid, f.threads, 0, stream>>>(p);
+  else if (f.values <= 32) row_kernel<XB, YB, VEC, 32 / VEC, false><<<grid, f.threads, 0, stream>>>(p);
+  else row_kernel<XB, YB, VEC, 32 / VEC, true><<<grid, f.threads, 0, stream>>>(p);
   return hipGetLastError();
 }
+
+int parts_of(int64_t M) { return (int)std::min<int64_t>(kCrossEntropyParts, (M + kCrossEntropyPartRows - 1) / kCrossEntropyPartRows); }
 
 }  // namespace xent
 
-hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, int32_t* counted, hipStream_t stream) {
-  xent::count_kernel<<<1, 1024, 0, stream>>>(targets, M, V, counted);
+hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, int32_t* part, int32_t* counted,
+                               hipStream_t stream) {
+  const int parts = xent::parts_of(M);
+  xent::count_kernel<<<dim3(parts > 1 ? parts : 1), 1024, 0, stream>>>(targets, M, V, parts > 1 ? part : counted);
+  if (parts > 1) xent::add_counts_kernel<<<1, kCrossEntropyParts, 0, stream>>>(part, parts, counted);
   return hipGetLastError();
 }
 
-hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16,
+hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16, float* loss,
                               hipStream_t stream) {
-  if (z_bf16) return d_bf16 ? xent::rows<true, true>(p, f, stream) : xent::rows<true, false>(p, f, stream);
-  return d_bf16 ? xent::rows<false, true>(p, f, stream) : xent::rows<false, false>(p, f, stream);
+  if (z_bf16) return d_bf16 ? xent::rows<true, true>(p, f, loss, stream) : xent::rows<true, false>(p, f, loss, stream);
+  return d_bf16 ? xent::rows<false, true>(p, f, loss, stream) : xent::rows<false, false>(p, f, loss, stream);
 }
 
-hipError_t cross_entropy_mean(const float* row_loss, int64_t M, const int32_t* counted, float* loss, hipStream_t stream) {
-  xent::mean_kernel<<<1, 1024, 0, stream>>>(row_loss, M, counted, loss);
+hipError_t cross_entropy_mean(const float* row_loss, int64_t M, float* part, const int32_t* counted, float* loss,
+                              hipStream_t stream) {
+  const int parts = xent::parts_of(M);
+  if (parts > 1) {
+    xent::mean_kernel<<<dim3(parts), 1024, 0, stream>>>(row_loss, M, nullptr, part);
+    xent::mean_kernel<<<1, 1024, 0, stream>>>(part, parts, counted, loss);
+  } else {
+    xent::mean_kernel<<<1, 1024, 0, stream>>>(row_loss, M, counted, loss);
+  }
   return hipGetLastError();
 }
 

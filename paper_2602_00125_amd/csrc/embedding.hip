@@ -22,6 +22,8 @@
 //    in order.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "language.hpp"
 
 namespace mt {
@@ -29,57 +31,38 @@ namespace embedding {
 
 using namespace vio;
 
-// VEC values a lane, G lanes a row (or a tile of it: blockIdx.y), 256 / G rows a block.
-template <bool TB, bool YB, int VEC>
+// VEC values a lane, G lanes a row (or a tile of it: blockIdx.y), U rows at a time.
+template <bool TB, bool YB, int VEC, int U>
 __global__ __launch_bounds__(256) void fwd_kernel(const EmbeddingParams p, int G_shift) {
-  const int G = 1 << G_shift;
-  const int64_t d = ((int64_t)blockIdx.y * G + (threadIdx.x & (G - 1))) * VEC;
-  if (d >= p.D) return;
-  const int64_t step = (int64_t)gridDim.x * (256 >> G_shift);
-  for (int64_t m = (int64_t)blockIdx.x * (256 >> G_shift) + (threadIdx.x >> G_shift); m < p.M; m += step) {
-    const int32_t id = p.ids[m];
-    float v[VEC];
+  const int G = 1 << G_shift, rows = 256 >> G_shift;
+  const int d = ((int)blockIdx.y * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
+  if (n <= 0) return;
+  for (int64_t m0 = (int64_t)blockIdx.x * rows * U + (threadIdx.x >> G_shift); m0 < p.M; m0 += (int64_t)gridDim.x * rows * U) {
+    int32_t id[U];
+    float v[U][VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) v[e] = 0.f;
-    if ((uint32_t)id < (uint64_t)p.V) {
-      load_some<TB, VEC>(p.table, id * p.ldt + d, (int)(p.D - d), 0.f, v);
+    for (int u = 0; u < U; ++u) id[u] = m0 + u * rows < p.M ? p.ids[m0 + u * rows] : -1;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] *= p.scale;
+    for (int u = 0; u < U; ++u)
+      load_some<TB, VEC>(p.table, id[u] * p.ldt + d, (uint32_t)id[u] < (uint64_t)p.V ? n : 0, 0.f, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[u][e] = (uint32_t)id[u] < (uint64_t)p.V ? v[u][e] * p.scale : 0.f;
+      store_some<YB, VEC>(p.y, (m0 + u * rows) * p.ldy + d, m0 + u * rows < p.M ? n : 0, v[u]);
     }
-    store_some<YB, VEC>(p.y, m * p.ldy + d, (int)(p.D - d), v);
   }
 }
 
+constexpr int64_t kManyBlocks = 4096;
 constexpr int kGroupWaves = 16, kGroupThreads = 64 * kGroupWaves;
 constexpr int kAhead = 8;  // loads of ids in flight a lane
-
-// Clears the rows of dE, by blocks of kGroupThreads.
-__device__ __forceinline__ void clear(const EmbeddingGradParams& p, int64_t block, int64_t blocks) {
-  const int64_t total = p.V * p.D, first = block * kGroupThreads + threadIdx.x, step = blocks * kGroupThreads;
-  if (p.ldt == p.D) {
-    // up to three values before the first 16-byte boundary and after the last
-    const int64_t head = min((int64_t)((16 - ((uintptr_t)p.dtable & 15)) & 15) / 4, total), quads = (total - head) / 4;
-    f32x4* q = (f32x4*)(p.dtable + head);
-    for (int64_t i = first; i < quads; i += step) q[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (first < head) p.dtable[first] = 0.f;
-    if (head + 4 * quads + first < total) p.dtable[head + 4 * quads + first] = 0.f;
-  } else {
-    for (int64_t i = first; i < total; i += step) {
-      const int64_t v = i / p.D;
-      p.dtable[v * p.ldt + (i - v * p.D)] = 0.f;
-    }
-  }
-}
 
 // counts: [kGroupWaves][locals], of the bucket's ids local 2^shift + bucket.
 __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGradParams p, int locals) {
   __shared__ int32_t counts[kGroupWaves * kEmbedBucketIds];
   __shared__ int32_t wave_lower[kGroupWaves], wave_sum[kGroupWaves];
   const int buckets = 1 << p.bucket_shift, bucket = blockIdx.x;
-  if (bucket >= buckets) {
-    clear(p, bucket - buckets, gridDim.x - buckets);
-    return;
-  }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for (int i = threadIdx.x; i < kGroupWaves * locals; i += kGroupThreads) counts[i] = 0;
   __syncthreads();
@@ -123,12 +106,16 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGra
     own += wave_lower[w] + wave_sum[w];
   }
   if (bucket == buckets - 1 && threadIdx.x == 0) *p.total = own;  // of all buckets
-  for (int l = l0; l < l1; ++l)
+  for (int l = l0; l < l1; ++l) {
+    const int from = at;
     for (int w = 0; w < kGroupWaves; ++w) {
       const int n = counts[w * locals + l];
       counts[w * locals + l] = at;
       at += n;
     }
+    const int64_t v = ((int64_t)l << p.bucket_shift) + bucket;
+    if (v < p.V) p.seen[v] = at > from;
+  }
   __syncthreads();
   for (int64_t m = m0; m < m1; m += 64 * kAhead) {
     int32_t id[kAhead];
@@ -158,71 +145,81 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGra
   }
 }
 
-// dE's values from column d on (+)= s sum
+// dE[id] = s sum (+ old), n values from column d on.
 template <int VEC>
-__device__ __forceinline__ void put(const EmbeddingGradParams& p, int32_t id, int64_t d, const float (&sum)[VEC]) {
-  float* row = p.dtable + id * p.ldt;
+__device__ __forceinline__ void put(const EmbeddingGradParams& p, int32_t id, int d, int n, const float (&sum)[VEC], const float (&old)[VEC]) {
   float v[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) v[e] = p.scale * sum[e];
-  if (p.accumulate) {
-    float old[VEC];
-    load_some<false, VEC>(row, d, (int)(p.D - d), 0.f, old);
+  if (p.accumulate)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[e] += old[e];
+  store_some<false, VEC>(p.dtable, id * p.ldt + d, n, v);
+}
+template <int VEC>
+__device__ __forceinline__ void load_old(const EmbeddingGradParams& p, int32_t id, int d, int n, float (&old)[VEC]) {
+  load_some<false, VEC>(p.dtable, id * p.ldt + d, p.accumulate ? n : 0, 0.f, old);
+}
+
+// Rows without a token become 0, by blocks past those of the sums.
+__device__ __forceinline__ void clear(const EmbeddingGradParams& p, int64_t block, int64_t blocks, int G_shift) {
+  const int G = 1 << G_shift, rows = 256 >> G_shift;
+  const float zero[4] = {};
+  for (int64_t v = block * rows + (threadIdx.x >> G_shift); v < p.V; v += blocks * rows) {
+    if (p.seen[v]) continue;
+    for (int d = (threadIdx.x & (G - 1)) * 4; d < p.D; d += G * 4) store_some<false, 4>(p.dtable, v * p.ldt + d, (int)p.D - d, zero);
   }
-  store_some<false, VEC>(row, d, (int)(p.D - d), v);
 }
 
 template <bool BF, int VEC>
-__global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, int G_shift) {
-  constexpr int U = 4;  // rows in flight
-  const int G = 1 << G_shift;
-  const int64_t c = (int64_t)blockIdx.x * (256 >> G_shift) + (threadIdx.x >> G_shift);
-  const int64_t d = ((int64_t)blockIdx.y * G + (threadIdx.x & (G - 1))) * VEC;
+__global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, int G_shift, int tiles, int sum_blocks, int clear_shift) {
+  if ((int)blockIdx.x >= sum_blocks) {
+    clear(p, blockIdx.x - sum_blocks, gridDim.x - sum_blocks, clear_shift);
+    return;
+  }
+  constexpr int U = 32 / VEC;  // rows in flight
+  const int G = 1 << G_shift, tile = blockIdx.x % tiles;
+  const int64_t c = (int64_t)(blockIdx.x / tiles) * (256 >> G_shift) + (threadIdx.x >> G_shift);
+  const int d = (tile * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
   const int64_t total = *p.total, i0 = c * p.chunk, i1 = min(i0 + p.chunk, total);
-  if (i0 >= i1 || d >= p.D) return;
-  const int32_t before = i0 > 0 ? p.id[i0 - 1] : -1, after = i1 < total ? p.id[i1] : -1;
-  int32_t cur = p.id[i0];
-  bool cut = cur == before;  // the run began in an earlier chunk
+  if (i0 >= i1 || n <= 0) return;
+  bool cut = i0 > 0 && p.id[i0 - 1] == p.id[i0];  // the run began in an earlier chunk
   float acc[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
   for (int64_t i = i0; i < i1; i += U) {
-    int32_t id[U];
-    float v[U][VEC];
+    int32_t id[U + 1], pos[U];
+    float v[U][VEC], old[U][VEC];
+#pragma unroll
+    for (int u = 0; u <= U; ++u) id[u] = i + u < total ? p.id[i + u] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) pos[u] = i + u < i1 ? p.pos[i + u] : 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      id[u] = -1;
-      if (i + u < i1) {
-        id[u] = p.id[i + u];
-        load_some<BF, VEC>(p.dy, p.pos[i + u] * p.ldy + d, (int)(p.D - d), 0.f, v[u]);
-      }
+      load_some<BF, VEC>(p.dy, pos[u] * p.ldy + d, i + u < i1 ? n : 0, 0.f, v[u]);
+      load_old(p, id[u], d, i + u < i1 && id[u] != id[u + 1] ? n : 0, old[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (id[u] < 0) break;
-      if (id[u] != cur) {
-        if (cut) store_some<false, VEC>(p.head + c * p.D, d, (int)(p.D - d), acc);
-        else put<VEC>(p, cur, d, acc);
-        cur = id[u];
-        cut = false;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-      }
+      if (i + u >= i1) break;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) acc[e] += v[u][e];
+      const bool ends = id[u] != id[u + 1];
+      if (!ends && i + u < i1 - 1) continue;
+      if (cut) store_some<false, VEC>(p.head, c * p.D + d, n, acc);
+      else if (ends) put(p, id[u], d, n, acc, old[u]);
+      else store_some<false, VEC>(p.tail, c * p.D + d, n, acc);
+      cut = false;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
     }
   }
-  if (cut) store_some<false, VEC>(p.head + c * p.D, d, (int)(p.D - d), acc);
-  else if (cur == after) store_some<false, VEC>(p.tail + c * p.D, d, (int)(p.D - d), acc);
-  else put<VEC>(p, cur, d, acc);
 }
 
 // A block for each chunk whose last run began in it and goes on. Its 256 / G
 // groups of lanes take the later pieces in turn; their sums meet in LDS.
-template <int VEC>
 __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, int G_shift) {
+  constexpr int VEC = 4, U = 8;
   __shared__ float sums[256 * VEC];
   const int G = 1 << G_shift, groups = 256 >> G_shift, grp = threadIdx.x >> G_shift, lane = threadIdx.x & 63;
   const int64_t c = blockIdx.x, total = *p.total, i0 = c * p.chunk, i1 = i0 + p.chunk;
@@ -238,75 +235,83 @@ __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, 
     pieces += n;
     if (n < 64) break;
   }
-  const int64_t d = ((int64_t)blockIdx.y * G + (threadIdx.x & (G - 1))) * VEC;
-  float acc[VEC];
+  const int d = ((int)blockIdx.y * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
+  float acc[VEC], old[VEC];
+  // a group takes a share of the pieces, one after another
+  const int64_t share = (pieces + groups - 1) / groups, j1 = min((grp + 1) * share, pieces);
+  load_some<false, VEC>(p.tail, c * p.D + d, grp == 0 ? n : 0, 0.f, acc);
+  load_old(p, id, d, grp == 0 ? n : 0, old);
+  for (int64_t j = grp * share; j < j1; j += U) {
+    float v[U][VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-  if (d < p.D) {
-    // a group takes a share of the pieces, one after another
-    const int64_t share = (pieces + groups - 1) / groups, j0 = grp * share, j1 = min(j0 + share, pieces);
-    if (grp == 0) load_some<false, VEC>(p.tail + c * p.D, d, (int)(p.D - d), 0.f, acc);
-#pragma unroll 4
-    for (int64_t j = j0; j < j1; ++j) {
-      float v[VEC];
-      load_some<false, VEC>(p.head + (c + 1 + j) * p.D, d, (int)(p.D - d), 0.f, v);
+    for (int u = 0; u < U; ++u) load_some<false, VEC>(p.head, (c + 1 + j + u) * p.D + d, j + u < j1 ? n : 0, 0.f, v[u]);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] += v[e];
-    }
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] += v[u][e];
   }
 #pragma unroll
   for (int e = 0; e < VEC; ++e) sums[threadIdx.x * VEC + e] = acc[e];
   __syncthreads();
-  if (grp || d >= p.D) return;
+  if (grp || n <= 0) return;
   for (int g = 1; g < groups; ++g)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] += sums[(g * G + threadIdx.x) * VEC + e];
-  put<VEC>(p, id, d, acc);
+  put(p, id, d, n, acc, old);
 }
 
-// Lanes of a row: a power of two, 256 at most.
-int lanes_shift(int64_t D, int vec) {
+// Lanes of a row: a power of two, 2^most at most.
+int lanes_shift(int64_t D, int vec, int most) {
   int s = 0;
-  while (s < 8 && (int64_t)vec << s < D) ++s;
+  while (s < most && (int64_t)vec << s < D) ++s;
   return s;
+}
+
+template <bool TB, bool YB, int VEC>
+hipError_t lookup(const EmbeddingParams& p, hipStream_t stream) {
+  const int s = lanes_shift(p.D, VEC, 8);
+  const int64_t rows = 256 >> s, tile = (int64_t)VEC << s, tiles = (p.D + tile - 1) / tile;
+  auto grid = [&](int U) { return dim3((unsigned)std::min<int64_t>((p.M + rows * U - 1) / (rows * U), 1 << 22), (unsigned)tiles); };
+  if (p.M / rows * tiles >= kManyBlocks) fwd_kernel<TB, YB, VEC, 4><<<grid(4), 256, 0, stream>>>(p, s);
+  else fwd_kernel<TB, YB, VEC, 1><<<grid(1), 256, 0, stream>>>(p, s);
+  return hipGetLastError();
 }
 
 }  // namespace embedding
 
 hipError_t embedding_fwd(const EmbeddingParams& p, bool t_bf16, bool y_bf16, hipStream_t stream) {
   using namespace embedding;
-  const int vec = t_bf16 || y_bf16 ? 8 : 4, s = lanes_shift(p.D, vec);
-  const int64_t rows = 256 >> s, tile = (int64_t)vec << s;
-  const int64_t blocks = (p.M + rows - 1) / rows;
-  const dim3 grid((unsigned)(blocks < (1 << 22) ? blocks : 1 << 22), (unsigned)((p.D + tile - 1) / tile));
-  if (t_bf16) {
-    if (y_bf16) fwd_kernel<true, true, 8><<<grid, 256, 0, stream>>>(p, s);
-    else fwd_kernel<true, false, 8><<<grid, 256, 0, stream>>>(p, s);
-  } else {
-    if (y_bf16) fwd_kernel<false, true, 8><<<grid, 256, 0, stream>>>(p, s);
-    else fwd_kernel<false, false, 4><<<grid, 256, 0, stream>>>(p, s);
-  }
-  return hipGetLastError();
+  if (t_bf16) return y_bf16 ? lookup<true, true, 8>(p, stream) : lookup<true, false, 8>(p, stream);
+  return y_bf16 ? lookup<false, true, 8>(p, stream) : lookup<false, false, 4>(p, stream);
 }
 
-hipError_t embedding_bwd(const EmbeddingGradParams& p, bool bf16, hipStream_t stream) {
+EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D, bool bf16) {
+  EmbeddingGradForm f;
+  const int vec = bf16 ? 8 : 4;
+  f.shift = embedding::lanes_shift(D, vec, 6);
+  f.tiles = (int32_t)((D + ((int64_t)vec << f.shift) - 1) / ((int64_t)vec << f.shift));
+  const int64_t groups = (int64_t)4096 * (64 >> f.shift);
+  for (f.chunk = 8; f.chunk < 64 && (M + f.chunk - 1) / f.chunk * f.tiles > groups; f.chunk *= 2) {}
+  f.chunks = (int32_t)((M + f.chunk - 1) / f.chunk);
+  return f;
+}
+
+hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& f, bool bf16, hipStream_t stream) {
   using namespace embedding;
   const int buckets = 1 << p.bucket_shift, locals = (int)((p.V + buckets - 1) >> p.bucket_shift);
-  // blocks that clear: 16 KB each at a time, two a CU at most
-  int64_t clear = p.accumulate ? 0 : (p.V * p.D + 4095) / 4096;
-  if (clear > 512) clear = 512;
-  group_kernel<<<dim3((unsigned)(buckets + clear)), kGroupThreads, 0, stream>>>(p, locals);
+  group_kernel<<<dim3((unsigned)buckets), kGroupThreads, 0, stream>>>(p, locals);
+  const int rows = 256 >> f.shift, clear_shift = lanes_shift(p.D, 4, 6);
+  const int64_t sums = (f.chunks + rows - 1) / rows * (int64_t)f.tiles;
+  // 16 KB each at a time, eight a CU at most
+  const int64_t clears = p.accumulate ? 0 : std::min<int64_t>((p.V * p.D + 4095) / 4096, 2048);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.M == 0) return e;
-  const int vec = bf16 ? 8 : 4, s = lanes_shift(p.D, vec);
-  const int64_t rows = 256 >> s, tile = (int64_t)vec << s;
-  const dim3 sums((unsigned)((p.chunks + rows - 1) / rows), (unsigned)((p.D + tile - 1) / tile));
-  if (bf16) sum_kernel<true, 8><<<sums, 256, 0, stream>>>(p, s);
-  else sum_kernel<false, 4><<<sums, 256, 0, stream>>>(p, s);
-  if ((e = hipGetLastError()) != hipSuccess || p.chunks < 2) return e;
-  const dim3 joins((unsigned)p.chunks, sums.y);
-  if (bf16) join_kernel<8><<<joins, 256, 0, stream>>>(p, s);
-  else join_kernel<4><<<joins, 256, 0, stream>>>(p, s);
+  if (e != hipSuccess || sums + clears == 0) return e;
+  const dim3 grid((unsigned)(sums + clears));
+  if (bf16) sum_kernel<true, 8><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, (int)sums, clear_shift);
+  else sum_kernel<false, 4><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, (int)sums, clear_shift);
+  if ((e = hipGetLastError()) != hipSuccess || f.chunks < 2) return e;
+  const int s = lanes_shift(p.D, 4, 6);
+  join_kernel<<<dim3((unsigned)f.chunks, (unsigned)((p.D + (4 << s) - 1) / (4 << s))), 256, 0, stream>>>(p, s);
   return hipGetLastError();
 }
 

@@ -29,14 +29,20 @@ struct EmbeddingGradParams {
   int64_t M, V, D, ldy, ldt;
   float scale;
   int accumulate;
-  int32_t chunk, chunks;       // tokens of a chunk, chunks of M tokens
+  int32_t chunk;               // tokens of a chunk
   int32_t bucket_shift;        // 2^bucket_shift buckets: the low bits of an id
   int32_t* total;              // tokens with an id in range
   int32_t *id, *pos;           // [M]: ids grouped, and the tokens they come from
+  uint8_t* seen;               // [V]: whether a row has a token
   float *head, *tail;          // [chunks][D]: a run that began before the chunk; one that ends after it
 };
 constexpr int kEmbedBucketIds = 1024;  // ids of a bucket, at most
-hipError_t embedding_bwd(const EmbeddingGradParams& p, bool bf16, hipStream_t stream);
+// How the sums are shared out: 2^shift lanes a row or tile of it, chunks of tokens.
+struct EmbeddingGradForm {
+  int32_t shift, tiles, chunk, chunks;
+};
+EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D, bool bf16);
+hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& f, bool bf16, hipStream_t stream);
 
 constexpr int kLayerNormMaxC = 16384;
 struct LayerNormParams {
@@ -69,13 +75,20 @@ struct CrossEntropyParams {
 };
 // How a row is held (cross_entropy.hip).
 struct CrossEntropyForm {
-  int32_t threads, values;  // values a thread holds; 0: none, the row is read twice
-  int32_t L, L_shift;            // lanes a row where a wave holds several, else 0
+  int32_t threads, values;  // a block a row: values a thread meets
+  int32_t L, L_shift;       // lanes a row where a wave holds several, else 0
+  bool few;                 // one launch of one block for everything
 };
-hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, int32_t* counted, hipStream_t stream);
-hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16,
+// The passes over the rows' classes and losses: shares of kCrossEntropyPartRows
+// rows, up to kCrossEntropyParts of them.
+constexpr int kCrossEntropyParts = 256, kCrossEntropyPartRows = 16384;
+hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, int32_t* part, int32_t* counted,
+                               hipStream_t stream);
+// loss: written where f.few
+hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16, float* loss,
                               hipStream_t stream);
-hipError_t cross_entropy_mean(const float* row_loss, int64_t M, const int32_t* counted, float* loss, hipStream_t stream);
+hipError_t cross_entropy_mean(const float* row_loss, int64_t M, float* part, const int32_t* counted, float* loss,
+                              hipStream_t stream);
 
 // Up to kClipTensors tensors of a launch, cut into chunks of kClipChunk values.
 constexpr int kClipTensors = 120;

@@ -109,18 +109,6 @@ mt_status embedding_fwd_impl(const mt_tensor* ids, const mt_tensor* table, float
   return hip_status(mt::embedding_fwd(p, table->dtype == MT_BF16, y->dtype == MT_BF16, stream));
 }
 
-namespace {
-// Tokens of a chunk: two blocks a CU of 256 lanes, at least 16 tokens.
-int embedding_chunk(int64_t M, int64_t D, int vec) {
-  int64_t lanes = 1;
-  while (lanes < 256 && lanes * vec < D) lanes *= 2;
-  const int64_t tiles = cdiv(D, lanes * vec), rows = 256 / lanes;  // a block takes `rows` chunks of a tile
-  int chunk = 16;
-  while (chunk < 256 && cdiv(cdiv(M, chunk), rows) * tiles > 2048) chunk *= 2;
-  return chunk;
-}
-}  // namespace
-
 mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float scale, const mt_tensor* dtable,
                              uint32_t flags, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
   if (flags & ~MT_ACCUMULATE) return fail(MT_ERR_INVALID, "mt_embedding_bwd: unknown flags");
@@ -139,10 +127,10 @@ mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float sc
   if (p.M > (1 << 26)) return fail(MT_ERR_SHAPE, "more than 2^26 tokens");
   if (!std::isfinite(scale)) return fail(MT_ERR_INVALID, "scale must be finite");
   if ((s = check_apart({dtable}, {ids, dy}))) return s;
-  p.chunk = embedding_chunk(p.M, p.D, vector_of({dy}));
-  p.chunks = (int32_t)cdiv(p.M, p.chunk);
-  const size_t list = round256(p.M * sizeof(int32_t)), sums = round256((size_t)p.chunks * p.D * sizeof(float));
-  const size_t need = p.V && p.D ? 256 + 2 * list + 2 * sums : 0;
+  const mt::EmbeddingGradForm f = mt::embedding_grad_form(p.M, p.D, dy->dtype == MT_BF16);
+  p.chunk = f.chunk;
+  const size_t list = round256(p.M * sizeof(int32_t)), sums = round256((size_t)f.chunks * p.D * sizeof(float));
+  const size_t need = p.V && p.D ? 256 + 2 * list + 2 * sums + round256(p.V) : 0;
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
@@ -155,6 +143,7 @@ mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float sc
   p.pos = (int32_t*)(at += list);
   p.head = (float*)(at += list);
   p.tail = (float*)(at += sums);
+  p.seen = (uint8_t*)(at += sums);
   p.dy = dy->data;
   p.dtable = (float*)dtable->data;
   p.ldy = row_pitch(dy);
@@ -165,7 +154,7 @@ mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float sc
   while (p.bucket_shift < 8 && (int64_t)1 << p.bucket_shift < p.V) ++p.bucket_shift;
   while (p.V > (int64_t)mt::kEmbedBucketIds << p.bucket_shift) ++p.bucket_shift;
   (void)hipGetLastError();
-  return hip_status(mt::embedding_bwd(p, dy->dtype == MT_BF16, stream));
+  return hip_status(mt::embedding_bwd(p, f, dy->dtype == MT_BF16, stream));
 }
 
 // --------------------------------------------------------------- layer norm
@@ -282,7 +271,7 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
   const int64_t V = logits->shape[1];
   if (n != p.M) return fail(MT_ERR_SHAPE, "targets must hold one class for each row of logits");
   if (V < 1 || V > (1 << 24)) return fail(MT_ERR_SHAPE, "a row must have 1 to 2^24 logits");
-  const size_t need = 256 + round256(p.M * sizeof(float));
+  const size_t need = 256 + kCrossEntropyParts * sizeof(float) + round256(p.M * sizeof(float));
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
@@ -303,9 +292,10 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
       (s = check_workspace(ws, ws_bytes, need, "mt_cross_entropy")))
     return s;
   int32_t* counted = (int32_t*)ws;
+  void* part = (char*)ws + 256;
   p.V = (int32_t)V;
   p.counted = counted;
-  p.row_loss = losses && p.M ? (float*)losses->data : (float*)((char*)ws + 256);
+  p.row_loss = losses && p.M ? (float*)losses->data : (float*)((char*)part + kCrossEntropyParts * sizeof(float));
   p.z = logits->data;
   p.ldz = row_pitch(logits);
   const bool zb = logits->dtype == MT_BF16, db = dlogits ? dlogits->dtype == MT_BF16 : zb;
@@ -313,19 +303,20 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
     p.dz = dlogits->data;
     p.ldd = row_pitch(dlogits);
   }
-  mt::CrossEntropyForm f{256, 0, 0, 0};
-  if (V <= 512) {
-    for (f.L = 1; f.L < 64 && f.L * 8 < V; f.L *= 2) ++f.L_shift;
+  mt::CrossEntropyForm f{64, 0, 0, 0, false};
+  if (V <= 1024) {
+    for (f.L = 1; f.L < 64 && f.L * 16 < V; f.L *= 2) ++f.L_shift;
+    f.few = p.M * f.L <= 4096;
   } else {
-    while (f.threads < 1024 && (int64_t)f.threads * 64 < V) f.threads *= 2;
-    if ((int64_t)f.threads * 64 >= V) f.values = (int32_t)cdiv(V, f.threads);
+    while (f.threads < 512 && f.threads * (zb ? 32 : 16) < V) f.threads *= 2;
+    f.values = (int32_t)cdiv(V, f.threads);
   }
+  float* to = loss ? (float*)loss->data : nullptr;
   (void)hipGetLastError();
-  const hipStream_t st = stream;
-  if ((s = hip_status(mt::cross_entropy_count(p.targets, p.M, V, counted, st)))) return s;
-  if (p.M > 0 && (s = hip_status(mt::cross_entropy_rows(p, f, zb, db, st)))) return s;
-  if (!loss) return MT_OK;
-  return hip_status(mt::cross_entropy_mean(p.row_loss, p.M, counted, (float*)loss->data, st));
+  if (!f.few && (s = hip_status(mt::cross_entropy_count(p.targets, p.M, V, (int32_t*)part, counted, stream)))) return s;
+  if ((p.M > 0 || f.few) && (s = hip_status(mt::cross_entropy_rows(p, f, zb, db, to, stream)))) return s;
+  if (f.few || !loss) return MT_OK;
+  return hip_status(mt::cross_entropy_mean(p.row_loss, p.M, (float*)part, counted, to, stream));
 }
 
 // ----------------------------------------------------------------- clipping
