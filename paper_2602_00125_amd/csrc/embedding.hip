@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(const EmbeddingParams p, int G
 
 constexpr int64_t kManyBlocks = 4096;
 constexpr int kGroupWaves = 16, kGroupThreads = 64 * kGroupWaves;
-constexpr int kAhead = 8;  // loads of ids in flight a lane
+constexpr int kAhead = 16;  // ids in flight a lane
 
 // counts: [kGroupWaves][locals], of the bucket's ids local 2^shift + bucket.
 __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGradParams p, int locals) {
@@ -71,13 +71,16 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGra
   const int64_t share = ((p.M + kGroupThreads - 1) / kGroupThreads) * 64;
   const int64_t m0 = wave * share, m1 = min(m0 + share, p.M);
   int lower = 0;  // of the wave, the same in every lane
-  for (int64_t m = m0; m < m1; m += 64 * kAhead) {
-    int32_t id[kAhead];
+  int32_t id[kAhead];
+  auto read = [&](int64_t m) {
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const int64_t i = m + 64 * j + lane;
       id[j] = i < m1 ? p.ids[i] : -1;
     }
+  };
+  for (int64_t m = m0; m < m1; m += 64 * kAhead) {
+    read(m);
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       const bool ok = (uint32_t)id[j] < (uint64_t)p.V;
@@ -92,6 +95,7 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGra
   const int per = (locals + kGroupThreads - 1) / kGroupThreads, l0 = threadIdx.x * per, l1 = min(l0 + per, locals);
   int sum = 0;
   for (int l = l0; l < l1; ++l)
+#pragma unroll
     for (int w = 0; w < kGroupWaves; ++w) sum += counts[w * locals + l];
   int scan = sum;  // inclusive over the wave
   for (int o = 1; o < 64; o <<= 1) {
@@ -105,35 +109,34 @@ __global__ __launch_bounds__(kGroupThreads) void group_kernel(const EmbeddingGra
     at += wave_lower[w] + (w < wave ? wave_sum[w] : 0);
     own += wave_lower[w] + wave_sum[w];
   }
-  if (bucket == buckets - 1 && threadIdx.x == 0) *p.total = own;  // of all buckets
+  if (bucket == buckets - 1)  // its end is that of all: no id after it
+    for (int64_t i = own + threadIdx.x; i < p.M; i += kGroupThreads) p.id[i] = -1;
   for (int l = l0; l < l1; ++l) {
     const int from = at;
+    int n[kGroupWaves];
+#pragma unroll
+    for (int w = 0; w < kGroupWaves; ++w) n[w] = counts[w * locals + l];
+#pragma unroll
     for (int w = 0; w < kGroupWaves; ++w) {
-      const int n = counts[w * locals + l];
       counts[w * locals + l] = at;
-      at += n;
+      at += n[w];
     }
     const int64_t v = ((int64_t)l << p.bucket_shift) + bucket;
     if (v < p.V) p.seen[v] = at > from;
   }
   __syncthreads();
   for (int64_t m = m0; m < m1; m += 64 * kAhead) {
-    int32_t id[kAhead];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const int64_t i = m + 64 * j + lane;
-      id[j] = i < m1 ? p.ids[i] : -1;
-    }
+    if (share > 64 * kAhead) read(m);  // else it still holds them
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
       uint64_t left = __ballot((uint32_t)id[j] < (uint64_t)p.V && (id[j] & (buckets - 1)) == bucket);
       while (left) {  // an id at a time; the same in every lane
         const int leader = __ffsll((unsigned long long)left) - 1;
-        const int32_t v = __shfl(id[j], leader, 64);
+        const int32_t v = __builtin_amdgcn_readlane(id[j], leader);
         const uint64_t same = __ballot(id[j] == v);
         int place = 0;
         if (lane == leader) place = atomicAdd(&mine[v >> p.bucket_shift], (int)__popcll(same));
-        place = __shfl(place, leader, 64);
+        place = __builtin_amdgcn_readlane(place, leader);
         if (id[j] == v) {
           const int k = place + (int)__popcll(same & ((1ull << lane) - 1));
           p.id[k] = v;
@@ -162,46 +165,47 @@ __device__ __forceinline__ void load_old(const EmbeddingGradParams& p, int32_t i
 }
 
 // Rows without a token become 0, by blocks past those of the sums.
-__device__ __forceinline__ void clear(const EmbeddingGradParams& p, int64_t block, int64_t blocks, int G_shift) {
+__device__ __forceinline__ void clear(const EmbeddingGradParams& p, int block, int blocks, int G_shift) {
   const int G = 1 << G_shift, rows = 256 >> G_shift;
   const float zero[4] = {};
-  for (int64_t v = block * rows + (threadIdx.x >> G_shift); v < p.V; v += blocks * rows) {
+  for (int64_t v = (int64_t)block * rows + (threadIdx.x >> G_shift); v < p.V; v += (int64_t)blocks * rows) {
     if (p.seen[v]) continue;
     for (int d = (threadIdx.x & (G - 1)) * 4; d < p.D; d += G * 4) store_some<false, 4>(p.dtable, v * p.ldt + d, (int)p.D - d, zero);
   }
 }
 
-template <bool BF, int VEC>
-__global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, int G_shift, int tiles, int sum_blocks, int clear_shift) {
+template <bool BF>
+__global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, int G_shift, int tiles, int sum_blocks) {
   if ((int)blockIdx.x >= sum_blocks) {
-    clear(p, blockIdx.x - sum_blocks, gridDim.x - sum_blocks, clear_shift);
+    clear(p, blockIdx.x - sum_blocks, gridDim.x - sum_blocks, G_shift);
     return;
   }
-  constexpr int U = 32 / VEC;  // rows in flight
+  constexpr int VEC = 4, U = 8;  // rows in flight
   const int G = 1 << G_shift, tile = blockIdx.x % tiles;
   const int64_t c = (int64_t)(blockIdx.x / tiles) * (256 >> G_shift) + (threadIdx.x >> G_shift);
   const int d = (tile * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
-  const int64_t total = *p.total, i0 = c * p.chunk, i1 = min(i0 + p.chunk, total);
+  const int64_t i0 = c * p.chunk, i1 = min(i0 + p.chunk, p.M);
   if (i0 >= i1 || n <= 0) return;
-  bool cut = i0 > 0 && p.id[i0 - 1] == p.id[i0];  // the run began in an earlier chunk
+  const int32_t before = i0 > 0 ? p.id[i0 - 1] : -1;
+  bool cut = before == p.id[i0];  // the run began in an earlier chunk
   float acc[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-  for (int64_t i = i0; i < i1; i += U) {
+  for (int64_t i = i0; i < i1; i += U) {  // a chunk is whole but for the last one's end, past which ids are -1
     int32_t id[U + 1], pos[U];
     float v[U][VEC], old[U][VEC];
 #pragma unroll
-    for (int u = 0; u <= U; ++u) id[u] = i + u < total ? p.id[i + u] : -1;
+    for (int u = 0; u <= U; ++u) id[u] = i + u < p.M ? p.id[i + u] : -1;
 #pragma unroll
     for (int u = 0; u < U; ++u) pos[u] = i + u < i1 ? p.pos[i + u] : 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      load_some<BF, VEC>(p.dy, pos[u] * p.ldy + d, i + u < i1 ? n : 0, 0.f, v[u]);
-      load_old(p, id[u], d, i + u < i1 && id[u] != id[u + 1] ? n : 0, old[u]);
+      load_some<BF, VEC>(p.dy, pos[u] * p.ldy + d, id[u] >= 0 ? n : 0, 0.f, v[u]);
+      load_old(p, id[u], d, id[u] >= 0 && id[u] != id[u + 1] ? n : 0, old[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i + u >= i1) break;
+      if (id[u] < 0) return;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) acc[e] += v[u][e];
       const bool ends = id[u] != id[u + 1];
@@ -218,24 +222,25 @@ __global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, i
 
 // A block for each chunk whose last run began in it and goes on. Its 256 / G
 // groups of lanes take the later pieces in turn; their sums meet in LDS.
-__global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, int G_shift) {
+__global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, int G_shift, int tiles) {
   constexpr int VEC = 4, U = 8;
   __shared__ float sums[256 * VEC];
   const int G = 1 << G_shift, groups = 256 >> G_shift, grp = threadIdx.x >> G_shift, lane = threadIdx.x & 63;
-  const int64_t c = blockIdx.x, total = *p.total, i0 = c * p.chunk, i1 = i0 + p.chunk;
-  if (i1 >= total) return;  // nothing after it
-  const int32_t id = p.id[i1];
-  if (p.id[i1 - 1] != id || (p.id[i0] == id && i0 > 0 && p.id[i0 - 1] == id)) return;
+  const int tile = blockIdx.x % tiles;
+  const int64_t c = blockIdx.x / tiles, i0 = c * p.chunk, i1 = i0 + p.chunk;
+  // together: the chunk's first id and the one before it, its last and the one after it
+  const int32_t id = i1 < p.M ? p.id[i1] : -1, last = p.id[min(i1, p.M) - 1], first = p.id[i0], before = i0 > 0 ? p.id[i0 - 1] : -1;
+  if (id < 0 || last != id || (first == id && before == id)) return;
   // how many chunks begin with the run
   int64_t pieces = 1;
   for (;;) {
     const int64_t i = (c + 1 + pieces + lane) * p.chunk;
-    const uint64_t in = __ballot(i < total && p.id[i < total ? i : 0] == id);
+    const uint64_t in = __ballot(i < p.M && p.id[i < p.M ? i : 0] == id);
     const int n = in == ~0ull ? 64 : __ffsll((unsigned long long)~in) - 1;
     pieces += n;
     if (n < 64) break;
   }
-  const int d = ((int)blockIdx.y * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
+  const int d = (tile * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
   float acc[VEC], old[VEC];
   // a group takes a share of the pieces, one after another
   const int64_t share = (pieces + groups - 1) / groups, j1 = min((grp + 1) * share, pieces);
@@ -285,13 +290,13 @@ hipError_t embedding_fwd(const EmbeddingParams& p, bool t_bf16, bool y_bf16, hip
   return y_bf16 ? lookup<false, true, 8>(p, stream) : lookup<false, false, 4>(p, stream);
 }
 
-EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D, bool bf16) {
+EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D) {
   EmbeddingGradForm f;
-  const int vec = bf16 ? 8 : 4;
-  f.shift = embedding::lanes_shift(D, vec, 6);
-  f.tiles = (int32_t)((D + ((int64_t)vec << f.shift) - 1) / ((int64_t)vec << f.shift));
-  const int64_t groups = (int64_t)4096 * (64 >> f.shift);
-  for (f.chunk = 8; f.chunk < 64 && (M + f.chunk - 1) / f.chunk * f.tiles > groups; f.chunk *= 2) {}
+  f.shift = embedding::lanes_shift(D, 4, 6);
+  f.tiles = (int32_t)((D + (4 << f.shift) - 1) >> (f.shift + 2));
+  // 4096 waves, then chunks of up to 64 tokens; longer ones for what a launch holds
+  auto items = [&] { return (M + f.chunk - 1) / f.chunk * f.tiles; };
+  for (f.chunk = 8; items() > (int64_t)4096 * (64 >> f.shift) && (f.chunk < 64 || items() > 1 << 22);) f.chunk *= 2;
   f.chunks = (int32_t)((M + f.chunk - 1) / f.chunk);
   return f;
 }
@@ -300,18 +305,17 @@ hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& 
   using namespace embedding;
   const int buckets = 1 << p.bucket_shift, locals = (int)((p.V + buckets - 1) >> p.bucket_shift);
   group_kernel<<<dim3((unsigned)buckets), kGroupThreads, 0, stream>>>(p, locals);
-  const int rows = 256 >> f.shift, clear_shift = lanes_shift(p.D, 4, 6);
-  const int64_t sums = (f.chunks + rows - 1) / rows * (int64_t)f.tiles;
+  const int rows = 256 >> f.shift;
+  const int sums = (int)((f.chunks + rows - 1) / rows) * f.tiles;
   // 16 KB each at a time, eight a CU at most
-  const int64_t clears = p.accumulate ? 0 : std::min<int64_t>((p.V * p.D + 4095) / 4096, 2048);
+  const int clears = p.accumulate ? 0 : (int)std::min<int64_t>((p.V * p.D + 4095) / 4096, 2048);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sums + clears == 0) return e;
   const dim3 grid((unsigned)(sums + clears));
-  if (bf16) sum_kernel<true, 8><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, (int)sums, clear_shift);
-  else sum_kernel<false, 4><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, (int)sums, clear_shift);
+  if (bf16) sum_kernel<true><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, sums);
+  else sum_kernel<false><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, sums);
   if ((e = hipGetLastError()) != hipSuccess || f.chunks < 2) return e;
-  const int s = lanes_shift(p.D, 4, 6);
-  join_kernel<<<dim3((unsigned)f.chunks, (unsigned)((p.D + (4 << s) - 1) / (4 << s))), 256, 0, stream>>>(p, s);
+  join_kernel<<<dim3((unsigned)(f.chunks * f.tiles)), 256, 0, stream>>>(p, f.shift, f.tiles);
   return hipGetLastError();
 }
 

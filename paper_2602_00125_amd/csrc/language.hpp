@@ -31,8 +31,7 @@ struct EmbeddingGradParams {
   int accumulate;
   int32_t chunk;               // tokens of a chunk
   int32_t bucket_shift;        // 2^bucket_shift buckets: the low bits of an id
-  int32_t* total;              // tokens with an id in range
-  int32_t *id, *pos;           // [M]: ids grouped, and the tokens they come from
+  int32_t *id, *pos;           // [M]: ids grouped (-1 after the last), and the tokens they come from
   uint8_t* seen;               // [V]: whether a row has a token
   float *head, *tail;          // [chunks][D]: a run that began before the chunk; one that ends after it
 };
@@ -41,7 +40,7 @@ constexpr int kEmbedBucketIds = 1024;  // ids of a bucket, at most
 struct EmbeddingGradForm {
   int32_t shift, tiles, chunk, chunks;
 };
-EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D, bool bf16);
+EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D);
 hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& f, bool bf16, hipStream_t stream);
 
 constexpr int kLayerNormMaxC = 16384;

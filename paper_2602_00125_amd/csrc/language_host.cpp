@@ -127,10 +127,10 @@ mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float sc
   if (p.M > (1 << 26)) return fail(MT_ERR_SHAPE, "more than 2^26 tokens");
   if (!std::isfinite(scale)) return fail(MT_ERR_INVALID, "scale must be finite");
   if ((s = check_apart({dtable}, {ids, dy}))) return s;
-  const mt::EmbeddingGradForm f = mt::embedding_grad_form(p.M, p.D, dy->dtype == MT_BF16);
+  const mt::EmbeddingGradForm f = mt::embedding_grad_form(p.M, p.D);
   p.chunk = f.chunk;
   const size_t list = round256(p.M * sizeof(int32_t)), sums = round256((size_t)f.chunks * p.D * sizeof(float));
-  const size_t need = p.V && p.D ? 256 + 2 * list + 2 * sums + round256(p.V) : 0;
+  const size_t need = p.V && p.D ? 2 * list + 2 * sums + round256(p.V) : 0;
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
@@ -138,8 +138,7 @@ mt_status embedding_bwd_impl(const mt_tensor* ids, const mt_tensor* dy, float sc
   if ((s = check_workspace(ws, ws_bytes, need, "mt_embedding_bwd"))) return s;
   if (p.V == 0 || p.D == 0) return MT_OK;
   char* at = (char*)ws;
-  p.total = (int32_t*)at;
-  p.id = (int32_t*)(at += 256);
+  p.id = (int32_t*)at;
   p.pos = (int32_t*)(at += list);
   p.head = (float*)(at += list);
   p.tail = (float*)(at += sums);

@@ -28,10 +28,17 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 
-// The VEC (4 fp32 or 8 of either) values from element i on.
+// The VEC (4 or 8) values from element i on.
 template <bool BF, int VEC>
 __device__ __forceinline__ void load(const void* p, int64_t i, float (&v)[VEC]) {
-  if constexpr (BF) {
+  if constexpr (BF && VEC == 4) {
+    const u32x2 u = *(const u32x2_any*)((const unsigned short*)p + i);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      v[2 * e] = low_bf16(u[e]);
+      v[2 * e + 1] = high_bf16(u[e]);
+    }
+  } else if constexpr (BF) {
     static_assert(VEC == 8);
     const u32x4 u = *(const u32x4_any*)((const unsigned short*)p + i);
 #pragma unroll
