@@ -8,6 +8,7 @@ native module beside it.
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import subprocess
 import sys
@@ -46,7 +47,8 @@ def _build_marshal() -> None:
     """The native half of binding.py: a CPython module, host code only."""
     out = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
     tmp = out + ".tmp"
-    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall",
+    torch_include = os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0], "include")
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-I", torch_include,
            "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "pymarshal.cpp"), "-o", tmp, "-ldl"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
