@@ -7,7 +7,7 @@
 // digits. Bound: HBM (the conversions and products of 64 bits are a tenth of the
 // time that the loads take).
 //
-// Two launches for each 120 tensors. norm_kernel: blocks take the chunks of the
+// Two launches for each 188 tensors, or 313 in place. norm_kernel: blocks take the chunks of the
 // tensors in turn and write a partial sum each. scale_kernel: every block adds
 // all partial sums in one order, so that all find the same factor, and takes the
 // chunks again, the last first: those are in the caches. In place and with
@@ -26,10 +26,25 @@ using namespace vio;
 // The tensor that chunk c belongs to; the same in every lane.
 __device__ __forceinline__ int tensor_of(const ClipBatch& b, int c) {
   const int lane = threadIdx.x & 63;
+  const uint32_t* starts = b.starts();
   int n = 0;
-#pragma unroll
-  for (int i = 0; i < kClipTensors; i += 64) n += __popcll(__ballot(i + lane < b.n && b.start[i + lane] <= c));
+  for (int i = 0; i < b.n; i += 64) n += __popcll(__ballot(i + lane < b.n && starts[min(i + lane, b.n - 1)] <= (uint32_t)c));
   return __builtin_amdgcn_readfirstlane(n - 1);
+}
+typedef __attribute__((address_space(1))) void Global;  // an address that is not of LDS
+__device__ __forceinline__ void* address(uint64_t w) { return (void*)(Global*)(w & 0xffffffffffffull); }
+// Where it is, its kind, the chunk's first value and how many it has.
+struct Chunk {
+  void* src;
+  int kind, n;
+  int64_t first;
+};
+__device__ __forceinline__ Chunk chunk_of(const ClipBatch& b, int t, int c) {
+  const uint64_t s = b.w[t];
+  const uint32_t* starts = b.starts();
+  const uint32_t next = t + 1 < b.n ? starts[t + 1] : (uint32_t)b.chunks;
+  return Chunk{address(s), (int)(s >> 48) & 15, (uint32_t)c + 1 < next ? kClipChunk : (int)(s >> 52) + 1,
+               (int64_t)((uint32_t)c - starts[t]) * kClipChunk};
 }
 
 // The 256 threads' values added by a fixed tree.
@@ -48,13 +63,13 @@ constexpr int kPer = kClipChunk / 256;  // values a thread of a chunk
 // f(i, n, values): the thread's values of a chunk by eights, the first n of which
 // exist.
 template <bool BF, typename F>
-__device__ __forceinline__ void chunk(const void* src, int64_t c0, int64_t numel, F f) {
+__device__ __forceinline__ void values(const Chunk& k, F f) {
   float v[kPer / 8][8];
-  const int n = (int)min(numel - c0, (int64_t)kClipChunk), at = (int)threadIdx.x * 8;
+  const int at = (int)threadIdx.x * 8;
 #pragma unroll
-  for (int j = 0; j < kPer / 8; ++j) load_some<BF, 8>(src, c0 + at + j * 2048, n - at - j * 2048, 0.f, v[j]);
+  for (int j = 0; j < kPer / 8; ++j) load_some<BF, 8>(k.src, k.first + at + j * 2048, k.n - at - j * 2048, 0.f, v[j]);
 #pragma unroll
-  for (int j = 0; j < kPer / 8; ++j) f(c0 + at + j * 2048, n - at - j * 2048, v[j]);
+  for (int j = 0; j < kPer / 8; ++j) f(k.first + at + j * 2048, k.n - at - j * 2048, v[j]);
 }
 
 __global__ __launch_bounds__(256) void norm_kernel(const ClipBatch b, double* part) {
@@ -63,11 +78,10 @@ __global__ __launch_bounds__(256) void norm_kernel(const ClipBatch b, double* pa
   auto add = [&](int64_t, int, const float (&v)[8]) {
     for (float x : v) sum = fma((double)x, (double)x, sum);
   };
-  for (int c = blockIdx.x; c < b.start[b.n]; c += gridDim.x) {
-    const int t = tensor_of(b, c);
-    const int64_t c0 = (int64_t)(c - b.start[t]) * kClipChunk;
-    if (b.kind[t] & 1) chunk<true>(b.src[t], c0, b.numel[t], add);
-    else chunk<false>(b.src[t], c0, b.numel[t], add);
+  for (int c = blockIdx.x; c < b.chunks; c += gridDim.x) {
+    const Chunk k = chunk_of(b, tensor_of(b, c), c);
+    if (k.kind & kClipSourceBf16) values<true>(k, add);
+    else values<false>(k, add);
   }
   sum = block_sum(sum, red);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -81,21 +95,20 @@ __global__ __launch_bounds__(256) void scale_kernel(const ClipBatch b, const dou
   if (out_norm && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = (float)norm;
   // a norm that is not finite clips nothing
   const bool clips = norm > (double)max_norm && norm < (double)INFINITY;
+  if (!clips && b.in_place) return;
   const float f = clips ? (float)((double)max_norm / norm) : 1.f;
-  for (int c = b.start[b.n] - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+  for (int c = b.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
     const int t = tensor_of(b, c);
-    if (!clips && b.src[t] == b.dst[t]) continue;
-    const int64_t c0 = (int64_t)(c - b.start[t]) * kClipChunk;
-    void* dst = b.dst[t];
-    const bool to_bf = b.kind[t] & 2;
+    const Chunk k = chunk_of(b, t, c);
+    void* dst = b.in_place ? k.src : address(b.w[b.n + t]);
     auto put = [&](int64_t i, int n, float (&v)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= f;
-      if (to_bf) store_some<true, 8>(dst, i, n, v);
+      if (k.kind & kClipDestBf16) store_some<true, 8>(dst, i, n, v);
       else store_some<false, 8>(dst, i, n, v);
     };
-    if (b.kind[t] & 1) chunk<true>(b.src[t], c0, b.numel[t], put);
-    else chunk<false>(b.src[t], c0, b.numel[t], put);
+    if (k.kind & kClipSourceBf16) values<true>(k, put);
+    else values<false>(k, put);
   }
 }
 

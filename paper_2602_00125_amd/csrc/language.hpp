@@ -89,16 +89,25 @@ hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyFor
 hipError_t cross_entropy_mean(const float* row_loss, int64_t M, float* part, const int32_t* counted, float* loss,
                               hipStream_t stream);
 
-// Up to kClipTensors tensors of a launch, cut into chunks of kClipChunk values.
-constexpr int kClipTensors = 120;
+// The tensors of a launch, cut into chunks of kClipChunk values, 20 bytes a tensor
+// in a launch's arguments (12 where they are scaled in place):
+//   w[0 .. n)       sources: 48 bits of address, kind, values of the last chunk - 1
+//   w[n .. 2 n)     destinations (not in place)
+//   then n 32-bit   chunks before each tensor
 constexpr int kClipChunk = 4096;
+constexpr int kClipWords = 470;
+constexpr int kClipSourceBf16 = 1, kClipDestBf16 = 2;  // kinds
 struct ClipBatch {
-  const void* src[kClipTensors];
-  void* dst[kClipTensors];
-  int64_t numel[kClipTensors];
-  int32_t start[kClipTensors + 1];  // chunks before tensor i
-  int8_t kind[kClipTensors];        // 1: src is bf16, 2: dst is bf16
-  int32_t n;
+  uint64_t w[kClipWords];
+  int32_t n, in_place, chunks;
+  static int most(bool in_place) { return kClipWords * 8 / (in_place ? 12 : 20); }
+  static uint64_t source(const void* p, int kind, int64_t numel) {
+    return ((uint64_t)(uintptr_t)p & 0xffffffffffffull) | (uint64_t)kind << 48 | (uint64_t)((numel - 1) % kClipChunk) << 52;
+  }
+#if defined(__HIPCC__)
+  __host__ __device__
+#endif
+  const uint32_t* starts() const { return (const uint32_t*)(w + (in_place ? n : 2 * n)); }
 };
 // part[block] = the block's sum of squares; blocks <= clip_blocks(chunks).
 int clip_blocks(int64_t chunks);

@@ -321,91 +321,125 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
 // ----------------------------------------------------------------- clipping
 mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
                               const mt_tensor* norm, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
-  const std::string who = "mt_clip_grad_norm: ";
-  if (n < 0) return fail(MT_ERR_INVALID, who + "negative tensor count");
-  if (n > 0 && !grads) return fail(MT_ERR_NULL, who + "null array");
+  if (n < 0) return fail(MT_ERR_INVALID, "mt_clip_grad_norm: negative tensor count");
+  if (n > 0 && !grads) return fail(MT_ERR_NULL, "mt_clip_grad_norm: null array");
   mt_status s;
-  struct Range {
-    uintptr_t lo, hi;
-    bool out;
+  // Every launch's tensors: f(first, end, how many are not empty, chunks).
+  auto each_batch = [&](bool in_place, auto f) -> mt_status {
+    const int most = mt::ClipBatch::most(in_place);
+    for (int32_t i = 0; i < n;) {
+      int32_t first = i, held = 0;
+      int64_t chunks = 0;
+      for (; i < n && held < most; ++i) {
+        const int64_t pieces = cdiv(numel(&grads[i]), mt::kClipChunk);
+        if (chunks + pieces > (1 << 30)) break;
+        chunks += pieces;
+        held += pieces > 0;
+      }
+      if (held == 0) continue;
+      if (mt_status e = f(first, i, held, chunks)) return e;
+    }
+    return MT_OK;
   };
-  std::vector<Range> ranges;
-  std::vector<mt::ClipBatch> batches;
-  size_t parts = 0;
-  int64_t chunks = 0;
-  auto close = [&] {
-    batches.back().start[batches.back().n] = (int32_t)chunks;
-    parts += mt::clip_blocks(chunks);
-  };
+  auto name = [&](bool o, int32_t i) { return (o ? "out " : "grad ") + std::to_string(i); };
   for (int32_t i = 0; i < n; ++i) {
-    const mt_tensor* ts[2] = {&grads[i], out ? &out[i] : &grads[i]};
     for (int j = 0; j < (out ? 2 : 1); ++j) {
-      const std::string name = who + (j ? "out " : "grad ") + std::to_string(i);
-      if ((s = check_tensor(ts[j], name.c_str(), 0, MT_MAX_DIMS))) return s;
-      if (!is_row_major(ts[j])) return fail(MT_ERR_LAYOUT, name + ": must be contiguous");
-      if (ts[j]->ndim != ts[0]->ndim || !std::equal(ts[j]->shape, ts[j]->shape + ts[j]->ndim, ts[0]->shape))
-        return fail(MT_ERR_SHAPE, name + " must have the shape of its gradient");
-      const uintptr_t lo = (uintptr_t)ts[j]->data;
-      if (numel(ts[j]) > 0) ranges.push_back({lo, lo + numel(ts[j]) * elem_size(ts[j]->dtype), j > 0});
+      const mt_tensor* t = j ? &out[i] : &grads[i];
+      if (check_tensor(t, "", 0, MT_MAX_DIMS)) return check_tensor(t, name(j, i).c_str(), 0, MT_MAX_DIMS);
+      if (!is_row_major(t)) return fail(MT_ERR_LAYOUT, name(j, i) + ": must be contiguous");
+      if (j && (t->ndim != grads[i].ndim || !std::equal(t->shape, t->shape + t->ndim, grads[i].shape)))
+        return fail(MT_ERR_SHAPE, name(j, i) + " must have the shape of its gradient");
+      if (numel(t) > (int64_t)1 << 40) return fail(MT_ERR_SHAPE, name(j, i) + ": more than 2^40 values");
     }
-    const int64_t count = numel(ts[0]), pieces = cdiv(count, mt::kClipChunk);
-    if (count == 0) continue;
-    if (pieces > (1 << 28)) return fail(MT_ERR_SHAPE, who + "tensor " + std::to_string(i) + " is too large");
-    if (batches.empty() || batches.back().n == mt::kClipTensors || chunks + pieces > (1 << 29)) {
-      if (!batches.empty()) close();
-      batches.emplace_back();
-      chunks = 0;
-    }
-    mt::ClipBatch& b = batches.back();
-    const int k = b.n++;
-    b.src[k] = ts[0]->data;
-    b.dst[k] = ts[1]->data;
-    b.numel[k] = count;
-    b.start[k] = (int32_t)chunks;
-    b.kind[k] = (int8_t)((ts[0]->dtype == MT_BF16 ? 1 : 0) | (ts[1]->dtype == MT_BF16 ? 2 : 0));
-    chunks += pieces;
   }
-  if (!batches.empty()) close();
-  const size_t need = round256(std::max<size_t>(1, parts) * sizeof(double));
+  auto parts_of = [&](bool in_place) {
+    size_t parts = 0;
+    each_batch(in_place, [&](int32_t, int32_t, int32_t, int64_t chunks) {
+      parts += mt::clip_blocks(chunks);
+      return MT_OK;
+    });
+    return parts;
+  };
+  // a workspace serves both forms: the query does not know of out
+  const size_t parts = parts_of(!out);
+  const size_t need = round256(std::max({(size_t)1, parts, parts_of(out != nullptr)}) * sizeof(double));
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
   }
-  if (!(max_norm >= 0.f)) return fail(MT_ERR_INVALID, who + "max_norm must not be negative");
+  if (!(max_norm >= 0.f)) return fail(MT_ERR_INVALID, "mt_clip_grad_norm: max_norm must not be negative");
   if (norm) {
     if ((s = check_tensor(norm, "norm", 0, MT_MAX_DIMS))) return s;
     if (norm->dtype != MT_F32) return fail(MT_ERR_DTYPE, "norm must be f32");
     if (numel(norm) != 1) return fail(MT_ERR_SHAPE, "norm must hold exactly one element");
-    ranges.push_back({(uintptr_t)norm->data, (uintptr_t)norm->data + 4, true});
   }
-  // what is written overlaps nothing else
-  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
-  uintptr_t far = 0, far_out = 0;  // ends of what came before: of all, of what is written
+  // What is written overlaps nothing else: by ascending address, which tensors
+  // cut from one buffer mostly are in already.
+  struct Range {
+    uintptr_t lo, hi;
+    bool written;
+  };
+  std::vector<Range> ranges;
+  ranges.reserve((size_t)n * (out ? 2 : 1) + 1);
+  auto take = [&](const mt_tensor* t, bool written) {
+    const uintptr_t lo = (uintptr_t)t->data;
+    if (const int64_t count = numel(t)) ranges.push_back({lo, lo + (uintptr_t)count * elem_size(t->dtype), written});
+  };
+  for (int32_t i = 0; i < n; ++i) take(&grads[i], !out);
+  for (int32_t i = 0; out && i < n; ++i) take(&out[i], true);
+  if (norm) take(norm, true);
+  auto before = [](const Range& a, const Range& b) { return a.lo < b.lo; };
+  if (!std::is_sorted(ranges.begin(), ranges.end(), before)) std::sort(ranges.begin(), ranges.end(), before);
+  uintptr_t far = 0, far_written = 0;  // ends of what came before: of all, of what is written
   for (const Range& r : ranges) {
-    const bool written = !out || r.out;
-    if (r.lo < far_out || (written && r.lo < far)) return fail(MT_ERR_ALIAS, who + "a tensor that is written overlaps another");
+    if (r.lo < far_written || (r.written && r.lo < far))
+      return fail(MT_ERR_ALIAS, "mt_clip_grad_norm: a tensor that is written overlaps another");
     far = std::max(far, r.hi);
-    if (written) far_out = std::max(far_out, r.hi);
+    if (r.written) far_written = std::max(far_written, r.hi);
   }
   if ((s = check_workspace(ws, ws_bytes, need, "mt_clip_grad_norm"))) return s;
+  mt::ClipBatch b;
+  auto pack = [&](int32_t first, int32_t end, int32_t held, int64_t chunks) {
+    b.n = held;
+    b.in_place = !out;
+    b.chunks = (int32_t)chunks;
+    uint32_t* starts = (uint32_t*)b.starts();
+    uint32_t at = 0;
+    int k = 0;
+    for (int32_t i = first; i < end; ++i) {
+      const int64_t count = numel(&grads[i]);
+      if (count == 0) continue;
+      const int kind = (grads[i].dtype == MT_BF16 ? mt::kClipSourceBf16 : 0) |
+                       ((out ? out[i] : grads[i]).dtype == MT_BF16 ? mt::kClipDestBf16 : 0);
+      b.w[k] = mt::ClipBatch::source(grads[i].data, kind, count);
+      if (out) b.w[held + k] = (uint64_t)(uintptr_t)out[i].data;
+      starts[k++] = at;
+      at += (uint32_t)cdiv(count, mt::kClipChunk);
+    }
+  };
   double* part = (double*)ws;
   float* to = norm ? (float*)norm->data : nullptr;
   (void)hipGetLastError();
-  size_t at = 0;
-  for (const mt::ClipBatch& b : batches) {
-    const int blocks = mt::clip_blocks(b.start[b.n]);
-    if ((s = hip_status(mt::clip_norm(b, part + at, blocks, stream)))) return s;
-    at += blocks;
-  }
-  if (batches.empty()) {
+  if (parts == 0) {
     if (!to) return MT_OK;
-    return hip_status(mt::clip_scale(mt::ClipBatch{}, part, 0, max_norm, to, 1, stream));
+    b.n = b.chunks = 0;
+    b.in_place = 1;
+    return hip_status(mt::clip_scale(b, part, 0, max_norm, to, 1, stream));
   }
-  for (const mt::ClipBatch& b : batches) {
-    if ((s = hip_status(mt::clip_scale(b, part, (int)parts, max_norm, to, mt::clip_blocks(b.start[b.n]), stream)))) return s;
-    to = nullptr;  // written once
-  }
-  return MT_OK;
+  size_t at = 0;
+  s = each_batch(!out, [&](int32_t first, int32_t end, int32_t held, int64_t chunks) {
+    pack(first, end, held, chunks);
+    const int blocks = mt::clip_blocks(chunks);
+    at += blocks;
+    return hip_status(mt::clip_norm(b, part + at - blocks, blocks, stream));
+  });
+  if (s) return s;
+  return each_batch(!out, [&](int32_t first, int32_t end, int32_t held, int64_t chunks) {
+    if (held < n) pack(first, end, held, chunks);  // else it still holds them
+    float* once = to;
+    to = nullptr;
+    return hip_status(mt::clip_scale(b, part, (int)parts, max_norm, once, mt::clip_blocks(chunks), stream));
+  });
 }
 
 }  // namespace mt::host

@@ -107,6 +107,20 @@ def test_large_tensors_and_reruns():
         close("out", got, *o)
 
 
+@pytest.mark.parametrize("large", [(200, 350), (100, 200), (0, 399), (312, 313), (187, 188)])
+def test_launches_of_many_tensors(large):
+    """Large tensors wherever the tensors are cut into launches; the workspace serves both forms."""
+    sizes = [(1 << 20) * 9 + 7 if i in large else i % 3 for i in range(400)]
+    grads = [torch.full((n,), 2.0 ** -10, dtype=torch.bfloat16, device=DEV) for n in sizes]
+    want = (sum(sizes) * 2.0 ** -20) ** 0.5
+    out = [torch.empty_like(g) for g in grads]
+    assert abs(float(run(grads, want / 4, out)) / want - 1) < 2.0 ** -23
+    assert abs(float(run(grads, want / 4)) / want - 1) < 2.0 ** -23
+    for g, o in zip(grads, out):  # a quarter, but for the factor's and the result's rounding
+        assert ((g.float() * 2 ** 12 - 1).abs() <= 2.0 ** -7).all()
+        assert torch.equal(g, o)
+
+
 def test_past_2_31_values():
     g = torch.zeros((1 << 31) + 5000, dtype=torch.bfloat16, device=DEV)
     g[-1], g[0] = 3.0, 4.0
