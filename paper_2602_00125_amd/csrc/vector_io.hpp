@@ -102,14 +102,35 @@ __device__ __forceinline__ void store_some(void* p, int64_t i, int n, const floa
   }
 }
 
-// Every lane of L (a power of two up to 64) consecutive ones gets their sum.
-__device__ __forceinline__ float lanes_sum(float v, int L) {
-  for (int o = L >> 1; o; o >>= 1) v += __shfl_xor(v, o, 64);
+// The value of a lane's partner, by the vector instructions' own lane paths
+// (__shfl goes through LDS): lanes 1 and 2 apart, then the mirrored one of 8 and of
+// 16, which holds the same as the one 4 and 8 apart once the smaller groups agree.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// Every lane of L (a power of two up to 64) consecutive ones gets their reduction.
+template <typename Op>
+__device__ __forceinline__ float lanes_reduce(float v, int L, Op op) {
+  if (L > 1) v = op(v, dpp<0xb1>(v));   // quad_perm 1 0 3 2
+  if (L > 2) v = op(v, dpp<0x4e>(v));   // quad_perm 2 3 0 1
+  if (L > 4) v = op(v, dpp<0x141>(v));  // row_half_mirror
+  if (L > 8) v = op(v, dpp<0x140>(v));  // row_mirror
+  if (L > 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  }
+  if (L > 32) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = op(__uint_as_float(s[0]), __uint_as_float(s[1]));
+  }
   return v;
 }
+__device__ __forceinline__ float lanes_sum(float v, int L) {
+  return lanes_reduce(v, L, [](float a, float b) { return a + b; });
+}
 __device__ __forceinline__ float lanes_max(float v, int L) {
-  for (int o = L >> 1; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+  return lanes_reduce(v, L, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // A view of int32 values (tokens, classes), row-major index m of [m / inner, m % inner].
