@@ -42,22 +42,44 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int L, float (*red)[16])
   }
 }
 
-// Column of value e of group k of a lane's: (l + k L) VEC + e.
-template <bool XB, bool YB, int VEC, int NV, bool WIDE>
+// Group k of lane l: columns (l + k L) VEC and on. A row's last group, where it is
+// not whole, is the row's last VEC values: those before `lo` belong to the group
+// before it, take no part in sums and are written twice alike. (By element a
+// wave would go through up to seven loads and stores for it: 32768 x 1023 bf16
+// 54 us, this way 31.) hi: VEC, or C where a row has less. WHOLE: C is a multiple
+// of VEC, and a group has all its columns or none (1024: 29.5 us as any, 28 whole).
+template <int VEC, bool WHOLE>
+struct Columns {
+  int c, lo, hi;
+  __device__ __forceinline__ Columns(int l, int k, const LayerNormParams& p) {
+    const int first = (l + (k << p.L_shift)) * VEC;
+    c = WHOLE ? first : max(min(first, p.C - VEC), 0);
+    lo = WHOLE ? (first < p.C ? 0 : VEC) : first - c;
+    hi = WHOLE ? VEC : min(p.C, VEC);
+  }
+  __device__ __forceinline__ bool any() const { return lo < hi; }
+  __device__ __forceinline__ bool has(int e) const { return WHOLE ? lo == 0 : e >= lo && e < hi; }
+  template <bool BF>
+  __device__ __forceinline__ void load(const void* p, int64_t row, bool on, float (&v)[VEC]) const {
+    load_some<BF, VEC>(p, row + c, on && any() ? (WHOLE ? VEC : hi) : 0, 0.f, v);
+  }
+};
+
+template <bool XB, bool YB, int VEC, int NV, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
   __shared__ float red[2][16];
   const int l = threadIdx.x & (p.L - 1), rows = blockDim.x >> p.L_shift;
   float w[NV][VEC], b[NV][VEC];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = (l + (k << p.L_shift)) * VEC;
+    const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       w[k][e] = 1.f;
       b[k][e] = 0.f;
     }
-    if (p.w) load_some<false, VEC>(p.w, c, p.C - c, 0.f, w[k]);
-    if (p.b) load_some<false, VEC>(p.b, c, p.C - c, 0.f, b[k]);
+    if (p.w) c.template load<false>(p.w, 0, true, w[k]);
+    if (p.b) c.template load<false>(p.b, 0, true, b[k]);
   }
   // all rows of a block go through the loop the same number of times
   for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
@@ -65,38 +87,37 @@ __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
     const bool on = m < p.M;
     float x[NV][VEC], s[1] = {0.f}, q[1] = {0.f};
 #pragma unroll
+    for (int k = 0; k < NV; ++k) Columns<VEC, WHOLE>(l, k, p).template load<XB>(p.x, m * p.ldx, on, x[k]);
+#pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
-      load_some<XB, VEC>(p.x, m * p.ldx + c, on ? p.C - c : 0, 0.f, x[k]);
+      const Columns<VEC, WHOLE> c(l, k, p);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
     }
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] += x[k][e];
     row_sums<WIDE, 1>(s, p.L, red);
     const float mu = s[0] / p.C_f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
+      const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        x[k][e] = c + e < p.C ? x[k][e] - mu : 0.f;
-        q[0] = fmaf(x[k][e], x[k][e], q[0]);
+        x[k][e] -= mu;
+        q[0] = fmaf(c.has(e) ? x[k][e] : 0.f, x[k][e], q[0]);
       }
     }
     row_sums<WIDE, 1>(q, p.L, red + 1);
     const float r = 1.f / sqrtf(q[0] / p.C_f + p.eps);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
+      const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[k][e] = fmaf(x[k][e] * r, w[k][e], b[k][e]);
-      store_some<YB, VEC>(p.out, m * p.ldo + c, on ? p.C - c : 0, x[k]);
+      store_some<YB, VEC>(p.out, m * p.ldo + c.c, on && c.any() ? c.hi : 0, x[k]);
     }
   }
 }
 
-template <bool XB, bool YB, int VEC, int NV, bool WIDE>
+template <bool XB, bool YB, int VEC, int NV, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
   __shared__ float red[4][16];
   __shared__ float cols[1024 * 16];  // [group][C], where a block has several groups
@@ -104,13 +125,12 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
   float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = (l + (k << p.L_shift)) * VEC;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       w[k][e] = 1.f;
       dw[k][e] = db[k][e] = 0.f;
     }
-    if (p.w) load_some<false, VEC>(p.w, c, p.C - c, 0.f, w[k]);
+    if (p.w) Columns<VEC, WHOLE>(l, k, p).template load<false>(p.w, 0, true, w[k]);
   }
   for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
     const int64_t m = m0 + grp;
@@ -118,27 +138,30 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
     float x[NV][VEC], g[NV][VEC], s[1] = {0.f}, t[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
-      load_some<XB, VEC>(p.x, m * p.ldx + c, on ? p.C - c : 0, 0.f, x[k]);
-      load_some<YB, VEC>(p.dy, m * p.ldd + c, on ? p.C - c : 0, 0.f, g[k]);
+      const Columns<VEC, WHOLE> c(l, k, p);
+      c.template load<XB>(p.x, m * p.ldx, on, x[k]);
+      c.template load<YB>(p.dy, m * p.ldd, on, g[k]);
     }
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k) {
+      const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] += x[k][e];
+      for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
+    }
     row_sums<WIDE, 1>(s, p.L, red);
     const float mu = s[0] / p.C_f;
     // squares of the deviations, sums of g and of g times the deviations
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
+      const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        x[k][e] = c + e < p.C ? x[k][e] - mu : 0.f;
+        x[k][e] -= mu;
+        const float d = c.has(e) ? x[k][e] : 0.f;
         const float gw = g[k][e] * w[k][e];
-        t[0] = fmaf(x[k][e], x[k][e], t[0]);
-        t[1] += gw;
-        t[2] = fmaf(x[k][e], gw, t[2]);
+        t[0] = fmaf(d, d, t[0]);
+        t[1] += c.has(e) ? gw : 0.f;
+        t[2] = fmaf(d, gw, t[2]);
       }
     }
     row_sums<WIDE, 3>(t, p.L, red + 1);
@@ -147,7 +170,7 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
     if (!on) continue;  // no barrier below
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
+      const Columns<VEC, WHOLE> c(l, k, p);
       float o[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -156,14 +179,22 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
         db[k][e] += g[k][e];
         o[e] = r * (fmaf(g[k][e], w[k][e], -mg) - n * mgn);
       }
-      if (!p.out) continue;
-      if (p.accumulate) {
-        float old[VEC];
-        load_some<YB, VEC>(p.out, m * p.ldo + c, p.C - c, 0.f, old);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] += old[e];
+      if (!p.out || !c.any()) continue;
+      if (!p.accumulate) {
+        store_some<YB, VEC>(p.out, m * p.ldo + c.c, c.hi, o);
+        continue;
       }
-      store_some<YB, VEC>(p.out, m * p.ldo + c, p.C - c, o);
+      float old[VEC];
+      load_some<YB, VEC>(p.out, m * p.ldo + c.c, c.hi, 0.f, old);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) o[e] += old[e];
+      if (c.lo == 0) {
+        store_some<YB, VEC>(p.out, m * p.ldo + c.c, c.hi, o);
+      } else {  // once only: another lane adds to the others
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (c.has(e)) store_one<YB>(p.out, m * p.ldo + c.c + e, o[e]);
+      }
     }
   }
   if (!p.part) return;
@@ -173,20 +204,20 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
     if (rows == 1) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        const int c = (l + (k << p.L_shift)) * VEC;
+        const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
-          if (c + e < p.C) part[c + e] = which ? db[k][e] : dw[k][e];
+          if (c.has(e)) part[c.c + e] = which ? db[k][e] : dw[k][e];
       }
       continue;
     }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      const int c = (l + (k << p.L_shift)) * VEC;
+      const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (c + e < p.C) cols[grp * p.C + c + e] = which ? db[k][e] : dw[k][e];
+        if (c.has(e)) cols[grp * p.C + c.c + e] = which ? db[k][e] : dw[k][e];
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
@@ -244,8 +275,12 @@ hipError_t layer_norm_fwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, in
     constexpr bool XB = decltype(xb)::value, YB = decltype(yb)::value;
     constexpr int VEC = XB || YB ? 8 : 4;
     return layernorm::by_form<VEC>(nv, p.L > 64, [&](auto n, auto wide) {
-      layernorm::fwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value>
-          <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
+      if (p.C % VEC == 0)
+        layernorm::fwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value, true>
+            <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
+      else
+        layernorm::fwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value, false>
+            <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
       return hipGetLastError();
     });
   });
@@ -257,8 +292,12 @@ hipError_t layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, in
     constexpr bool XB = decltype(xb)::value, YB = decltype(yb)::value;
     constexpr int VEC = XB || YB ? 8 : 4;
     return layernorm::by_form<VEC>(nv, p.L > 64, [&](auto n, auto wide) {
-      layernorm::bwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value>
-          <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
+      if (p.C % VEC == 0)
+        layernorm::bwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value, true>
+            <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
+      else
+        layernorm::bwd_kernel<XB, YB, VEC, decltype(n)::value, decltype(wide)::value, false>
+            <<<dim3((unsigned)blocks), threads, 0, stream>>>(p);
       return hipGetLastError();
     });
   });
