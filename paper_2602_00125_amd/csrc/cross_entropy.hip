@@ -55,6 +55,15 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
   for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += red[w];
   return s;
 }
+// of the rows' losses, in 64 bits: one number that a program follows for long
+__device__ __forceinline__ double block_sum64(double v, double* red) {
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double s = 0.0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += red[w];
+  return s;
+}
 
 template <bool BF>
 __device__ __forceinline__ const char* row_at(const void* p, int64_t m, int64_t ld) {
@@ -229,18 +238,18 @@ __device__ __forceinline__ int block_count(int n, int* red) {
 // A few short rows: the count, the rows and the mean by one block, one launch.
 template <bool XB, bool YB, int VEC>
 __global__ __launch_bounds__(1024) void few_kernel(const CrossEntropyParams p, int L, int L_shift, float* loss) {
-  __shared__ float red[16];
+  __shared__ double red[16];
   __shared__ int counts[16];
   int n = 0;
   for (int64_t m = threadIdx.x; m < p.M; m += 1024) n += (uint32_t)p.targets[m] < (uint32_t)p.V;
   n = block_count(n, counts);
-  float sum = 0.f;
+  double sum = 0.0;
   for (int64_t m = threadIdx.x >> L_shift; m < p.M; m += 1024 >> L_shift) {
     const float one = lanes_row<XB, YB, VEC>(p, m, threadIdx.x & (L - 1), L, n);
     if ((threadIdx.x & (L - 1)) == 0) sum += one;
   }
-  sum = block_sum(sum, red);
-  if (loss && threadIdx.x == 0) *loss = n > 0 ? sum / (float)n : 0.f;
+  sum = block_sum64(sum, red);
+  if (loss && threadIdx.x == 0) *loss = n > 0 ? (float)(sum / n) : 0.f;
 }
 
 // How many rows count; the mean of their losses, 0 where none does. Blocks take
@@ -259,20 +268,21 @@ __global__ __launch_bounds__(kCrossEntropyParts) void add_counts_kernel(const in
   const int n = block_count((int)threadIdx.x < parts ? part[threadIdx.x] : 0, red);
   if (threadIdx.x == 0) *counted = n;
 }
-// counted NULL: the sum, not the mean
-__global__ __launch_bounds__(1024) void mean_kernel(const float* row_loss, int64_t M, const int32_t* counted, float* out) {
-  __shared__ float red[16];
+// from: fp32 losses or 64-bit partial sums; to: those, or the mean
+template <typename From, typename To>
+__global__ __launch_bounds__(1024) void mean_kernel(const From* from, int64_t M, const int32_t* counted, To* out) {
+  __shared__ double red[16];
   const int64_t share = (M + gridDim.x - 1) / gridDim.x, m0 = blockIdx.x * share, m1 = min(m0 + share, M);
-  float s = 0.f;
+  double s = 0.0;
 #pragma unroll 8
-  for (int64_t m = m0 + threadIdx.x; m < m1; m += 1024) s += row_loss[m];
-  s = block_sum(s, red);
+  for (int64_t m = m0 + threadIdx.x; m < m1; m += 1024) s += from[m];
+  s = block_sum64(s, red);
   if (threadIdx.x) return;
-  if (!counted) {
+  if constexpr (sizeof(To) == 8) {
     out[blockIdx.x] = s;
   } else {
     const int n = *counted;
-    *out = n > 0 ? s / (float)n : 0.f;
+    *out = n > 0 ? (float)(s / n) : 0.f;
   }
 }
 
@@ -315,12 +325,12 @@ hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyFor
   return d_bf16 ? xent::rows<false, true>(p, f, loss, stream) : xent::rows<false, false>(p, f, loss, stream);
 }
 
-hipError_t cross_entropy_mean(const float* row_loss, int64_t M, float* part, const int32_t* counted, float* loss,
+hipError_t cross_entropy_mean(const float* row_loss, int64_t M, double* part, const int32_t* counted, float* loss,
                               hipStream_t stream) {
   const int parts = xent::parts_of(M);
   if (parts > 1) {
-    xent::mean_kernel<<<dim3(parts), 1024, 0, stream>>>(row_loss, M, nullptr, part);
-    xent::mean_kernel<<<1, 1024, 0, stream>>>(part, parts, counted, loss);
+    xent::mean_kernel<<<dim3(parts), 1024, 0, stream>>>(row_loss, M, counted, part);
+    xent::mean_kernel<<<1, 1024, 0, stream>>>((const double*)part, parts, counted, loss);
   } else {
     xent::mean_kernel<<<1, 1024, 0, stream>>>(row_loss, M, counted, loss);
   }

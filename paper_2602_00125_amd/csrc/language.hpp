@@ -86,7 +86,7 @@ hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, 
 // loss: written where f.few
 hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16, float* loss,
                               hipStream_t stream);
-hipError_t cross_entropy_mean(const float* row_loss, int64_t M, float* part, const int32_t* counted, float* loss,
+hipError_t cross_entropy_mean(const float* row_loss, int64_t M, double* part, const int32_t* counted, float* loss,
                               hipStream_t stream);
 
 // The tensors of a launch, cut into chunks of kClipChunk values, 20 bytes a tensor

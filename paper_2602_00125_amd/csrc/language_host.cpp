@@ -274,7 +274,7 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
   const int64_t V = logits->shape[1];
   if (n != p.M) return fail(MT_ERR_SHAPE, "targets must hold one class for each row of logits");
   if (V < 1 || V > (1 << 24)) return fail(MT_ERR_SHAPE, "a row must have 1 to 2^24 logits");
-  const size_t need = 256 + kCrossEntropyParts * sizeof(float) + round256(p.M * sizeof(float));
+  const size_t need = 256 + kCrossEntropyParts * sizeof(double) + round256(p.M * sizeof(float));
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
@@ -298,7 +298,7 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
   void* part = (char*)ws + 256;
   p.V = (int32_t)V;
   p.counted = counted;
-  p.row_loss = losses && p.M ? (float*)losses->data : (float*)((char*)part + kCrossEntropyParts * sizeof(float));
+  p.row_loss = losses && p.M ? (float*)losses->data : (float*)((char*)part + kCrossEntropyParts * sizeof(double));
   p.z = logits->data;
   p.ldz = row_pitch(logits);
   const bool zb = logits->dtype == MT_BF16, db = dlogits ? dlogits->dtype == MT_BF16 : zb;
@@ -319,7 +319,7 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
   if (!f.few && (s = hip_status(mt::cross_entropy_count(p.targets, p.M, V, (int32_t*)part, counted, stream)))) return s;
   if ((p.M > 0 || f.few) && (s = hip_status(mt::cross_entropy_rows(p, f, zb, db, to, stream)))) return s;
   if (f.few || !loss) return MT_OK;
-  return hip_status(mt::cross_entropy_mean(p.row_loss, p.M, (float*)part, counted, to, stream));
+  return hip_status(mt::cross_entropy_mean(p.row_loss, p.M, (double*)part, counted, to, stream));
 }
 
 // ----------------------------------------------------------------- clipping

@@ -9,7 +9,8 @@
 // takes them again from the row that it reads anyway. Bound: HBM.
 //
 // dw, db: a lane keeps the sums of its columns over the rows that it meets, a
-// block adds its groups' in order, a second launch the blocks' in order.
+// block adds its groups' in order, a second launch the blocks' in order, both in
+// 64 bits (with 32 the sums of 3506 x 64 were off by 2.2e-7 of their norm).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -221,9 +222,9 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.C; c += blockDim.x) {
-      float s = 0.f;
+      double s = 0.0;
       for (int i = 0; i < rows; ++i) s += cols[i * p.C + c];
-      part[c] = s;
+      part[c] = (float)s;
     }
   }
 }
@@ -231,9 +232,9 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
 // dw, db (+)= the blocks' parts, in order within each of 64 interleaved shares,
 // then over the shares; a block covers 16 of the 2 C columns.
 __global__ __launch_bounds__(1024) void finish_kernel(const float* part, int parts, int C, float* dw, float* db, int add) {
-  __shared__ float sums[64][17];
+  __shared__ double sums[64][17];
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
-  float s = 0.f;
+  double s = 0.0;
   if (c < 2 * C) {
 #pragma unroll 8
     for (int i = share; i < parts; i += 64) s += part[(int64_t)i * 2 * C + c];
@@ -241,13 +242,13 @@ __global__ __launch_bounds__(1024) void finish_kernel(const float* part, int par
   sums[share][threadIdx.x & 15] = s;
   __syncthreads();
   if (share || c >= 2 * C) return;
-  s = 0.f;
+  s = 0.0;
 #pragma unroll 16
   for (int i = 0; i < 64; ++i) s += sums[i][threadIdx.x];
   float* out = c < C ? dw : db;
   if (!out) return;
   out += c < C ? c : c - C;
-  *out = add ? *out + s : s;
+  *out = (float)(add ? *out + s : s);
 }
 
 template <typename F>
