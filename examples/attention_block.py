@@ -101,7 +101,7 @@ class AttentionBlock:
         return self._heads(self.qkv)[2] if self.dtype == torch.float32 else self.vv
 
     def _operand(self, name, t):
-        return t if self.dtype == torch.float32 else self.x16
+        return t if t.dtype == self.dtype else self.x16
 
     def _weight(self, name):
         return self.params[name] if self.dtype == torch.float32 else self.w16[name]
@@ -116,10 +116,11 @@ class AttentionBlock:
             self._cast(self.params[n], w)
 
     # ---------------------------------------------------------------------- training
-    def forward(self, x, kv_len):
-        """x [B T, C] fp32 -> h [B T, C]; tokens from kv_len on are padding."""
+    def forward(self, x, kv_len, residual=None):
+        """x [B T, C] (fp32 or the products' type) -> h [B T, C]; tokens from kv_len on are padding. residual: what the
+        attention is added to, by default x (then fp32)."""
         P, M = self.params, self.B * self.T
-        if self.dtype != torch.float32:
+        if x.dtype != self.dtype:
             self._cast(x, self.x16)
         self.refresh()
         mt.linear_fwd(self._operand("x", x), self._weight("wqkv"), P["bqkv"], self.qkv)
@@ -129,13 +130,13 @@ class AttentionBlock:
             self._cast(self.qkv[:, (self.HQ + self.HK) * self.D:], self.vv.view(M, -1))
         mt.attention_fwd(self.q, self.k, self._values(), self.o, self.lse, kv_len=kv_len, causal=True, workspace=self.ws)
         mt.linear_fwd(self.o.view(M, -1), self._weight("wo"), P["bo"], self.y)
-        mt.dropout_fwd(self.y, x, self.p, self.seed, self._offset(), self.h)
+        mt.dropout_fwd(self.y, x if residual is None else residual, self.p, self.seed, self._offset(), self.h)
 
     def _offset(self):
         return self.t * ((self.B * self.T * self.C + 7) // 8)  # a step's share of the generator's counters
 
-    def backward(self, x, kv_len):
-        """From dh: the gradients of the parameters and, in dx, of x."""
+    def backward(self, x, kv_len, through=True):
+        """From dh: the gradients of the parameters and, in dx, of x (through: which is the residual too)."""
         P, G, M = self.params, self.grads, self.B * self.T
         mt.dropout_bwd(self.dh, self.p, self.seed, self._offset(), self.dy)
         o = self.o.view(M, -1)
@@ -149,9 +150,10 @@ class AttentionBlock:
         q, k, _ = self._heads(self.qkv)
         mt.qk_norm_rope_bwd(q, k, P["gq"], P["gk"], self.cos, self.sin, self.dq, self.dk, dq, dk, G["gq"], G["gk"], eps=EPS,
                             workspace=self.ws)
-        self.dx.copy_(self.dh)  # through the residual
+        if through:
+            self.dx.copy_(self.dh)
         mt.linear_bwd(self._operand("x", x), self._weight("wqkv"), self.dqkv, None, G["wqkv"], G["bqkv"], workspace=self.ws)
-        mt.linear_bwd(None, self._weight("wqkv"), self.dqkv, self.dx, accumulate=True, workspace=self.ws)
+        mt.linear_bwd(None, self._weight("wqkv"), self.dqkv, self.dx, accumulate=through, workspace=self.ws)
 
     def step(self, x, target, kv_len):
         """One training step; the loss stays on the device (self.loss)."""
@@ -164,11 +166,11 @@ class AttentionBlock:
         self.refresh()
 
     # ----------------------------------------------------------------------- serving
-    def decode(self, x, k_cache, v_cache, lens):
-        """One token of each sequence: x [B, C] fp32 and caches [B, tokens, HK, D] holding lens [B] int32 tokens each;
-        appends the new keys and values and returns h [B, C] (no dropout). The caller counts lens up."""
+    def decode(self, x, k_cache, v_cache, lens, residual=None):
+        """One token of each sequence: x [B, C] and caches [B, tokens, HK, D] holding lens [B] int32 tokens each; appends
+        the new keys and values and returns h [B, C] (no dropout). The caller counts lens up."""
         B, P = x.shape[0], self.params
-        x16 = x if self.dtype == torch.float32 else x.to(self.dtype)
+        x16 = x.to(self.dtype)
         qkv = torch.empty(B, self.qkv.shape[1], device=DEV)
         mt.linear_fwd(x16, self._weight("wqkv"), P["bqkv"], qkv)
         q32, k32, v32 = self._heads(qkv, B, 1)
@@ -183,7 +185,7 @@ class AttentionBlock:
         mt.attention_fwd(q, k_cache, v_cache, o, causal=True, kv_len=lens + 1, q_start=lens, workspace=ws)
         y, h = torch.empty(B, self.C, device=DEV), torch.empty(B, self.C, device=DEV)
         mt.linear_fwd(o.view(B, -1), self._weight("wo"), P["bo"], y)
-        mt.dropout_fwd(y, x, 0.0, 0, 0, h)
+        mt.dropout_fwd(y, x if residual is None else residual, 0.0, 0, 0, h)
         return h
 
 
