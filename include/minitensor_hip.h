@@ -514,7 +514,8 @@ mt_status mt_embedding_bwd_workspace(const mt_tensor* ids, const mt_tensor* dy,
  * var the mean of (x - mean x)^2.
  *   x, y [M, C] f32 or bf16 each, any row pitch, rows contiguous; C is 1 to 16384
  *   w, b [C] f32, or NULL (ones, zeros); eps >= 0
- * Arithmetic is fp32; y is rounded once.
+ * Arithmetic is fp32; y is rounded once. Deviations from the mean of up to 2^56
+ * (their squares' sum is finite in fp32) and, with eps = 0, of 2^-60 and more.
  */
 mt_status mt_layer_norm_fwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* b, float eps,
                             const mt_tensor* y, void* stream);

@@ -186,8 +186,9 @@ def _current_stream() -> int:
     return _raw_stream(_device())
 
 
-_m.init(lib._handle, torch.float32, torch.bfloat16, torch.int32, desc, _current_stream, _stream, torch.Tensor,
-        torch.nn.Parameter)
+_INIT = (lib._handle, torch.float32, torch.bfloat16, torch.int32, desc, _current_stream, _stream, torch.Tensor,
+         torch.nn.Parameter, _device)
+_m.init(*_INIT)
 
 
 def linear_fwd(x, w, b, y, stream=None) -> None:

@@ -96,8 +96,8 @@ __device__ __forceinline__ void put(void* dr, int e0, int n, int32_t t, float c,
 // far, raised together, and reads them again for the gradient, 16 values at a
 // time, from the caches.
 template <bool XB, bool YB, int VEC, int NV, bool REST>
-__global__ __launch_bounds__(512, REST ? 4 : 6) void row_kernel(const CrossEntropyParams p) {
-  __shared__ float red[2][8];
+__global__ __launch_bounds__(REST ? 1024 : 512, REST ? 4 : 6) void row_kernel(const CrossEntropyParams p) {
+  __shared__ float red[2][16];
   const int step = (int)blockDim.x * VEC, first = (int)threadIdx.x * VEC;
   for (int64_t m = blockIdx.x; m < p.M; m += gridDim.x) {
     const int32_t t = p.targets[m];

@@ -7,10 +7,10 @@
 // tensor), anything else by its Python attributes (0.5 us).
 //
 // init(handle, float32, bfloat16, int32, describe, current_stream, stream_of,
-// tensor, parameter): the library's dlopen handle, torch's dtypes, binding.desc
+// tensor, parameter, device): the library's dlopen handle, torch's dtypes, binding.desc
 // (called to raise its error for a tensor that is refused), how a stream is found
-// (none given / given) and torch's two plain tensor types. Every other function
-// returns the entry point's status.
+// (none given / given), torch's two plain tensor types and how the current device
+// is found. Every other function returns the entry point's status.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/dlpack.h>
@@ -20,7 +20,7 @@
 
 namespace {
 
-PyObject *g_f32, *g_bf16, *g_i32, *g_describe, *g_current, *g_stream_of, *g_tensor, *g_parameter;
+PyObject *g_f32, *g_bf16, *g_i32, *g_describe, *g_current, *g_stream_of, *g_tensor, *g_parameter, *g_device;
 const DLPackExchangeAPI* g_exchange;  // torch's; NULL: none
 PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_numel, *s_element_size;
 
@@ -101,7 +101,8 @@ bool view_of(PyObject* t, DLTensor* x) {
 bool on_device(const DLTensor& x) { return x.device.device_type == kDLROCM || x.device.device_type == kDLCUDA; }
 
 // index: a tensor of int32 lengths, positions, tokens or classes, else one of the two dtypes.
-bool describe(PyObject* t, mt_tensor* d, bool index = false) {
+// device: receives a plain tensor's.
+bool describe(PyObject* t, mt_tensor* d, bool index = false, int* device = nullptr) {
   DLTensor x;
   if (view_of(t, &x)) {
     if (!on_device(x) || x.dtype.lanes != 1 || x.ndim > MT_MAX_DIMS) return refuse(t, index);
@@ -109,6 +110,7 @@ bool describe(PyObject* t, mt_tensor* d, bool index = false) {
     else if (!index && x.dtype.code == kDLFloat && x.dtype.bits == 32) d->dtype = MT_F32;
     else if (!index && x.dtype.code == kDLBfloat && x.dtype.bits == 16) d->dtype = MT_BF16;
     else return refuse(t, index);
+    if (device) *device = x.device.device_id;
     d->data = (char*)x.data + x.byte_offset;
     d->ndim = x.ndim;
     for (int i = 0; i < x.ndim; ++i) {
@@ -143,6 +145,8 @@ struct Args {
   bool ok = true;
   mt_tensor d[12];
   int used = 0;
+  int device = -1;  // of the tensors so far
+  bool mixed = false;
   Args(PyObject* const* args, Py_ssize_t n, Py_ssize_t want) : a(args) {
     if (n != want) {
       PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
@@ -152,8 +156,30 @@ struct Args {
   const mt_tensor* tensor(int i, bool index = false) {
     if (!ok || a[i] == Py_None) return nullptr;
     mt_tensor* t = &d[used++];
-    ok = describe(a[i], t, index);
+    int dev = -1;
+    ok = describe(a[i], t, index, &dev);
+    met(dev);
     return t;
+  }
+  void met(int dev) {
+    if (dev < 0) return;
+    mixed = mixed || (device >= 0 && device != dev);
+    device = dev;
+  }
+  // The tensors lie on one device, where none is given for the stream the current one.
+  bool one_device(int stream) {
+    if (!ok) return false;
+    if (mixed) {
+      PyErr_SetString(PyExc_ValueError, "the tensors lie on different devices");
+      return ok = false;
+    }
+    if (device < 0 || a[stream] != Py_None) return true;
+    PyObject* now = PyObject_CallNoArgs(g_device);
+    const long n = now ? PyLong_AsLong(now) : -1;
+    Py_XDECREF(now);
+    if (PyErr_Occurred()) return ok = false;
+    if (n != device) PyErr_Format(PyExc_ValueError, "the tensors lie on device %d, the current one is %ld", device, n);
+    return ok = n == device;
   }
   uint64_t u64(int i) {
     if (!ok) return 0;
@@ -181,6 +207,7 @@ struct Args {
     if (!ok || a[i] == Py_None) return w;
     DLTensor x;
     if (view_of(a[i], &x) && on_device(x)) {
+      met(x.device.device_id);
       w.p = (char*)x.data + x.byte_offset;
       w.n = ((size_t)x.dtype.bits * x.dtype.lanes + 7) / 8;
       for (int d = 0; d < x.ndim; ++d) w.n *= (size_t)x.shape[d];
@@ -366,7 +393,7 @@ FN(embedding_fwd) {  // ids, table, scale, y, stream
   const float scale = g.f32(2);
   const mt_tensor* y = g.tensor(3);
   void* st = g.stream(4);
-  return call(g.ok, [&] { return L.embedding_fwd(ids, t, scale, y, st); });
+  return call(g.one_device(4), [&] { return L.embedding_fwd(ids, t, scale, y, st); });
 }
 FN(embedding_bwd) {  // ids, dy, scale, dtable, flags, ws, stream
   Args g(a, n, 7);
@@ -376,7 +403,7 @@ FN(embedding_bwd) {  // ids, dy, scale, dtable, flags, ws, stream
   const uint32_t flags = (uint32_t)g.i64(4);
   const Args::Ws ws = g.ws(5);
   void* st = g.stream(6);
-  return call(g.ok, [&] { return L.embedding_bwd(ids, dy, scale, d, flags, ws.p, ws.n, st); });
+  return call(g.one_device(6), [&] { return L.embedding_bwd(ids, dy, scale, d, flags, ws.p, ws.n, st); });
 }
 FN(layer_norm_fwd) {  // x, w, b, eps, y, stream
   Args g(a, n, 6);
@@ -384,7 +411,7 @@ FN(layer_norm_fwd) {  // x, w, b, eps, y, stream
   const float eps = g.f32(3);
   const mt_tensor* y = g.tensor(4);
   void* st = g.stream(5);
-  return call(g.ok, [&] { return L.layer_norm_fwd(x, w, b, eps, y, st); });
+  return call(g.one_device(5), [&] { return L.layer_norm_fwd(x, w, b, eps, y, st); });
 }
 FN(layer_norm_bwd) {  // x, w, dy, eps, dx, dw, db, flags, ws, stream
   Args g(a, n, 10);
@@ -394,14 +421,14 @@ FN(layer_norm_bwd) {  // x, w, dy, eps, dx, dw, db, flags, ws, stream
   const uint32_t flags = (uint32_t)g.i64(7);
   const Args::Ws ws = g.ws(8);
   void* st = g.stream(9);
-  return call(g.ok, [&] { return L.layer_norm_bwd(x, w, dy, eps, dx, dw, db, flags, ws.p, ws.n, st); });
+  return call(g.one_device(9), [&] { return L.layer_norm_bwd(x, w, dy, eps, dx, dw, db, flags, ws.p, ws.n, st); });
 }
 FN(cross_entropy) {  // logits, targets, loss, losses, dlogits, ws, stream
   Args g(a, n, 7);
   const mt_tensor *z = g.tensor(0), *t = g.tensor(1, true), *l = g.tensor(2), *ls = g.tensor(3), *d = g.tensor(4);
   const Args::Ws ws = g.ws(5);
   void* st = g.stream(6);
-  return call(g.ok, [&] { return L.cross_entropy(z, t, l, ls, d, ws.p, ws.n, st); });
+  return call(g.one_device(6), [&] { return L.cross_entropy(z, t, l, ls, d, ws.p, ws.n, st); });
 }
 
 // Descriptors of up to four lists of n tensors each, one list after another.
@@ -413,7 +440,7 @@ struct Lists {
   mt_tensor* d = nullptr;
   Py_ssize_t n = 0;
   bool ok = true;
-  Lists(PyObject* const* a, int lists) {
+  Lists(PyObject* const* a, int lists, Args* args = nullptr) {
     for (int l = 0; ok && l < lists; ++l) ok = PyObject_Size(a[l]) >= 0 && (held[l] = PySequence_Tuple(a[l])) != nullptr;
     if (!ok) return;
     n = PyTuple_GET_SIZE(held[0]);
@@ -429,7 +456,11 @@ struct Lists {
       ok = false;
     }
     for (int l = 0; ok && l < lists; ++l)
-      for (Py_ssize_t i = 0; ok && i < n; ++i) ok = describe(PyTuple_GET_ITEM(held[l], i), &d[l * n + i]);
+      for (Py_ssize_t i = 0; ok && i < n; ++i) {
+        int dev = -1;
+        ok = describe(PyTuple_GET_ITEM(held[l], i), &d[l * n + i], false, &dev);
+        if (args) args->met(dev);
+      }
   }
   ~Lists() {
     PyMem_Free(d);
@@ -470,20 +501,20 @@ FN(clip_grad_norm) {  // grads, out, max_norm, norm, ws, stream
   Args g(a, n, 6);
   if (!g.ok) return nullptr;
   const bool in_place = a[1] == Py_None;
-  const Lists t(a, in_place ? 1 : 2);
+  const Lists t(a, in_place ? 1 : 2, &g);
   if (!t.ok) return nullptr;
   const float most = g.f32(2);
   const mt_tensor* norm = g.tensor(3);
   const Args::Ws ws = g.ws(4);
   void* st = g.stream(5);
-  return call(g.ok, [&] {
+  return call(g.one_device(5), [&] {
     return L.clip_grad_norm((int32_t)t.n, t[0], most, in_place ? nullptr : t[1], norm, ws.p, ws.n, st);
   });
 }
 
 FN(init) {
-  if (n != 9) {
-    PyErr_SetString(PyExc_TypeError, "init(handle, float32, bfloat16, int32, describe, current_stream, stream_of, tensor, parameter)");
+  if (n != 10) {
+    PyErr_SetString(PyExc_TypeError, "init(handle, float32, bfloat16, int32, describe, current_stream, stream_of, tensor, parameter, device)");
     return nullptr;
   }
   void* h = PyLong_AsVoidPtr(a[0]);
@@ -502,8 +533,8 @@ FN(init) {
   SYM(dropout_bwd) SYM(embedding_fwd) SYM(embedding_bwd) SYM(layer_norm_fwd) SYM(layer_norm_bwd) SYM(cross_entropy)
   SYM(clip_grad_norm)
 #undef SYM
-  PyObject** to[] = {&g_f32, &g_bf16, &g_i32, &g_describe, &g_current, &g_stream_of, &g_tensor, &g_parameter};
-  for (int i = 0; i < 8; ++i) {
+  PyObject** to[] = {&g_f32, &g_bf16, &g_i32, &g_describe, &g_current, &g_stream_of, &g_tensor, &g_parameter, &g_device};
+  for (int i = 0; i < 9; ++i) {
     Py_INCREF(a[i + 1]);
     Py_XSETREF(*to[i], a[i + 1]);
   }

@@ -53,3 +53,26 @@ def test_refusals():
         b.linear_bwd(t, t, t, t.clone(), workspace=torch.empty(64))
     with pytest.raises(TypeError, match="int32"):
         b.embedding_fwd(t.long(), t, t.clone())
+
+
+def test_tensors_of_another_device_are_refused():
+    """With another current device than the tensors' (one card: the binding is told so) the newer calls refuse, unless
+    their stream is given."""
+    t, ids = torch.zeros(4, 4, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+    calls = [lambda **k: b.embedding_fwd(ids, t, t.clone(), **k), lambda **k: b.layer_norm_fwd(t, None, None, t.clone(), **k),
+             lambda **k: b.embedding_bwd(ids, t, t.clone(), workspace=ws, **k), lambda **k: b.layer_norm_bwd(t, None, t, t.clone(), **k),
+             lambda **k: b.cross_entropy(t, ids, losses=t[0].clone(), workspace=ws, **k),
+             lambda **k: b.clip_grad_norm([t.clone()], 1.0, workspace=ws, **k)]
+    for call in calls:
+        call()
+    b._m.init(*b._INIT[:-1], lambda: 1)
+    try:
+        for call in calls:
+            with pytest.raises(ValueError, match="device"):
+                call()
+            call(stream=torch.cuda.current_stream())
+    finally:
+        b._m.init(*b._INIT)
+    calls[0]()
+    torch.cuda.synchronize()
