@@ -4,22 +4,29 @@
 //
 // A token whose id is not a row of E (padding) gets zeros and gives nothing.
 //
-// The lookup is bound by HBM: a group of lanes copies a token's row.
+// The lookup is bound by HBM: a group of lanes copies a token's row, four at a time
+// where there are many (16384 x 1024 fp32 22.8 -> 20.6 us: 4.4 TB/s).
 //
 // The gradient groups the tokens by id, without atomics in memory and with the
 // tokens of an id in ascending order, so that its sums have one order:
 //
 // 1. group_kernel. The low bits of an id name its bucket, a block each. A block
 //    reads all ids: it counts those of lower buckets (where its own begin) and
-//    its own, by wave and id, in LDS; a scan turns the counts into places; a
-//    second reading hands the places out, 64 tokens at a time, tokens of one id
-//    by their order among the lanes. Integers throughout. Blocks past the
-//    buckets clear dE meanwhile.
-// 2. sum_kernel. Chunks of the grouped tokens, a group of lanes each: a run
-//    (the tokens of an id) inside a chunk goes to dE, what belongs to a run that
-//    the chunk cuts goes to the workspace. Work is even whatever the ids are.
+//    its own, by wave and id, in LDS; a scan turns the counts into places; the
+//    ids, still in registers or read again, are handed the places, 64 tokens at a
+//    time, tokens of one id by their order among the lanes. Integers throughout.
+// 2. sum_kernel. Chunks of the grouped tokens, a wave or less each and tile of
+//    columns: a run (the tokens of an id) inside a chunk goes to dE, what belongs
+//    to a run that the chunk cuts goes to the workspace. Work is even whatever the
+//    ids are. Beside it, blocks clear the rows without a token.
 // 3. join_kernel. Where a run goes on past its first chunk, its pieces are added
 //    in order.
+//
+// 16384 tokens of 1024 fp32 values into 50001 rows: 73 us for 272 MB, of which the
+// first launch takes 9 (it waits for loads, LDS and its own order), the second 55
+// (276 MB moved, 5.0 TB/s), the third 7 (a chain of loads). Clearing part of the
+// rows in the first and the last launch too moved their time, and saved none.
+// A few tokens take one launch instead (few_kernel).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -265,6 +272,92 @@ __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, 
   put(p, id, d, n, acc, old);
 }
 
+constexpr int kFewThreads = 512;
+// A few tokens: one launch, no lists. A block takes a token and a tile of
+// columns; where no earlier token has its id it finds those that have, in order,
+// and its groups of G lanes add equal shares of their rows, which meet in
+// LDS. Blocks past these clear ranges of rows, which they look up in all tokens.
+template <bool BF>
+__global__ __launch_bounds__(kFewThreads) void few_kernel(const EmbeddingGradParams p, int G_shift, int tiles, int sum_blocks, int clear_rows) {
+  constexpr int VEC = 4, U = 8, PER = kEmbedFewTokens / kFewThreads;
+  __shared__ float sums[kFewThreads * VEC];
+  __shared__ uint16_t list[kEmbedFewTokens];
+  __shared__ int wave_count[kFewThreads / 64];
+  __shared__ uint8_t seen[kEmbedFewClear];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, M = (int)p.M;
+  const int G = 1 << G_shift, groups = kFewThreads >> G_shift, grp = threadIdx.x >> G_shift, D = (int)p.D;
+  int32_t id[PER];  // of the wave's share of the tokens, 64 at a time
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int m = wave * (64 * PER) + 64 * j + lane;
+    id[j] = m < M ? p.ids[m] : -1;
+  }
+  if ((int)blockIdx.x >= sum_blocks) {
+    const int64_t v0 = (int64_t)(blockIdx.x - sum_blocks) * clear_rows;
+    for (int i = threadIdx.x; i < clear_rows; i += kFewThreads) seen[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (id[j] >= v0 && id[j] < v0 + clear_rows) seen[id[j] - v0] = 1;
+    __syncthreads();
+    const float zero[4] = {};
+    for (int i = grp; i < clear_rows && v0 + i < p.V; i += groups) {
+      if (seen[i]) continue;
+      for (int d = (threadIdx.x & (G - 1)) * 4; d < D; d += G * 4) store_some<false, 4>(p.dtable, (v0 + i) * p.ldt + d, D - d, zero);
+    }
+    return;
+  }
+  const int m = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+  const int32_t v = p.ids[m];
+  if ((uint32_t)v >= (uint64_t)p.V) return;
+  uint64_t same[PER];
+  int mine = 0, earlier = 0;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    same[j] = __ballot(id[j] == v);
+    mine += __popcll(same[j]);
+    earlier += __popcll(__ballot(id[j] == v && wave * (64 * PER) + 64 * j + lane < m));
+  }
+  if (__syncthreads_or(earlier)) return;
+  if (lane == 0) wave_count[wave] = mine;
+  __syncthreads();
+  int at = 0, n = 0;
+  for (int w = 0; w < kFewThreads / 64; ++w) {
+    at += w < wave ? wave_count[w] : 0;
+    n += wave_count[w];
+  }
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    if (id[j] == v) list[at + __popcll(same[j] & ((1ull << lane) - 1))] = (uint16_t)(wave * (64 * PER) + 64 * j + lane);
+    at += __popcll(same[j]);
+  }
+  __syncthreads();
+  const int d = (tile * G + (threadIdx.x & (G - 1))) * VEC, left = D - d;
+  float acc[VEC], old[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+  load_some<false, VEC>(p.dtable, v * p.ldt + d, p.accumulate && grp == 0 ? left : 0, 0.f, old);
+  const int share = (n + groups - 1) / groups, i1 = min((grp + 1) * share, n);
+  for (int i = grp * share; i < i1; i += U) {
+    float x[U][VEC];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      load_some<BF, VEC>(p.dy, (i + u < i1 ? list[i + u] : 0) * p.ldy + d, i + u < i1 ? left : 0, 0.f, x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] += x[u][e];
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sums[threadIdx.x * VEC + e] = acc[e];
+  __syncthreads();
+  if (grp || left <= 0) return;
+  for (int g = 1; g < groups && g * share < n; ++g)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc[e] += sums[(g * G + threadIdx.x) * VEC + e];
+  put(p, v, d, left, acc, old);
+}
+
 // Lanes of a row: a power of two, 2^most at most.
 int lanes_shift(int64_t D, int vec, int most) {
   int s = 0;
@@ -303,6 +396,18 @@ EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D) {
 
 hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& f, bool bf16, hipStream_t stream) {
   using namespace embedding;
+  // One launch for few tokens: 64 of 64 columns into 50001 rows 16.1 -> 5.7 us, 2000 of 256 added to 20000 rows
+  // 16.2 -> 8.1, 1000 of 1024 bf16 17.7 -> 15.5; past 4096 tiles each block's search costs more than the other two
+  // launches (1000 of 2048: 19 -> 27). A batch of one token alone may lose (2000 of 256: 22 -> 36).
+  if (p.M > 0 && p.M <= kEmbedFewTokens && p.M * f.tiles <= 4096) {
+    const int sums = (int)p.M * f.tiles;
+    const int clear_rows = (int)std::max<int64_t>((p.V + 1023) / 1024, std::max<int64_t>(1, std::min<int64_t>(1024, 4096 / p.D)));
+    const int clears = p.accumulate ? 0 : (int)((p.V + clear_rows - 1) / clear_rows);
+    const dim3 grid((unsigned)(sums + clears));
+    if (bf16) few_kernel<true><<<grid, kFewThreads, 0, stream>>>(p, f.shift, f.tiles, sums, clear_rows);
+    else few_kernel<false><<<grid, kFewThreads, 0, stream>>>(p, f.shift, f.tiles, sums, clear_rows);
+    return hipGetLastError();
+  }
   const int buckets = 1 << p.bucket_shift, locals = (int)((p.V + buckets - 1) >> p.bucket_shift);
   group_kernel<<<dim3((unsigned)buckets), kGroupThreads, 0, stream>>>(p, locals);
   const int rows = 256 >> f.shift;

@@ -60,7 +60,8 @@ def test_lookup_of_views(t, y):
 @pytest.mark.parametrize("y", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["even", "few", "one", "padded"])
 @pytest.mark.parametrize("M,V,D", [(1, 1, 1), (16, 1, 8), (17, 5, 33), (1000, 300, 77), (5000, 70000, 24), (4096, 513, 256),
-                                   (2500, 20, 1030), (33, 100000, 5)])
+                                   (2500, 20, 1030), (33, 100000, 5), (2048, 700, 500),
+                                   (2049, 700, 40), (300, 17000, 4100)])
 def test_gradient(M, V, D, kind, y):
     ids, dy = tokens((M,), V, kind, 5), draw((M, D), y, 6)
     if kind == "padded":  # rows without a token may hold anything
@@ -86,7 +87,8 @@ def test_gradient_is_added(kind, y):
 def test_gradient_of_views(y):
     place = Apart()
     ids = tokens((12, 40), 25, "padded", 10)
-    for view in (ids, ids.T, ids[::2, 1::3]):
+    ids = torch.cat([ids, tokens((60, 40), 25, "padded", 18)])  # many tokens, and below a few
+    for view in (ids, ids.T, ids[::2, 1::3], ids[:12], ids[:12].T):
         dy = place.inside(draw((view.numel(), 21), y, 11))
         dt = place.out(25, 21, torch.float32)
         run_bwd(view, dy, dt)
@@ -109,6 +111,20 @@ def test_runs_that_end_at_every_place():
     dt = torch.empty((119, 300), device=DEV)
     run_bwd(ids, dy, dt)
     close("dtable", dt, *embedding_grad(ids, dy, 119, 1.0))
+
+
+@pytest.mark.parametrize("M", [2000, 5000])
+def test_few_and_many_tokens_keep_apart(M):
+    """Rows between those that tokens name stay as they are, or become 0, at every place of a range of rows."""
+    V = 40000
+    ids = torch.randperm(V, generator=torch.Generator("cpu").manual_seed(M))[:M].int().to(DEV)
+    dy, old = draw((M, 12), "f32", 19), draw((V, 12), "f32", 20)
+    dt = run_bwd(ids, dy, old.clone(), accumulate=True)
+    want = old.clone()
+    want[ids.long()] += dy
+    assert torch.equal(dt, want)
+    run_bwd(ids, dy, dt.fill_(float("nan")))
+    assert torch.equal(dt, torch.zeros_like(dt).index_copy_(0, ids.long(), dy))
 
 
 def test_the_order_of_a_token_s_rows_is_theirs():
