@@ -51,7 +51,7 @@ struct LayerNormParams {
   void* out;  // y, or dx (NULL: none)
   float* part;  // backward: [blocks][2][C] sums of dw and db, or NULL
   int64_t M, ldx, ldd, ldo;
-  int32_t C, L, L_shift;  // L lanes a row (a power of two)
+  int32_t C, L;  // L lanes a row: a power of two up to a wave, or whole waves
   int32_t accumulate;
   float eps, C_f;  // C as a float: means are quotients, so that rows of one value have exact ones
 };

@@ -194,11 +194,18 @@ NormForm norm_form(mt::LayerNormParams* p, int vec, int threads, int most_blocks
   // groups a lane: 8 values of short rows, 16 of others (524288 x 64 bf16 33 -> 26 us, its gradient
   // 55 -> 49; at 1024 columns, by 128 lanes, the gradient 47 -> 62)
   const int most = (p->C <= 512 ? 8 : 16) / vec;
-  for (p->L = 1, p->L_shift = 0; p->L < 64 && p->L * vec * most < p->C; p->L *= 2) ++p->L_shift;
-  while (p->L * vec * most < p->C) p->L *= 2, ++p->L_shift;
+  for (p->L = 1; p->L < 64 && p->L * vec * most < p->C;) p->L *= 2;
+  if (p->L * vec * most < p->C) {
+    // as few whole waves as hold a row (13107 x 2560 bf16 40 us by four, 28 by three; 2730 x 12288 44 by 16, 36 by
+    // 12), but eight rather than six or seven (5461 x 6144 32 us by eight, 38 by six)
+    int waves = (int)cdiv(p->C, (int64_t)64 * vec * most);
+    if (waves == 6 || waves == 7) waves = 8;
+    p->L = 64 * waves;
+  }
   f.nv = (int)cdiv(p->C, (int64_t)p->L * vec);
-  f.threads = std::max(threads, p->L);
-  f.blocks = (int)std::min<int64_t>(most_blocks, std::max<int64_t>(1, cdiv(p->M, f.threads / p->L)));
+  const int rows = std::max(1, threads / p->L);
+  f.threads = rows * p->L;
+  f.blocks = (int)std::min<int64_t>(most_blocks, std::max<int64_t>(1, cdiv(p->M, rows)));
   return f;
 }
 
@@ -235,9 +242,9 @@ mt_status layer_norm_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
   if ((dw && (s = check_vector(dw, "dw", p.C))) || (db && (s = check_vector(db, "db", p.C))) ||
       (s = check_apart({dx, dw, db}, {x, w, dy})))
     return s;
-  // two blocks a CU where a row is a wave's (524288 x 64 fp32 93 -> 86 us, 32768 x 1024 bf16 50 -> 47);
-  // of longer rows one, whose sums of dw and db are half as many
-  const NormForm f = norm_form(&p, vector_of({x, dy}), p.C <= 1024 ? 512 : 1024, p.C <= 1024 ? 512 : 256);
+  // two blocks a CU up to 4096 columns (524288 x 64 fp32 93 -> 86 us, 16384 x 2048 bf16 61 -> 55); of longer rows
+  // one, whose sums of dw and db are half as many (4096 x 8192 bf16 70 us, two blocks 74)
+  const NormForm f = norm_form(&p, vector_of({x, dy}), p.C <= 4096 ? 512 : 1024, p.C <= 4096 ? 512 : 256);
   const bool weights = dw || db;
   const size_t need = weights ? (size_t)f.blocks * 2 * p.C * sizeof(float) : 0;
   if (ws_query) {

@@ -3,8 +3,8 @@
 //   mu = mean x,  r = (mean (x - mu)^2 + eps)^(-1/2),  n = (x - mu) r,  y = n w + b
 //   g = dy w,  dx = r (g - mean g - n mean(g n)),  dw = sum over rows of dy n,  db = of dy
 //
-// A row is read once and held in registers by L lanes (a power of two, up to a
-// block), so that the variance is a mean of squared deviations and not a
+// A row is read once and held in registers by L lanes (a power of two up to a
+// wave, or whole waves), so that the variance is a mean of squared deviations and not a
 // difference of large numbers, and the gradient needs no saved statistics: it
 // takes them again from the row that it reads anyway. Bound: HBM (16384 x 1024 fp32
 // to bf16 18.9 us, 5.3 TB/s; gradient of 8192 x 8192 fp32 170 us, 4.7 TB/s; bf16
@@ -27,11 +27,11 @@ using namespace vio;
 // Sums over a row's lanes; rows of more than a wave (WIDE) meet in LDS, one
 // buffer a sum, used again only after another sum's barrier.
 template <bool WIDE, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], int L, float (*red)[16]) {
+__device__ __forceinline__ void row_sums(float (&v)[N], int L, int grp, float (*red)[16]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = lanes_sum(v[i], WIDE ? 64 : L);
   if constexpr (WIDE) {
-    const int wave = threadIdx.x >> 6, W = L >> 6, first = wave & ~(W - 1);
+    const int wave = threadIdx.x >> 6, W = L >> 6, first = grp * W;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
       for (int i = 0; i < N; ++i) red[i][wave] = v[i];
@@ -55,7 +55,7 @@ template <int VEC, bool WHOLE>
 struct Columns {
   int c, lo, hi;
   __device__ __forceinline__ Columns(int l, int k, const LayerNormParams& p) {
-    const int first = (l + (k << p.L_shift)) * VEC;
+    const int first = (l + k * p.L) * VEC;
     c = WHOLE ? first : max(min(first, p.C - VEC), 0);
     lo = WHOLE ? (first < p.C ? 0 : VEC) : first - c;
     hi = WHOLE ? VEC : min(p.C, VEC);
@@ -71,7 +71,7 @@ struct Columns {
 template <bool XB, bool YB, int VEC, int NV, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
   __shared__ float red[2][16];
-  const int l = threadIdx.x & (p.L - 1), rows = blockDim.x >> p.L_shift;
+  const int grp = threadIdx.x / (unsigned)p.L, l = threadIdx.x - grp * p.L, rows = blockDim.x / (unsigned)p.L;
   float w[NV][VEC], b[NV][VEC];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
   }
   // all rows of a block go through the loop the same number of times
   for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
-    const int64_t m = m0 + (threadIdx.x >> p.L_shift);
+    const int64_t m = m0 + grp;
     const bool on = m < p.M;
     float x[NV][VEC], s[1] = {0.f}, q[1] = {0.f};
 #pragma unroll
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
     }
-    row_sums<WIDE, 1>(s, p.L, red);
+    row_sums<WIDE, 1>(s, p.L, grp, red);
     const float mu = s[0] / p.C_f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
         q[0] = fmaf(c.has(e) ? x[k][e] : 0.f, x[k][e], q[0]);
       }
     }
-    row_sums<WIDE, 1>(q, p.L, red + 1);
+    row_sums<WIDE, 1>(q, p.L, grp, red + 1);
     const float r = 1.f / sqrtf(q[0] / p.C_f + p.eps);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -124,7 +124,7 @@ template <bool XB, bool YB, int VEC, int NV, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
   __shared__ float red[4][16];
   __shared__ float cols[1024 * 16];  // [group][C], where a block has several groups
-  const int l = threadIdx.x & (p.L - 1), rows = blockDim.x >> p.L_shift, grp = threadIdx.x >> p.L_shift;
+  const int grp = threadIdx.x / (unsigned)p.L, l = threadIdx.x - grp * p.L, rows = blockDim.x / (unsigned)p.L;
   float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
     }
-    row_sums<WIDE, 1>(s, p.L, red);
+    row_sums<WIDE, 1>(s, p.L, grp, red);
     const float mu = s[0] / p.C_f;
     // squares of the deviations, sums of g and of g times the deviations
 #pragma unroll
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
         t[2] = fmaf(d, gw, t[2]);
       }
     }
-    row_sums<WIDE, 3>(t, p.L, red + 1);
+    row_sums<WIDE, 3>(t, p.L, grp, red + 1);
     const float r = 1.f / sqrtf(t[0] / p.C_f + p.eps);
     const float mg = t[1] / p.C_f, mgn = t[2] * r / p.C_f;  // the means of g and of g n
     if (!on) continue;  // no barrier below

@@ -145,6 +145,23 @@ def test_many_rows(M, V):
     assert all(torch.equal(a, c) for a, c in zip(got, again))
 
 
+@pytest.mark.parametrize("V,L", [(1030, 1), (3, 256)])
+def test_more_rows_than_blocks(V, L):
+    """More rows than the blocks of a launch (2^20, of L rows each) hold at a time."""
+    M = (1 << 20) * L + 300
+    z = torch.zeros((M, V), dtype=torch.bfloat16, device=DEV)
+    t = torch.full((M,), -1, dtype=torch.int32, device=DEV)
+    at = torch.tensor([0, 5, (1 << 20) * L - 1, (1 << 20) * L, M - 1], device=DEV)
+    z[at] = draw((5, V), "bf16", 20)
+    t[at] = targets(5, V, False, 21)
+    loss, losses, dz = run(z, t, torch.bfloat16)
+    want = cross_entropy(z[at], t[at], torch.bfloat16)
+    close("loss", loss, *want[0])
+    close("losses", losses[at], *want[1])
+    close("dlogits", dz[at], *want[2])
+    assert torch.count_nonzero(losses) == 5 and torch.count_nonzero(dz.any(-1)) == 5
+
+
 def test_gradient_against_differences():
     """Of the loss in 64 bits, by central differences, off by h^2 / 6 of a third derivative below 1."""
     z, t = draw((3, 9), "f32", 17), torch.tensor([2, -1, 8], dtype=torch.int32, device=DEV)

@@ -35,7 +35,8 @@ def run_bwd(x, w, dy, dx, dw, db, eps=EPS, accumulate=False):
 
 
 SIZES = [(1, 1), (1, 4096), (7, 16384), (3, 16383), (64, 4096), (100, 1), (130, 3), (1000, 16), (33, 17), (257, 100),
-         (50, 255), (50, 777), (9, 1025), (21, 2048), (5, 5000), (2, 8193), (700, 513)]
+         (50, 255), (50, 777), (9, 1025), (21, 2048), (5, 5000), (2, 8193), (700, 513), (40, 2560), (11, 2999), (13, 6144),
+         (5, 7001), (4, 12288), (3, 10007)]
 
 
 @pytest.mark.parametrize("x,y", TYPES)
