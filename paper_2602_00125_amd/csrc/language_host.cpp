@@ -189,11 +189,9 @@ mt_status like(const mt_tensor* t, const char* name, const mt_tensor* x, bool ou
 struct NormForm {
   int nv, threads, blocks;
 };
-NormForm norm_form(mt::LayerNormParams* p, int vec, int threads, int most_blocks) {
+NormForm norm_form(mt::LayerNormParams* p, int vec, int values, int threads, int most_blocks) {
   NormForm f{1, threads, 1};
-  // groups a lane: 8 values of short rows, 16 of others (524288 x 64 bf16 33 -> 26 us, its gradient
-  // 55 -> 49; at 1024 columns, by 128 lanes, the gradient 47 -> 62)
-  const int most = (p->C <= 512 ? 8 : 16) / vec;
+  const int most = values / vec;  // groups a lane
   for (p->L = 1; p->L < 64 && p->L * vec * most < p->C;) p->L *= 2;
   if (p->L * vec * most < p->C) {
     // as few whole waves as hold a row (13107 x 2560 bf16 40 us by four, 28 by three; 2730 x 12288 44 by 16, 36 by
@@ -222,7 +220,11 @@ mt_status layer_norm_fwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
   p.b = b ? (const float*)b->data : nullptr;
   p.out = y->data;
   p.ldo = row_pitch(y);
-  const NormForm f = norm_form(&p, vector_of({x, y}), 256, 2048);
+  // 16 values a lane, or 8 where that takes a part of a wave, three, four or eight waves (524288 x 64 bf16 33 -> 26
+  // us, 21845 x 1536 35 -> 28, 8192 x 4096 32 -> 29; by five waves 13107 x 2560 28 -> 32)
+  const int waves = (int)cdiv(p.C, 512);
+  const int values = p.C <= 512 || waves == 3 || waves == 4 || waves == 8 ? 8 : 16;
+  const NormForm f = norm_form(&p, vector_of({x, y}), values, 256, 2048);
   (void)hipGetLastError();
   return hip_status(mt::layer_norm_fwd(p, x->dtype == MT_BF16, y->dtype == MT_BF16, f.nv, f.threads, f.blocks, stream));
 }
@@ -244,7 +246,9 @@ mt_status layer_norm_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
     return s;
   // two blocks a CU up to 4096 columns (524288 x 64 fp32 93 -> 86 us, 16384 x 2048 bf16 61 -> 55); of longer rows
   // one, whose sums of dw and db are half as many (4096 x 8192 bf16 70 us, two blocks 74)
-  const NormForm f = norm_form(&p, vector_of({x, dy}), p.C <= 4096 ? 512 : 1024, p.C <= 4096 ? 512 : 256);
+  // 8 values a lane for short rows (524288 x 64 bf16 55 -> 49), 16 for others (32768 x 1024 bf16 47, 8 values 62)
+  const NormForm f = norm_form(&p, vector_of({x, dy}), p.C <= 512 ? 8 : 16, p.C <= 4096 ? 512 : 1024,
+                               p.C <= 4096 ? 512 : 256);
   const bool weights = dw || db;
   const size_t need = weights ? (size_t)f.blocks * 2 * p.C * sizeof(float) : 0;
   if (ws_query) {
