@@ -340,50 +340,114 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
 }
 
 // ----------------------------------------------------------------- clipping
+namespace {
+
+// How many values a tensor that clipping takes has, -1 where something about it
+// is wrong; what, the checks of check_clip say.
+int64_t dense_numel(const mt_tensor* t) {
+  if (t->ndim < 0 || t->ndim > MT_MAX_DIMS || (t->dtype != MT_F32 && t->dtype != MT_BF16)) return -1;
+  int64_t n = 1;
+  for (int i = t->ndim - 1; i >= 0; --i) {
+    const int64_t size = t->shape[i];
+    if (size < 0 || size > (int64_t)1 << 40 || t->stride[i] < 0 || (size != 1 && t->stride[i] != n)) return -1;
+    n *= size;
+    if (n > (int64_t)1 << 40) return -1;
+  }
+  return n == 0 || t->data ? n : -1;
+}
+mt_status check_clip(const mt_tensor* t, bool out, int32_t i) {
+  const std::string name = (out ? "out " : "grad ") + std::to_string(i);
+  mt_status s = check_tensor(t, name.c_str(), 0, MT_MAX_DIMS);
+  if (s) return s;
+  if (!is_row_major(t)) return fail(MT_ERR_LAYOUT, name + ": must be contiguous");
+  return fail(MT_ERR_SHAPE, name + ": more than 2^40 values");
+}
+
+// A gradient that is not empty.
+struct ClipItem {
+  const mt_tensor* grad;
+  const mt_tensor* out;
+  int64_t numel;
+  int64_t chunks() const { return cdiv(numel, mt::kClipChunk); }
+};
+// What one launch takes of the items from `first` on: up to which, and its chunks.
+size_t clip_batch(const std::vector<ClipItem>& items, size_t first, bool in_place, int64_t* chunks) {
+  const size_t end = std::min(items.size(), first + (size_t)mt::ClipBatch::most(in_place));
+  *chunks = 0;
+  size_t i = first;
+  for (; i < end && *chunks + items[i].chunks() <= (1 << 30); ++i) *chunks += items[i].chunks();
+  return i;
+}
+size_t clip_parts(const std::vector<ClipItem>& items, bool in_place) {
+  size_t parts = 0;
+  int64_t chunks;
+  for (size_t i = 0; i < items.size(); parts += mt::clip_blocks(chunks)) i = clip_batch(items, i, in_place, &chunks);
+  return parts;
+}
+void clip_pack(const std::vector<ClipItem>& items, size_t first, size_t end, int64_t chunks, bool in_place, mt::ClipBatch* b) {
+  b->n = (int32_t)(end - first);
+  b->in_place = in_place;
+  b->chunks = (int32_t)chunks;
+  uint32_t* starts = (uint32_t*)b->starts();
+  uint32_t at = 0;
+  for (size_t i = first; i < end; ++i) {
+    const ClipItem& t = items[i];
+    const int kind = (t.grad->dtype == MT_BF16 ? mt::kClipSourceBf16 : 0) | (t.out->dtype == MT_BF16 ? mt::kClipDestBf16 : 0);
+    b->w[i - first] = mt::ClipBatch::source(t.grad->data, kind, t.numel);
+    if (!in_place) b->w[end - first + (i - first)] = (uint64_t)(uintptr_t)t.out->data;
+    starts[i - first] = at;
+    at += (uint32_t)t.chunks();
+  }
+}
+
+struct Range {
+  uintptr_t lo, hi;
+  bool written;
+};
+// Whether what is written overlaps anything else. Tensors cut from one buffer
+// mostly come by ascending address.
+bool any_written_overlaps(std::vector<Range>& r) {
+  auto before = [](const Range& a, const Range& b) { return a.lo < b.lo; };
+  if (!std::is_sorted(r.begin(), r.end(), before)) std::sort(r.begin(), r.end(), before);
+  uintptr_t far = 0, far_written = 0;  // ends of what came before: of all, of what is written
+  for (const Range& x : r) {
+    if (x.lo < far_written || (x.written && x.lo < far)) return true;
+    far = std::max(far, x.hi);
+    if (x.written) far_written = std::max(far_written, x.hi);
+  }
+  return false;
+}
+
+}  // namespace
+
 mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
                               const mt_tensor* norm, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
   if (n < 0) return fail(MT_ERR_INVALID, "mt_clip_grad_norm: negative tensor count");
   if (n > 0 && !grads) return fail(MT_ERR_NULL, "mt_clip_grad_norm: null array");
   mt_status s;
-  // Every launch's tensors: f(first, end, how many are not empty, chunks).
-  auto each_batch = [&](bool in_place, auto f) -> mt_status {
-    const int most = mt::ClipBatch::most(in_place);
-    for (int32_t i = 0; i < n;) {
-      int32_t first = i, held = 0;
-      int64_t chunks = 0;
-      for (; i < n && held < most; ++i) {
-        const int64_t pieces = cdiv(numel(&grads[i]), mt::kClipChunk);
-        if (chunks + pieces > (1 << 30)) break;
-        chunks += pieces;
-        held += pieces > 0;
-      }
-      if (held == 0) continue;
-      if (mt_status e = f(first, i, held, chunks)) return e;
-    }
-    return MT_OK;
+  std::vector<ClipItem> items;
+  std::vector<Range> ranges;
+  items.reserve(n);
+  ranges.reserve((size_t)n * (out ? 2 : 1) + 1);
+  auto take = [&](const mt_tensor* t, int64_t count, bool written) {
+    const uintptr_t lo = (uintptr_t)t->data;
+    ranges.push_back({lo, lo + (uintptr_t)count * elem_size(t->dtype), written});
   };
-  auto name = [&](bool o, int32_t i) { return (o ? "out " : "grad ") + std::to_string(i); };
   for (int32_t i = 0; i < n; ++i) {
-    for (int j = 0; j < (out ? 2 : 1); ++j) {
-      const mt_tensor* t = j ? &out[i] : &grads[i];
-      if (check_tensor(t, "", 0, MT_MAX_DIMS)) return check_tensor(t, name(j, i).c_str(), 0, MT_MAX_DIMS);
-      if (!is_row_major(t)) return fail(MT_ERR_LAYOUT, name(j, i) + ": must be contiguous");
-      if (j && (t->ndim != grads[i].ndim || !std::equal(t->shape, t->shape + t->ndim, grads[i].shape)))
-        return fail(MT_ERR_SHAPE, name(j, i) + " must have the shape of its gradient");
-      if (numel(t) > (int64_t)1 << 40) return fail(MT_ERR_SHAPE, name(j, i) + ": more than 2^40 values");
+    const int64_t count = dense_numel(&grads[i]);
+    if (count < 0) return check_clip(&grads[i], false, i);
+    if (out) {
+      if (dense_numel(&out[i]) < 0) return check_clip(&out[i], true, i);
+      if (out[i].ndim != grads[i].ndim || !std::equal(out[i].shape, out[i].shape + out[i].ndim, grads[i].shape))
+        return fail(MT_ERR_SHAPE, "out " + std::to_string(i) + " must have the shape of its gradient");
     }
+    if (count == 0) continue;
+    items.push_back({&grads[i], out ? &out[i] : &grads[i], count});
+    take(&grads[i], count, !out);
   }
-  auto parts_of = [&](bool in_place) {
-    size_t parts = 0;
-    each_batch(in_place, [&](int32_t, int32_t, int32_t, int64_t chunks) {
-      parts += mt::clip_blocks(chunks);
-      return MT_OK;
-    });
-    return parts;
-  };
   // a workspace serves both forms: the query does not know of out
-  const size_t parts = parts_of(!out);
-  const size_t need = round256(std::max({(size_t)1, parts, parts_of(out != nullptr)}) * sizeof(double));
+  const size_t parts = clip_parts(items, !out);
+  const size_t need = round256(std::max({(size_t)1, parts, clip_parts(items, out != nullptr)}) * sizeof(double));
   if (ws_query) {
     *ws_query = need;
     return MT_OK;
@@ -393,74 +457,38 @@ mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm,
     if ((s = check_tensor(norm, "norm", 0, MT_MAX_DIMS))) return s;
     if (norm->dtype != MT_F32) return fail(MT_ERR_DTYPE, "norm must be f32");
     if (numel(norm) != 1) return fail(MT_ERR_SHAPE, "norm must hold exactly one element");
+    take(norm, 1, true);
   }
-  // What is written overlaps nothing else: by ascending address, which tensors
-  // cut from one buffer mostly are in already.
-  struct Range {
-    uintptr_t lo, hi;
-    bool written;
-  };
-  std::vector<Range> ranges;
-  ranges.reserve((size_t)n * (out ? 2 : 1) + 1);
-  auto take = [&](const mt_tensor* t, bool written) {
-    const uintptr_t lo = (uintptr_t)t->data;
-    if (const int64_t count = numel(t)) ranges.push_back({lo, lo + (uintptr_t)count * elem_size(t->dtype), written});
-  };
-  for (int32_t i = 0; i < n; ++i) take(&grads[i], !out);
-  for (int32_t i = 0; out && i < n; ++i) take(&out[i], true);
-  if (norm) take(norm, true);
-  auto before = [](const Range& a, const Range& b) { return a.lo < b.lo; };
-  if (!std::is_sorted(ranges.begin(), ranges.end(), before)) std::sort(ranges.begin(), ranges.end(), before);
-  uintptr_t far = 0, far_written = 0;  // ends of what came before: of all, of what is written
-  for (const Range& r : ranges) {
-    if (r.lo < far_written || (r.written && r.lo < far))
-      return fail(MT_ERR_ALIAS, "mt_clip_grad_norm: a tensor that is written overlaps another");
-    far = std::max(far, r.hi);
-    if (r.written) far_written = std::max(far_written, r.hi);
-  }
+  if (out)
+    for (const ClipItem& t : items) take(t.out, t.numel, true);
+  if (any_written_overlaps(ranges)) return fail(MT_ERR_ALIAS, "mt_clip_grad_norm: a tensor that is written overlaps another");
   if ((s = check_workspace(ws, ws_bytes, need, "mt_clip_grad_norm"))) return s;
   mt::ClipBatch b;
-  auto pack = [&](int32_t first, int32_t end, int32_t held, int64_t chunks) {
-    b.n = held;
-    b.in_place = !out;
-    b.chunks = (int32_t)chunks;
-    uint32_t* starts = (uint32_t*)b.starts();
-    uint32_t at = 0;
-    int k = 0;
-    for (int32_t i = first; i < end; ++i) {
-      const int64_t count = numel(&grads[i]);
-      if (count == 0) continue;
-      const int kind = (grads[i].dtype == MT_BF16 ? mt::kClipSourceBf16 : 0) |
-                       ((out ? out[i] : grads[i]).dtype == MT_BF16 ? mt::kClipDestBf16 : 0);
-      b.w[k] = mt::ClipBatch::source(grads[i].data, kind, count);
-      if (out) b.w[held + k] = (uint64_t)(uintptr_t)out[i].data;
-      starts[k++] = at;
-      at += (uint32_t)cdiv(count, mt::kClipChunk);
-    }
-  };
   double* part = (double*)ws;
   float* to = norm ? (float*)norm->data : nullptr;
   (void)hipGetLastError();
-  if (parts == 0) {
+  if (items.empty()) {
     if (!to) return MT_OK;
     b.n = b.chunks = 0;
     b.in_place = 1;
     return hip_status(mt::clip_scale(b, part, 0, max_norm, to, 1, stream));
   }
-  size_t at = 0;
-  s = each_batch(!out, [&](int32_t first, int32_t end, int32_t held, int64_t chunks) {
-    pack(first, end, held, chunks);
+  int64_t chunks;
+  size_t at = 0, end = 0;
+  for (size_t first = 0; first < items.size(); first = end) {
+    end = clip_batch(items, first, !out, &chunks);
+    clip_pack(items, first, end, chunks, !out, &b);
     const int blocks = mt::clip_blocks(chunks);
+    if ((s = hip_status(mt::clip_norm(b, part + at, blocks, stream)))) return s;
     at += blocks;
-    return hip_status(mt::clip_norm(b, part + at - blocks, blocks, stream));
-  });
-  if (s) return s;
-  return each_batch(!out, [&](int32_t first, int32_t end, int32_t held, int64_t chunks) {
-    if (held < n) pack(first, end, held, chunks);  // else it still holds them
-    float* once = to;
+  }
+  for (size_t first = 0; first < items.size(); first = end) {
+    end = clip_batch(items, first, !out, &chunks);
+    if (end - first < items.size()) clip_pack(items, first, end, chunks, !out, &b);  // else it still holds them
+    if ((s = hip_status(mt::clip_scale(b, part, (int)parts, max_norm, to, mt::clip_blocks(chunks), stream)))) return s;
     to = nullptr;
-    return hip_status(mt::clip_scale(b, part, (int)parts, max_norm, once, mt::clip_blocks(chunks), stream));
-  });
+  }
+  return MT_OK;
 }
 
 }  // namespace mt::host
