@@ -565,11 +565,12 @@ mt_status mt_cross_entropy_workspace(const mt_tensor* logits, const mt_tensor* t
  * grads: n tensors, f32 or bf16 each, contiguous, any rank. out: n tensors of
  * their shapes, f32 or bf16 each, contiguous, overlapping nothing; or NULL: the
  * gradients are scaled in place (and not written where nothing is clipped).
- * norm: f32, one element, or NULL. Squares are formed and added in 64 bits. A
+ * norm: f32, one element, or NULL. Squares are formed and added, and products with the
+ * factor formed, in 64 bits: a result is rounded once. A
  * norm that is not finite clips nothing: the caller reads it from norm.
  * ws: REQUIRED (mt_clip_grad_norm_workspace): partial sums.
  */
-mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, double max_norm, const mt_tensor* out,
                             const mt_tensor* norm, void* ws, size_t ws_bytes, void* stream);
 mt_status mt_clip_grad_norm_workspace(int32_t n, const mt_tensor* grads, size_t* bytes);
 

@@ -105,7 +105,7 @@ lib.mt_layer_norm_bwd.argtypes = [_P, _P, _P, _f, _P, _P, _P, _u32, _vp, _sz, _v
 lib.mt_layer_norm_bwd_workspace.argtypes = [_P] * 6 + [ctypes.POINTER(_sz)]
 lib.mt_cross_entropy.argtypes = [_P] * 5 + [_vp, _sz, _vp]
 lib.mt_cross_entropy_workspace.argtypes = [_P, _P, ctypes.POINTER(_sz)]
-lib.mt_clip_grad_norm.argtypes = [_i32, _P, _f, _P, _P, _vp, _sz, _vp]
+lib.mt_clip_grad_norm.argtypes = [_i32, _P, ctypes.c_double, _P, _P, _vp, _sz, _vp]
 lib.mt_clip_grad_norm_workspace.argtypes = [_i32, _P, ctypes.POINTER(_sz)]
 lib.mt_workspace_bytes.argtypes = [ctypes.c_int32, ctypes.POINTER(_P), ctypes.c_int32]
 lib.mt_debug_set.argtypes = [ctypes.c_char_p, ctypes.c_int64]

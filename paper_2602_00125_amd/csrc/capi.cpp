@@ -1451,7 +1451,7 @@ mt_status mt_cross_entropy_workspace(const mt_tensor* logits, const mt_tensor* t
   }
 }
 
-mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, double max_norm, const mt_tensor* out,
                             const mt_tensor* norm, void* ws, size_t ws_bytes, void* stream) {
   try {
     return clip_grad_norm_impl(n, grads, max_norm, out, norm, ws, ws_bytes, (hipStream_t)stream, nullptr);
@@ -1463,7 +1463,7 @@ mt_status mt_clip_grad_norm(int32_t n, const mt_tensor* grads, float max_norm, c
 mt_status mt_clip_grad_norm_workspace(int32_t n, const mt_tensor* grads, size_t* bytes) {
   try {
     if (!bytes) return fail(MT_ERR_NULL, "bytes is null");
-    return clip_grad_norm_impl(n, grads, 0.f, nullptr, nullptr, nullptr, 0, nullptr, bytes);
+    return clip_grad_norm_impl(n, grads, 0.0, nullptr, nullptr, nullptr, 0, nullptr, bytes);
   } catch (...) {
     return fail(MT_ERR_INVALID, "internal error");
   }

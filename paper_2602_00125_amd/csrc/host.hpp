@@ -98,7 +98,7 @@ mt_status layer_norm_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
 mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, const mt_tensor* loss,
                              const mt_tensor* losses, const mt_tensor* dlogits, void* ws, size_t ws_bytes,
                              hipStream_t stream, size_t* ws_query);
-mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, double max_norm, const mt_tensor* out,
                               const mt_tensor* norm, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query);
 
 }  // namespace mt::host

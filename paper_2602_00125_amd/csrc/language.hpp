@@ -114,7 +114,7 @@ struct ClipBatch {
 int clip_blocks(int64_t chunks);
 hipError_t clip_norm(const ClipBatch& b, double* part, int blocks, hipStream_t stream);
 // norm = sqrt of the parts' sum (where not NULL); dst = src min(1, max_norm / norm).
-hipError_t clip_scale(const ClipBatch& b, const double* part, int parts, float max_norm, float* norm, int blocks,
+hipError_t clip_scale(const ClipBatch& b, const double* part, int parts, double max_norm, float* norm, int blocks,
                       hipStream_t stream);
 
 }  // namespace mt

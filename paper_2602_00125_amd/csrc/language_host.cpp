@@ -420,7 +420,7 @@ bool any_written_overlaps(std::vector<Range>& r) {
 
 }  // namespace
 
-mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm, const mt_tensor* out,
+mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, double max_norm, const mt_tensor* out,
                               const mt_tensor* norm, void* ws, size_t ws_bytes, hipStream_t stream, size_t* ws_query) {
   if (n < 0) return fail(MT_ERR_INVALID, "mt_clip_grad_norm: negative tensor count");
   if (n > 0 && !grads) return fail(MT_ERR_NULL, "mt_clip_grad_norm: null array");
@@ -452,7 +452,7 @@ mt_status clip_grad_norm_impl(int32_t n, const mt_tensor* grads, float max_norm,
     *ws_query = need;
     return MT_OK;
   }
-  if (!(max_norm >= 0.f)) return fail(MT_ERR_INVALID, "mt_clip_grad_norm: max_norm must not be negative");
+  if (!(max_norm >= 0.0)) return fail(MT_ERR_INVALID, "mt_clip_grad_norm: max_norm must not be negative");
   if (norm) {
     if ((s = check_tensor(norm, "norm", 0, MT_MAX_DIMS))) return s;
     if (norm->dtype != MT_F32) return fail(MT_ERR_DTYPE, "norm must be f32");

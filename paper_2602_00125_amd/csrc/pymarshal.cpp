@@ -192,12 +192,13 @@ struct Args {
     if (ok) ok = as_i64(a[i], &v);
     return v;
   }
-  float f32(int i) {
-    if (!ok) return 0.f;
+  double f64(int i) {
+    if (!ok) return 0.0;
     const double v = PyFloat_AsDouble(a[i]);
     ok = v != -1.0 || !PyErr_Occurred();
-    return (float)v;
+    return v;
   }
+  float f32(int i) { return (float)f64(i); }
   struct Ws {
     void* p = nullptr;
     size_t n = 0;
@@ -503,7 +504,7 @@ FN(clip_grad_norm) {  // grads, out, max_norm, norm, ws, stream
   const bool in_place = a[1] == Py_None;
   const Lists t(a, in_place ? 1 : 2, &g);
   if (!t.ok) return nullptr;
-  const float most = g.f32(2);
+  const double most = g.f64(2);
   const mt_tensor* norm = g.tensor(3);
   const Args::Ws ws = g.ws(4);
   void* st = g.stream(5);

@@ -188,10 +188,10 @@ def cross_entropy(logits, targets, dtype):
 def clip(grads, max_norm, out_dtypes):
     """(norm, bound) and [(out, bound)]; squares and their sum in 64 bits are exact to 1e-12."""
     norm = sum((g.double().square().sum() for g in grads), torch.zeros((), dtype=torch.float64, device=DEV)).sqrt()
-    most = float(torch.tensor(max_norm, dtype=torch.float32))
-    f = min(1.0, most / float(norm)) if float(norm) > 0 else 1.0
+    f = min(1.0, max_norm / float(norm)) if float(norm) > 0 else 1.0
     outs = []
     for g, dt in zip(grads, out_dtypes):
         y = g.double() * f
-        outs.append((y, ((2 * U if f < 1 else 0.0) + (half(dt) if f < 1 or dt != g.dtype else 0.0) + 1e-12) * y.abs()))
+        # by way of fp32 where the result is bf16
+        outs.append((y, ((U if f < 1 else 0.0) + (half(dt) if f < 1 or dt != g.dtype else 0.0) + 1e-12) * y.abs()))
     return (norm.view(1), (U + 1e-12) * norm.view(1)), outs
