@@ -69,7 +69,7 @@ struct CrossEntropyParams {
   void* dz;  // or NULL
   vio::Index targets;
   float* row_loss;
-  const int32_t* counted;  // n, or NULL where nothing needs it
+  const int32_t* counted;  // n, or NULL where blocks count the rows themselves
   int64_t M, ldz, ldd;
   int32_t V;
 };
@@ -87,8 +87,7 @@ hipError_t cross_entropy_count(const vio::Index& targets, int64_t M, int64_t V, 
 // loss: written where f.few
 hipError_t cross_entropy_rows(const CrossEntropyParams& p, const CrossEntropyForm& f, bool z_bf16, bool d_bf16, float* loss,
                               hipStream_t stream);
-hipError_t cross_entropy_mean(const float* row_loss, int64_t M, double* part, const int32_t* counted, float* loss,
-                              hipStream_t stream);
+hipError_t cross_entropy_mean(const CrossEntropyParams& p, double* part, float* loss, hipStream_t stream);
 
 // The tensors of a launch, cut into chunks of kClipChunk values, 20 bytes a tensor
 // in a launch's arguments (12 where they are scaled in place):

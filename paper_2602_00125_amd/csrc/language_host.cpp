@@ -305,10 +305,8 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
   if ((s = check_apart({loss, losses, dlogits}, {logits, targets})) ||
       (s = check_workspace(ws, ws_bytes, need, "mt_cross_entropy")))
     return s;
-  int32_t* counted = (int32_t*)ws;
   void* part = (char*)ws + 256;
   p.V = (int32_t)V;
-  p.counted = counted;
   p.row_loss = losses && p.M ? (float*)losses->data : (float*)((char*)part + kCrossEntropyParts * sizeof(double));
   p.z = logits->data;
   p.ldz = row_pitch(logits);
@@ -323,20 +321,25 @@ mt_status cross_entropy_impl(const mt_tensor* logits, const mt_tensor* targets, 
     f.few = p.M * f.L <= 4096;
   } else {
     // 16 values a thread, of bf16 32 (8192 x 16384 fp32 189 us against 200 the other way, bf16 128 against
-    // 131); one block a CU where the rows of two would not stay in the caches (2048 x 131072 fp32 565 ->
-    // 493, 4096 x 65537 485 -> 460; 5336 x 50001 fp32 to bf16 355 -> 368, so not below 65536)
+    // 131). 1024 threads, one block a CU, where the rows of two would not stay in the caches (2048 x 131072
+    // fp32 565 -> 493, 4096 x 65537 485 -> 460; 5336 x 50001 fp32 to bf16 355 -> 368, so not below 65536) or
+    // where all rows have a CU (64 x 50001 20.5 -> 17.4); only past 32 values a thread: shorter rows' kernels
+    // take 512 threads at most
     while (f.threads < 512 && f.threads * (zb ? 32 : 16) < V) f.threads *= 2;
-    if (V > 65536) f.threads = 1024;
+    if (V > 65536 || (V > 32768 && p.M <= 256)) f.threads = 1024;
     f.values = (int32_t)cdiv(V, f.threads);
   }
   float* to = loss ? (float*)loss->data : nullptr;
   (void)hipGetLastError();
-  if (!f.few && (loss || dlogits) &&
-      (s = hip_status(mt::cross_entropy_count(p.targets, p.M, V, (int32_t*)part, counted, stream))))
+  // every block counts the rows itself where they read 2^18 classes in all
+  const int64_t blocks = f.L ? cdiv(p.M * f.L, 256) : p.M;
+  if (!f.few && blocks * p.M > (1 << 18)) p.counted = (int32_t*)ws;
+  if (p.counted && (loss || dlogits) &&
+      (s = hip_status(mt::cross_entropy_count(p.targets, p.M, V, (int32_t*)part, (int32_t*)ws, stream))))
     return s;
   if ((p.M > 0 || f.few) && (s = hip_status(mt::cross_entropy_rows(p, f, zb, db, to, stream)))) return s;
   if (f.few || !loss) return MT_OK;
-  return hip_status(mt::cross_entropy_mean(p.row_loss, p.M, (double*)part, counted, to, stream));
+  return hip_status(mt::cross_entropy_mean(p, (double*)part, to, stream));
 }
 
 // ----------------------------------------------------------------- clipping
