@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256) void fwd_kernel(const EmbeddingParams p, int G
   }
 }
 
-constexpr int64_t kManyBlocks = 4096;
+constexpr int64_t kManyBlocks = 4096;  // a lookup of so many keeps four rows in flight a lane
 constexpr int kGroupWaves = 16, kGroupThreads = 64 * kGroupWaves;
 constexpr int kAhead = 16;  // ids in flight a lane
 
@@ -228,7 +228,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, i
 }
 
 // A block for each chunk whose last run began in it and goes on. Its 256 / G
-// groups of lanes take the later pieces in turn; their sums meet in LDS.
+// groups of lanes take equal shares of the later pieces; their sums meet in LDS.
 __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, int G_shift, int tiles) {
   constexpr int VEC = 4, U = 8;
   __shared__ float sums[256 * VEC];

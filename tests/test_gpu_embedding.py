@@ -142,6 +142,17 @@ def test_the_order_of_a_token_s_rows_is_theirs():
         assert (dt[first + 1].cpu() == want).all()
 
 
+@pytest.mark.parametrize("M,V,D", [(50, 30, 21), (3000, 400, 70)])
+def test_gradient_is_the_lookup_s_adjoint(M, V, D):
+    """<dy, lookup(H)> = <gradient(dy), H> for every H; of small whole numbers both are exact."""
+    ids = tokens((M,), V, "padded", 21)
+    H, dy = (integers(s, -8, 9, 22 + i).float() for i, s in enumerate(((V, D), (M, D))))
+    out, dt = torch.empty((M, D), device=DEV), torch.empty((V, D), device=DEV)
+    b.embedding_fwd(ids, H, out, scale=2.0)
+    run_bwd(ids, dy, dt, 2.0)
+    assert (out.double() * dy.double()).sum() == (dt.double() * H.double()).sum() != 0
+
+
 def test_nothing_to_look_up():
     table = draw((5, 6), "f32", 15)
     none = torch.empty((0,), dtype=torch.int32, device=DEV)

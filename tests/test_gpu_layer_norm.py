@@ -160,6 +160,27 @@ def test_reruns_give_the_same_bits(M, C):
         close(name, got, *want)
 
 
+def test_gradients_against_differences():
+    """Of sum(y G) in 64 bits, by central differences: off by h^2 = 1e-10 times a third derivative, which for rows whose
+    deviation is about 1 is below 100, and by 2^-53 of the sum over h."""
+    x, g, w = draw((3, 7), "f32", 23), draw((3, 7), "f32", 24), weights(7, 25)[0]
+    bias = weights(7, 26)[1]
+    dx, dw, db = new(3, 7, "f32"), new(1, 7, "f32")[0], new(1, 7, "f32")[0]
+    run_bwd(x, w, g, dx, dw, db)
+    want = layer_norm_grad(x, w, g, EPS)
+    f = lambda x, w, bias: float((layer_norm(x, w, bias, EPS, torch.float32)[0] * g.double()).sum())
+    h = 1e-5
+    args = [x.double(), w.double(), bias.double()]
+    for k, (got, (_, bound)) in enumerate(zip((dx, dw, db), want)):
+        for i in range(got.numel()):
+            ends = []
+            for s in (h, -h):
+                moved = [a.clone() for a in args]
+                moved[k].view(-1)[i] += s
+                ends.append(f(*moved))
+            assert abs((ends[0] - ends[1]) / (2 * h) - float(got.flatten()[i])) < 1e-8 + 1.05 * float(bound.flatten()[i]), (k, i)
+
+
 def test_past_2_31_values():
     M, C = 140000, 16384
     x = torch.zeros((M, C), dtype=torch.bfloat16, device=DEV)
