@@ -145,6 +145,15 @@ def test_many_rows(M, V):
     assert all(torch.equal(a, c) for a, c in zip(got, again))
 
 
+@pytest.mark.parametrize("x,y", TYPES)
+@pytest.mark.parametrize("V", [64, 65, 1024, 1025, 8192, 8193, 16384, 16385, 32768, 32769])
+def test_where_the_forms_meet(V, x, y):
+    """At the numbers of rows and logits where another way of sharing the work out begins."""
+    for M in (256, 257, 512, 513):
+        z, t = draw((M, V), x, 30, 2.0), targets(M, V, True, 31)
+        compare(run(z, t, DT[y]), cross_entropy(z, t, DT[y]))
+
+
 @pytest.mark.parametrize("V,L", [(1030, 1), (3, 256)])
 def test_more_rows_than_blocks(V, L):
     """More rows than the blocks of a launch (2^20, of L rows each) hold at a time."""
