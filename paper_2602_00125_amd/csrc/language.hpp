@@ -53,7 +53,7 @@ struct LayerNormParams {
   int64_t M, ldx, ldd, ldo;
   int32_t C, L;  // L lanes a row: a power of two up to a wave, or whole waves
   int32_t accumulate;
-  float eps, C_f;  // C as a float: means are quotients, so that rows of one value have exact ones
+  float eps, C_f, inv_C;  // C as a float and 1 / C: a quotient where the mean of like values must be exact
 };
 // nv: groups of values (8 where a side is bf16, else 4) a lane holds, 16 values
 // at most; threads of a block, blocks.

@@ -174,6 +174,7 @@ mt_status check_norm(const mt_tensor* x, const mt_tensor* w, float eps, mt::Laye
   p->ldx = row_pitch(x);
   p->eps = eps;
   p->C_f = (float)C;
+  p->inv_C = 1.f / (float)C;
   return MT_OK;
 }
 
@@ -224,7 +225,10 @@ mt_status layer_norm_fwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
   // us, 21845 x 1536 35 -> 28, 8192 x 4096 32 -> 29; by five waves 13107 x 2560 28 -> 32)
   const int waves = (int)cdiv(p.C, 512);
   const int values = p.C <= 512 || waves == 3 || waves == 4 || waves == 8 ? 8 : 16;
-  const NormForm f = norm_form(&p, vector_of({x, y}), values, 256, 2048);
+  // eight blocks a CU, or seven of the forms of 512 to 1024 columns, whose registers have room for no more: of eight the
+  // last would run alone (32768 x 1024 bf16 31 -> 26 us, 32768 x 1023 33 -> 30)
+  const int blocks = p.C > 512 && p.C <= 1024 ? 7 * 256 : 8 * 256;
+  const NormForm f = norm_form(&p, vector_of({x, y}), values, 256, blocks);
   (void)hipGetLastError();
   return hip_status(mt::layer_norm_fwd(p, x->dtype == MT_BF16, y->dtype == MT_BF16, f.nv, f.threads, f.blocks, stream));
 }

@@ -6,9 +6,18 @@
 // A row is read once and held in registers by L lanes (a power of two up to a
 // wave, or whole waves), so that the variance is a mean of squared deviations and not a
 // difference of large numbers, and the gradient needs no saved statistics: it
-// takes them again from the row that it reads anyway. Bound: HBM (16384 x 1024 fp32
-// to bf16 18.9 us, 5.3 TB/s; gradient of 8192 x 8192 fp32 170 us, 4.7 TB/s; bf16
-// gradients, half the bytes, by the vector instructions too: 32768 x 1024 47 us, 4.3).
+// takes them again from the row that it reads anyway.
+//
+// The mean is taken twice, of the values and of what is left of them. The first is
+// off by some ulps of itself, which rows of small deviations would show (16384 times
+// 12345.678 had an n of 0.5); the second by some ulps of the deviations. The second
+// is a quotient: what the first leaves of like values has few digits, the sum and the
+// quotient are exact, and a row of one value has deviations of 0. The pass costs up
+// to 3% of the gradient's time and up to 8% of the forward's (43690 x 768 bf16).
+//
+// Bound: HBM (16384 x 1024 fp32 to bf16 18.9 us, 5.3 TB/s; gradient of 8192 x 8192
+// fp32 169 us, 4.8 TB/s; bf16 gradients, half the bytes, by the vector instructions
+// too: 32768 x 1024 49 us, 4.1).
 //
 // dw, db: a lane keeps the sums of its columns over the rows that it meets, a
 // block adds its groups' in order, a second launch the blocks' in order, both in
@@ -37,10 +46,9 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int L, int grp, float (*
       for (int i = 0; i < N; ++i) red[i][wave] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      float s = 0.f;
-      for (int w = 0; w < W; ++w) s += red[i][first + w];
-      v[i] = s;
+    for (int i = 0; i < N; ++i) {  // 16 lanes read a wave's sum each, at once (one after another 2730 x 12288 bf16 37 us, so 36)
+      const int w = threadIdx.x & 15;
+      v[i] = lanes_sum(w < W ? red[i][first + w] : 0.f, 16);
     }
   }
 }
@@ -68,9 +76,32 @@ struct Columns {
   }
 };
 
+// The row's values less their mean, and less the mean of that. (contract(off): a
+// mean is rounded before it is subtracted.)
+template <bool WIDE, bool WHOLE, int NV, int VEC>
+__device__ __forceinline__ void center(float (&x)[NV][VEC], const LayerNormParams& p, int l, int grp, float (*red)[16]) {
+#pragma clang fp contract(off)
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const Columns<VEC, WHOLE> c(l, k, p);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
+    }
+    row_sums<WIDE, 1>(s, p.L, grp, red + pass);
+    const float mean = pass ? s[0] / p.C_f : s[0] * p.inv_C;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[k][e] -= mean;
+  }
+}
+
 template <bool XB, bool YB, int VEC, int NV, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
-  __shared__ float red[2][16];
+  __shared__ float red[3][16];
   const int grp = threadIdx.x / (unsigned)p.L, l = threadIdx.x - grp * p.L, rows = blockDim.x / (unsigned)p.L;
   float w[NV][VEC], b[NV][VEC];
 #pragma unroll
@@ -88,28 +119,18 @@ __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
   for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
     const int64_t m = m0 + grp;
     const bool on = m < p.M;
-    float x[NV][VEC], s[1] = {0.f}, q[1] = {0.f};
+    float x[NV][VEC], q[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) Columns<VEC, WHOLE>(l, k, p).template load<XB>(p.x, m * p.ldx, on, x[k]);
+    center<WIDE, WHOLE>(x, p, l, grp, red);
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
+      for (int e = 0; e < VEC; ++e) q[0] = fmaf(c.has(e) ? x[k][e] : 0.f, x[k][e], q[0]);
     }
-    row_sums<WIDE, 1>(s, p.L, grp, red);
-    const float mu = s[0] / p.C_f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const Columns<VEC, WHOLE> c(l, k, p);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        x[k][e] -= mu;
-        q[0] = fmaf(c.has(e) ? x[k][e] : 0.f, x[k][e], q[0]);
-      }
-    }
-    row_sums<WIDE, 1>(q, p.L, grp, red + 1);
-    const float r = 1.f / sqrtf(q[0] / p.C_f + p.eps);
+    row_sums<WIDE, 1>(q, p.L, grp, red + 2);
+    const float r = 1.f / sqrtf(fmaf(q[0], p.inv_C, p.eps));
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const Columns<VEC, WHOLE> c(l, k, p);
@@ -122,7 +143,7 @@ __global__ __launch_bounds__(1024) void fwd_kernel(const LayerNormParams p) {
 
 template <bool XB, bool YB, int VEC, int NV, bool WIDE, bool WHOLE>
 __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
-  __shared__ float red[4][16];
+  __shared__ float red[5][16];
   __shared__ float cols[1024 * 16];  // [group][C], where a block has several groups
   const int grp = threadIdx.x / (unsigned)p.L, l = threadIdx.x - grp * p.L, rows = blockDim.x / (unsigned)p.L;
   float w[NV][VEC], dw[NV][VEC], db[NV][VEC];
@@ -138,28 +159,20 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
   for (int64_t m0 = (int64_t)blockIdx.x * rows; m0 < p.M; m0 += (int64_t)gridDim.x * rows) {
     const int64_t m = m0 + grp;
     const bool on = m < p.M;
-    float x[NV][VEC], g[NV][VEC], s[1] = {0.f}, t[3] = {0.f, 0.f, 0.f};
+    float x[NV][VEC], g[NV][VEC], t[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const Columns<VEC, WHOLE> c(l, k, p);
       c.template load<XB>(p.x, m * p.ldx, on, x[k]);
       c.template load<YB>(p.dy, m * p.ldd, on, g[k]);
     }
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const Columns<VEC, WHOLE> c(l, k, p);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) s[0] += c.has(e) ? x[k][e] : 0.f;
-    }
-    row_sums<WIDE, 1>(s, p.L, grp, red);
-    const float mu = s[0] / p.C_f;
+    center<WIDE, WHOLE>(x, p, l, grp, red);
     // squares of the deviations, sums of g and of g times the deviations
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
       const Columns<VEC, WHOLE> c(l, k, p);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        x[k][e] -= mu;
         const float d = c.has(e) ? x[k][e] : 0.f;
         const float gw = g[k][e] * w[k][e];
         t[0] = fmaf(d, d, t[0]);
@@ -167,9 +180,9 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
         t[2] = fmaf(d, gw, t[2]);
       }
     }
-    row_sums<WIDE, 3>(t, p.L, grp, red + 1);
-    const float r = 1.f / sqrtf(t[0] / p.C_f + p.eps);
-    const float mg = t[1] / p.C_f, mgn = t[2] * r / p.C_f;  // the means of g and of g n
+    row_sums<WIDE, 3>(t, p.L, grp, red + 2);
+    const float r = 1.f / sqrtf(fmaf(t[0], p.inv_C, p.eps));
+    const float mg = t[1] / p.C_f, mgn = t[2] * (r * p.inv_C);  // the means of g and of g n
     if (!on) continue;  // no barrier below
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
