@@ -498,7 +498,9 @@ mt_status mt_embedding_fwd(const mt_tensor* ids, const mt_tensor* table, float s
  *   dy [M, D] f32 or bf16; dtable [V, D] f32. Rows without a token become 0,
  *   or with MT_ACCUMULATE stay as they are and the others are added to. Rows
  *   of dy whose token is outside 0 .. V-1 are not read.
- *   Up to 2^26 tokens, V up to 2^24. Sums are fp32, in one order for given ids.
+ *   Up to 2^26 tokens, V up to 2^24. Sums have one order for given ids: the
+ *   rows of an id in fp32 where there are up to 2048 tokens, else in fp32 by
+ *   up to 64 rows and these sums in 64 bits.
  *   ws: REQUIRED (mt_embedding_bwd_workspace): the tokens sorted by id, and the
  *   partial sums of ids that many tokens share.
  */

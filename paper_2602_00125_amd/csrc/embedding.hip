@@ -20,7 +20,7 @@
 //    to a run that the chunk cuts goes to the workspace. Work is even whatever the
 //    ids are. Beside it, blocks clear the rows without a token.
 // 3. join_kernel. Where a run goes on past its first chunk, its pieces are added
-//    in order.
+//    in order, in 64 bits.
 //
 // 16384 tokens of 1024 fp32 values into 50001 rows: 73 us for 272 MB, of which the
 // first launch takes 9 (it waits for loads, LDS and its own order), the second 55
@@ -181,7 +181,9 @@ __device__ __forceinline__ void clear(const EmbeddingGradParams& p, int block, i
   }
 }
 
-template <bool BF>
+// Sum: what a run's rows are added in, fp32 where a chunk has up to kEmbedChunk of
+// them (in 64 bits three waves a SIMD would be left for four).
+template <bool BF, typename Sum>
 __global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, int G_shift, int tiles, int sum_blocks) {
   if ((int)blockIdx.x >= sum_blocks) {
     clear(p, blockIdx.x - sum_blocks, gridDim.x - sum_blocks, G_shift);
@@ -195,9 +197,9 @@ __global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, i
   if (i0 >= i1 || n <= 0) return;
   const int32_t before = i0 > 0 ? p.id[i0 - 1] : -1;
   bool cut = before == p.id[i0];  // the run began in an earlier chunk
-  float acc[VEC];
+  Sum acc[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+  for (int e = 0; e < VEC; ++e) acc[e] = 0;
   for (int64_t i = i0; i < i1; i += U) {  // a chunk is whole but for the last one's end, past which ids are -1
     int32_t id[U + 1], pos[U];
     float v[U][VEC], old[U][VEC];
@@ -217,21 +219,26 @@ __global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, i
       for (int e = 0; e < VEC; ++e) acc[e] += v[u][e];
       const bool ends = id[u] != id[u + 1];
       if (!ends && i + u < i1 - 1) continue;
-      if (cut) store_some<false, VEC>(p.head, c * p.D + d, n, acc);
-      else if (ends) put(p, id[u], d, n, acc, old[u]);
-      else store_some<false, VEC>(p.tail, c * p.D + d, n, acc);
+      float sum[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e] = (float)acc[e];
+      if (cut) store_some<false, VEC>(p.head, c * p.D + d, n, sum);
+      else if (ends) put(p, id[u], d, n, sum, old[u]);
+      else store_some<false, VEC>(p.tail, c * p.D + d, n, sum);
       cut = false;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+      for (int e = 0; e < VEC; ++e) acc[e] = 0;
     }
   }
 }
 
 // A block for each chunk whose last run began in it and goes on. Its 256 / G
-// groups of lanes take equal shares of the later pieces; their sums meet in LDS.
+// groups of lanes take equal shares of the later pieces; their sums meet in LDS. In
+// 64 bits: a frequent id has a piece in every chunk, and added in fp32 the like
+// rows of 2^24 tokens were off by 6e-4 of their sum.
 __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, int G_shift, int tiles) {
   constexpr int VEC = 4, U = 8;
-  __shared__ float sums[256 * VEC];
+  __shared__ double sums[256 * VEC];
   const int G = 1 << G_shift, groups = 256 >> G_shift, grp = threadIdx.x >> G_shift, lane = threadIdx.x & 63;
   const int tile = blockIdx.x % tiles;
   const int64_t c = blockIdx.x / tiles, i0 = c * p.chunk, i1 = i0 + p.chunk;
@@ -248,15 +255,24 @@ __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, 
     if (n < 64) break;
   }
   const int d = (tile * G + (threadIdx.x & (G - 1))) * VEC, n = (int)p.D - d;
-  float acc[VEC], old[VEC];
+  float first_piece[VEC], old[VEC];
   // a group takes a share of the pieces, one after another
   const int64_t share = (pieces + groups - 1) / groups, j1 = min((grp + 1) * share, pieces);
-  load_some<false, VEC>(p.tail, c * p.D + d, grp == 0 ? n : 0, 0.f, acc);
+  load_some<false, VEC>(p.tail, c * p.D + d, grp == 0 ? n : 0, 0.f, first_piece);
+  double acc[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) acc[e] = first_piece[e];
   load_old(p, id, d, grp == 0 ? n : 0, old);
   for (int64_t j = grp * share; j < j1; j += U) {
     float v[U][VEC];
 #pragma unroll
     for (int u = 0; u < U; ++u) load_some<false, VEC>(p.head, (c + 1 + j + u) * p.D + d, j + u < j1 ? n : 0, 0.f, v[u]);
+    // all loads first: else a value is widened behind its own load, which waits for it (65536 tokens of 64 columns, 16
+    // ids 68 -> 97 us)
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) __asm__ __volatile__("" : "+v"(v[u][e]));
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -269,7 +285,10 @@ __global__ __launch_bounds__(256) void join_kernel(const EmbeddingGradParams p, 
   for (int g = 1; g < groups; ++g)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] += sums[(g * G + threadIdx.x) * VEC + e];
-  put(p, id, d, n, acc, old);
+  float sum[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) sum[e] = (float)acc[e];
+  put(p, id, d, n, sum, old);
 }
 
 constexpr int kFewThreads = 512;
@@ -387,9 +406,9 @@ EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D) {
   EmbeddingGradForm f;
   f.shift = embedding::lanes_shift(D, 4, 6);
   f.tiles = (int32_t)((D + (4 << f.shift) - 1) >> (f.shift + 2));
-  // 4096 waves, then chunks of up to 64 tokens; longer ones for what a launch holds
+  // 4096 waves, then chunks of up to kEmbedChunk tokens; longer ones for what a launch holds
   auto items = [&] { return (M + f.chunk - 1) / f.chunk * f.tiles; };
-  for (f.chunk = 8; items() > (int64_t)4096 * (64 >> f.shift) && (f.chunk < 64 || items() > 1 << 22);) f.chunk *= 2;
+  for (f.chunk = 8; items() > (int64_t)4096 * (64 >> f.shift) && (f.chunk < kEmbedChunk || items() > 1 << 22);) f.chunk *= 2;
   f.chunks = (int32_t)((M + f.chunk - 1) / f.chunk);
   return f;
 }
@@ -417,8 +436,9 @@ hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || sums + clears == 0) return e;
   const dim3 grid((unsigned)(sums + clears));
-  if (bf16) sum_kernel<true><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, sums);
-  else sum_kernel<false><<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, sums);
+  auto sum = [&](auto kernel) { kernel<<<grid, 256, 0, stream>>>(p, f.shift, f.tiles, sums); };
+  if (f.chunk <= kEmbedChunk) bf16 ? sum(sum_kernel<true, float>) : sum(sum_kernel<false, float>);
+  else bf16 ? sum(sum_kernel<true, double>) : sum(sum_kernel<false, double>);
   if ((e = hipGetLastError()) != hipSuccess || f.chunks < 2) return e;
   join_kernel<<<dim3((unsigned)(f.chunks * f.tiles)), 256, 0, stream>>>(p, f.shift, f.tiles);
   return hipGetLastError();

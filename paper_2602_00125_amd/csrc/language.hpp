@@ -36,6 +36,7 @@ struct EmbeddingGradParams {
   float *head, *tail;          // [chunks][D]: a run that began before the chunk; one that ends after it
 };
 constexpr int kEmbedBucketIds = 1024;  // ids of a bucket, at most
+constexpr int kEmbedChunk = 64;        // rows of an id that are added in fp32, at most
 constexpr int kEmbedFewTokens = 2048, kEmbedFewClear = 16384;  // tokens of a single launch, rows that a block of it clears, at most
 // How the sums are shared out: 2^shift lanes a row or tile of it, chunks of tokens.
 struct EmbeddingGradForm {
