@@ -118,7 +118,8 @@ __device__ __forceinline__ void put(void* dr, int e0, int n, int32_t t, float c,
 // A block a row. A thread holds the first NV groups of VEC values it meets; of
 // the rest (REST: the held part is whole) it keeps the maximum and the sum so
 // far, raised together, and reads them again for the gradient, 16 values at a
-// time, from the caches.
+// time, from the caches. Sixteens are added in 64 bits: a thread meets 16384 values
+// of a row of 2^24, and a sum in fp32 was off by 2e-4 of like ones.
 template <bool XB, bool YB, int VEC, int NV, bool REST>
 __global__ __launch_bounds__(REST ? 1024 : 512, REST ? 4 : 6) void row_kernel(const CrossEntropyParams p) {
   __shared__ float red[2][16];
@@ -140,6 +141,7 @@ __global__ __launch_bounds__(REST ? 1024 : 512, REST ? 4 : 6) void row_kernel(co
     const float zt = load_one<XB>(zr, t);
     const int n = dr ? counted(p, counts) : 1;
     constexpr int U = 16 / VEC;  // groups of the rest in flight
+    double sum_rest = 0.0;
     if constexpr (REST) {
       for (int e0 = first + NV * step; e0 < p.V; e0 += U * step) {
         float v[U][VEC];
@@ -151,14 +153,16 @@ __global__ __launch_bounds__(REST ? 1024 : 512, REST ? 4 : 6) void row_kernel(co
 #pragma unroll
           for (int e = 0; e < VEC; ++e) most = fmaxf(most, v[u][e]);
         if (most > top) {
-          sum *= exp_of<XB>(top - most);
+          sum_rest *= exp_of<XB>(top - most);
           top = most;
         }
         const float from = top == -INFINITY ? 0.f : top;  // nothing but -inf so far adds nothing
+        float some = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) sum += exp_of<XB>(v[u][e] - from);
+          for (int e = 0; e < VEC; ++e) some += exp_of<XB>(v[u][e] - from);
+        sum_rest += some;
       }
     }
     const float rest = top;  // of the rest
@@ -168,7 +172,7 @@ __global__ __launch_bounds__(REST ? 1024 : 512, REST ? 4 : 6) void row_kernel(co
       for (int e = 0; e < VEC; ++e) top = fmaxf(top, z[k][e]);
     top = block_max(top, red[0]);
     // a rest of nothing but -inf adds nothing, unless there was a NaN
-    if (REST && rest > -INFINITY) sum *= exp_of<XB>(rest - top);
+    if constexpr (REST) sum = (float)(rest > -INFINITY ? sum_rest * exp_of<XB>(rest - top) : sum_rest);
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
