@@ -527,7 +527,8 @@ mt_status mt_layer_norm_fwd(const mt_tensor* x, const mt_tensor* w, const mt_ten
  *   dx = r (g - mean g - n mean(g n));   dw = sum over rows of dy n;
  *   db = sum over rows of dy
  *   dy [M, C] f32 or bf16; dx [M, C] of dy's type; dw, db [C] f32; outputs may
- *   be NULL (not all). flags: MT_ACCUMULATE, for all three.
+ *   be NULL (not all). flags: MT_ACCUMULATE, for all three. Sums over rows are
+ *   fp32 over up to 128 of them, and these in 64 bits.
  *   ws: required for dw and db (mt_layer_norm_bwd_workspace): partial sums.
  */
 mt_status mt_layer_norm_bwd(const mt_tensor* x, const mt_tensor* w, const mt_tensor* dy, float eps,

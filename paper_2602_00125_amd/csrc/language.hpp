@@ -46,6 +46,7 @@ EmbeddingGradForm embedding_grad_form(int64_t M, int64_t D);
 hipError_t embedding_bwd(const EmbeddingGradParams& p, const EmbeddingGradForm& f, bool bf16, hipStream_t stream);
 
 constexpr int kLayerNormMaxC = 16384;
+constexpr int kLayerNormLaneRows = 128;  // rows whose dy and dy n a lane adds in fp32, at most
 struct LayerNormParams {
   const void *x, *dy;
   const float *w, *b;
@@ -62,7 +63,9 @@ hipError_t layer_norm_fwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, in
                           hipStream_t stream);
 hipError_t layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, int nv, int threads, int blocks,
                           hipStream_t stream);
-hipError_t layer_norm_finish(const float* part, int parts, int C, float* dw, float* db, bool add, hipStream_t stream);
+// dw, db (+)= the sum of the parts and, where not NULL, of from; to: receives it instead ([2][C]).
+hipError_t layer_norm_finish(const float* part, int parts, int C, const double* from, double* to, float* dw, float* db, bool add,
+                             hipStream_t stream);
 
 // Cross-entropy: row_loss[m] = lse_m - z[m][t], dz = (softmax - onehot) / n.
 struct CrossEntropyParams {

@@ -21,7 +21,9 @@
 //
 // dw, db: a lane keeps the sums of its columns over the rows that it meets, a
 // block adds its groups' in order, a second launch the blocks' in order, both in
-// 64 bits (with 32 the sums of 3506 x 64 were off by 2.2e-7 of their norm).
+// 64 bits (with 32 the sums of 3506 x 64 were off by 2.2e-7 of their norm). A lane
+// meets kLayerNormLaneRows rows at most: more rows take several launches, whose parts
+// the last one adds (of 4096 like rows a lane the sums were off by 4e-5).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -245,8 +247,10 @@ __global__ __launch_bounds__(1024) void bwd_kernel(const LayerNormParams p) {
 }
 
 // dw, db (+)= the blocks' parts, in order within each of 64 interleaved shares,
-// then over the shares; a block covers 16 of the 2 C columns.
-__global__ __launch_bounds__(1024) void finish_kernel(const float* part, int parts, int C, float* dw, float* db, int add) {
+// then over the shares; a block covers 16 of the 2 C columns. from: added to that
+// (or NULL); to: receives the sums in dw's and db's place.
+__global__ __launch_bounds__(1024) void finish_kernel(const float* part, int parts, int C, const double* from, double* to, float* dw,
+                                                      float* db, int add) {
   __shared__ double sums[64][17];
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), share = threadIdx.x >> 4;
   double s = 0.0;
@@ -257,9 +261,13 @@ __global__ __launch_bounds__(1024) void finish_kernel(const float* part, int par
   sums[share][threadIdx.x & 15] = s;
   __syncthreads();
   if (share || c >= 2 * C) return;
-  s = 0.0;
+  s = from ? from[c] : 0.0;
 #pragma unroll 16
   for (int i = 0; i < 64; ++i) s += sums[i][threadIdx.x];
+  if (to) {
+    to[c] = s;
+    return;
+  }
   float* out = c < C ? dw : db;
   if (!out) return;
   out += c < C ? c : c - C;
@@ -319,8 +327,9 @@ hipError_t layer_norm_bwd(const LayerNormParams& p, bool x_bf16, bool y_bf16, in
   });
 }
 
-hipError_t layer_norm_finish(const float* part, int parts, int C, float* dw, float* db, bool add, hipStream_t stream) {
-  layernorm::finish_kernel<<<dim3((unsigned)((2 * C + 15) / 16)), 1024, 0, stream>>>(part, parts, C, dw, db, add);
+hipError_t layer_norm_finish(const float* part, int parts, int C, const double* from, double* to, float* dw, float* db, bool add,
+                             hipStream_t stream) {
+  layernorm::finish_kernel<<<dim3((unsigned)((2 * C + 15) / 16)), 1024, 0, stream>>>(part, parts, C, from, to, dw, db, add);
   return hipGetLastError();
 }
 
