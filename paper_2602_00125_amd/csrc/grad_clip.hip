@@ -94,8 +94,8 @@ __global__ __launch_bounds__(256) void scale_kernel(const ClipBatch b, const dou
   for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
   const double norm = sqrt(block_sum(sum, red));
   if (out_norm && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = (float)norm;
-  // a norm that is not finite clips nothing
-  const bool clips = norm > max_norm && norm < (double)INFINITY;
+  // a norm that is not finite, as the caller reads it, clips nothing
+  const bool clips = norm > max_norm && (float)norm < INFINITY;
   if (!clips && b.in_place) return;
   const double f = clips ? max_norm / norm : 1.0;
   for (int c = b.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
