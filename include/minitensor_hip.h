@@ -569,7 +569,7 @@ mt_status mt_cross_entropy_workspace(const mt_tensor* logits, const mt_tensor* t
  * their shapes, f32 or bf16 each, contiguous, overlapping nothing; or NULL: the
  * gradients are scaled in place (and not written where nothing is clipped).
  * norm: f32, one element, or NULL. Squares are formed and added, and products with the
- * factor formed, in 64 bits: a result is rounded once. A
+ * factor formed, in 64 bits: a result is rounded once, to its type. A
  * norm that is not finite in fp32 clips nothing: the caller reads it from norm.
  * ws: REQUIRED (mt_clip_grad_norm_workspace): partial sums.
  */

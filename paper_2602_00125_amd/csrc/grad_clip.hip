@@ -4,7 +4,8 @@
 //
 // Squares are formed and added in 64 bits: no finite gradient overflows or
 // vanishes in them, and the sum of hundreds of millions of values keeps its
-// digits. So is the factor, and a result is rounded once. Bound: HBM (vector instructions 11% busy).
+// digits. So is the factor, and a result is rounded once, to bf16 too. Bound: HBM
+// (vector instructions 11% busy).
 //
 // Two launches for each 188 tensors, or 313 in place. norm_kernel: blocks take the
 // chunks of the tensors in turn and write a partial sum each. scale_kernel: every
@@ -59,6 +60,14 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   return red[0];
 }
 
+// v cut off to fp32, the last bit set where that is not v: what is rounded to bf16
+// from there is v itself (by way of the nearest fp32 value it would be rounded twice).
+__device__ __forceinline__ float cut_odd(double v) {
+  const float f = (float)v;
+  const uint32_t u = __float_as_uint(f) - (fabs((double)f) > fabs(v));
+  return __uint_as_float((double)f != v ? u | 1u : u);
+}
+
 constexpr int kPer = kClipChunk / 256;  // values a thread of a chunk
 
 // f(i, n, values): the thread's values of a chunk by eights, the first n of which
@@ -103,10 +112,15 @@ __global__ __launch_bounds__(256) void scale_kernel(const ClipBatch b, const dou
     const Chunk k = chunk_of(b, t, c);
     void* dst = b.in_place ? k.src : address(b.w[b.n + t]);
     auto put = [&](int64_t i, int n, float (&v)[8]) {
+      if (k.kind & kClipDestBf16) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = (float)(v[e] * f);
-      if (k.kind & kClipDestBf16) store_some<true, 8>(dst, i, n, v);
-      else store_some<false, 8>(dst, i, n, v);
+        for (int e = 0; e < 8; ++e) v[e] = cut_odd(v[e] * f);
+        store_some<true, 8>(dst, i, n, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)(v[e] * f);
+        store_some<false, 8>(dst, i, n, v);
+      }
     };
     if (k.kind & kClipSourceBf16) values<true>(k, put);
     else values<false>(k, put);
