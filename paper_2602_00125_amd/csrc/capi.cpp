@@ -42,6 +42,9 @@ mt_status fail(mt_status s, const std::string& msg) {
   return s;
 }
 
+// a tensor's, at most: their bytes fit 64 bits (sizes are a caller's numbers)
+constexpr int64_t kMostValues = (int64_t)1 << 60;
+
 size_t elem_size(int32_t dt) { return dt == MT_BF16 ? 2 : 4; }
 
 mt_status check_tensor(const mt_tensor* t, const char* name, int min_nd, int max_nd) {
@@ -52,18 +55,26 @@ mt_status check_tensor(const mt_tensor* t, const char* name, int min_nd, int max
                                  std::to_string(max_nd));
   if (t->dtype != MT_F32 && t->dtype != MT_BF16)
     return fail(MT_ERR_DTYPE, std::string(name) + ": unknown dtype " + std::to_string(t->dtype));
-  int64_t n = 1;
+  bool none = false;
   for (int i = 0; i < t->ndim; ++i) {
     if (t->shape[i] < 0) return fail(MT_ERR_SHAPE, std::string(name) + ": negative size");
     if (t->stride[i] < 0) return fail(MT_ERR_LAYOUT, std::string(name) + ": negative stride");
+    none = none || t->shape[i] == 0;
+  }
+  if (none) return MT_OK;
+  int64_t n = 1;
+  for (int i = 0; i < t->ndim; ++i) {
+    if (t->shape[i] > kMostValues / n) return fail(MT_ERR_SHAPE, std::string(name) + ": more than 2^60 values");
     n *= t->shape[i];
   }
-  if (n > 0 && !t->data) return fail(MT_ERR_NULL, std::string(name) + ": null data pointer");
+  if (!t->data) return fail(MT_ERR_NULL, std::string(name) + ": null data pointer");
   return MT_OK;
 }
 
 int64_t numel(const mt_tensor* t) {
   int64_t n = 1;
+  for (int i = 0; i < t->ndim; ++i)
+    if (t->shape[i] == 0) return 0;
   for (int i = 0; i < t->ndim; ++i) n *= t->shape[i];
   return n;
 }
@@ -85,6 +96,7 @@ bool overlaps(const mt_tensor* a, const mt_tensor* b) {
 
 bool is_row_major(const mt_tensor* t) {
   int64_t expect = 1;
+  if (numel(t) == 0) return true;
   for (int i = t->ndim - 1; i >= 0; --i) {
     if (t->shape[i] != 1 && t->stride[i] != expect) return false;
     expect *= t->shape[i];

@@ -371,14 +371,20 @@ namespace {
 // is wrong; what, the checks of check_clip say.
 int64_t dense_numel(const mt_tensor* t) {
   if (t->ndim < 0 || t->ndim > MT_MAX_DIMS || (t->dtype != MT_F32 && t->dtype != MT_BF16)) return -1;
+  bool none = false;
+  for (int i = 0; i < t->ndim; ++i) {
+    if (t->shape[i] < 0 || t->stride[i] < 0) return -1;
+    none = none || t->shape[i] == 0;
+  }
+  if (none) return 0;
   int64_t n = 1;
   for (int i = t->ndim - 1; i >= 0; --i) {
     const int64_t size = t->shape[i];
-    if (size < 0 || size > (int64_t)1 << 40 || t->stride[i] < 0 || (size != 1 && t->stride[i] != n)) return -1;
+    if (size != 1 && t->stride[i] != n) return -1;
+    if (size > ((int64_t)1 << 40) / n) return -1;
     n *= size;
-    if (n > (int64_t)1 << 40) return -1;
   }
-  return n == 0 || t->data ? n : -1;
+  return t->data ? n : -1;
 }
 mt_status check_clip(const mt_tensor* t, bool out, int32_t i) {
   const std::string name = (out ? "out " : "grad ") + std::to_string(i);

@@ -166,6 +166,32 @@ def test_clipping():
     assert clip([A, B], ws=None, ws_bytes=0) == WS and clip([A, B], ws_bytes=4) == WS and clip([A, B], ws=WORK + 8) == WS
 
 
+def test_clipping_of_sizes_whose_product_overflows():
+    """2^64 values are not none: in 64 bits the product wraps to 0."""
+    wide = 1 << 32
+    for shape in ([wide, wide], [wide, wide, 3], [1 << 22] * 3, [1 << 40, 2], [(1 << 40) + 1]):
+        t = D(shape, ptr=0x100000)
+        assert clip([t]) == SHAPE and clip([D([5], ptr=0x200000)], [t]) == SHAPE
+        assert b.lib.mt_clip_grad_norm_workspace(1, R(t), ctypes.byref(ctypes.c_size_t())) == SHAPE
+    assert clip([D([5], ptr=0x200000)], norm=D([wide, wide], ptr=0x900000)) == SHAPE
+    for norm in (D([wide, wide], ptr=0x100000), D([1 << 31, 1 << 31, 4], ptr=0x100000)):
+        assert b.lib.mt_mse_loss(R(norm), R(norm), R(D([1], ptr=0x900000)), None, None, 0, None) == SHAPE
+
+
+def test_clipping_of_empty_tensors():
+    """A tensor without values is contiguous whatever its strides are (torch gives [5, 0] the strides 1 and 1), and without
+    data; sizes beside the 0 do not overflow."""
+    for shape, stride in (([0], [1]), ([0, 5], [5, 1]), ([5, 0], [1, 1]), ([5, 0], [0, 1]), ([3, 0, 7], [7, 7, 1]),
+                          ([1 << 40, 1 << 40, 0], [9, 9, 1])):
+        t = D(shape, ptr=0, stride=stride)
+        assert clip([t], norm=None) == 0 and clip([t], [D(shape, BF16, 0, stride)], norm=None) == 0
+        assert clip([t, D([5], ptr=0x200000)], ws_bytes=4) == WS  # the next check
+        assert clip([t], norm=None, ws_bytes=4) == WS
+    assert clip([D([5, 0], ptr=0, stride=[-1, 1])]) == LAYOUT and clip([D([-5, 0], ptr=0)]) == SHAPE
+    assert clip([D([5, 0], I32, 0)]) == DTYPE
+    assert clip([D([5, 0], ptr=0)], [D([0, 5], ptr=0)]) == SHAPE
+
+
 def test_workspaces():
     n = ctypes.c_size_t()
     ask = lambda f, *a: f(*[R(t) if isinstance(t, b.MtTensor) else t for t in a], ctypes.byref(n))

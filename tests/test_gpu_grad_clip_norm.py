@@ -27,3 +27,14 @@ def test_a_norm_past_fp32_clips_nothing(dtype):
     # the largest norm that fp32 holds clips
     one = [torch.full((1,), torch.finfo(torch.float32).max, device=DEV)]
     assert run(one, 2.0) == torch.finfo(torch.float32).max and one[0] == 2
+
+
+def test_parameters_without_values():
+    """Their gradients are clipped, and they are stepped, beside others, whatever strides torch gives them."""
+    make = lambda: [torch.empty(5, 0, device=DEV), torch.full((4, 3), 2.0, device=DEV), torch.empty(3, 0, 7, device=DEV),
+                    torch.empty(0, 6, device=DEV).T]
+    grads, params, velocity = make(), make(), make()
+    norm = run(grads, 1.0)
+    assert abs(float(norm) - 48 ** 0.5) < 1e-5 and torch.allclose(grads[1], torch.full_like(grads[1], 12 ** -0.5))
+    b.sgd_step(params, grads, velocity, 0.5)
+    assert torch.equal(params[1], 2 - 0.5 * grads[1]) and torch.equal(velocity[1], grads[1])
