@@ -22,7 +22,7 @@ namespace {
 
 PyObject *g_f32, *g_bf16, *g_i32, *g_describe, *g_current, *g_stream_of, *g_tensor, *g_parameter, *g_device;
 const DLPackExchangeAPI* g_exchange;  // torch's; NULL: none
-PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_numel, *s_element_size;
+PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_numel, *s_element_size, *s_get_device;
 
 struct Lib {
   decltype(&mt_linear_fwd) linear_fwd;
@@ -91,6 +91,19 @@ bool refuse(PyObject* t, bool index) {
   return false;
 }
 
+// The device of a tensor that is read by its attributes; -1: it names none.
+bool device_of(PyObject* t, int* device) {
+  *device = -1;
+  PyObject* v = PyObject_CallMethodNoArgs(t, s_get_device);
+  if (v) {
+    *device = (int)PyLong_AsLong(v);
+    Py_DECREF(v);
+  } else if (PyErr_ExceptionMatches(PyExc_AttributeError)) {
+    PyErr_Clear();
+  }
+  return !PyErr_Occurred();
+}
+
 // What a plain tensor holds, without taking hold of it; false: by its attributes.
 bool view_of(PyObject* t, DLTensor* x) {
   if (!g_exchange || ((PyObject*)Py_TYPE(t) != g_tensor && (PyObject*)Py_TYPE(t) != g_parameter)) return false;
@@ -147,6 +160,8 @@ struct Args {
   int used = 0;
   int device = -1;  // of the tensors so far
   bool mixed = false;
+  PyObject* unseen[13];  // tensors (12) and a workspace whose device is asked for where it matters (one_device)
+  int n_unseen = 0;
   Args(PyObject* const* args, Py_ssize_t n, Py_ssize_t want) : a(args) {
     if (n != want) {
       PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", want, n);
@@ -158,6 +173,7 @@ struct Args {
     mt_tensor* t = &d[used++];
     int dev = -1;
     ok = describe(a[i], t, index, &dev);
+    if (dev < 0) unseen[n_unseen++] = a[i];
     met(dev);
     return t;
   }
@@ -168,6 +184,11 @@ struct Args {
   }
   // The tensors lie on one device, where none is given for the stream the current one.
   bool one_device(int stream) {
+    for (int i = 0; ok && i < n_unseen; ++i) {
+      int dev = -1;
+      ok = device_of(unseen[i], &dev);
+      met(dev);
+    }
     if (!ok) return false;
     if (mixed) {
       PyErr_SetString(PyExc_ValueError, "the tensors lie on different devices");
@@ -214,6 +235,7 @@ struct Args {
       for (int d = 0; d < x.ndim; ++d) w.n *= (size_t)x.shape[d];
       return w;
     }
+    unseen[n_unseen++] = a[i];
     PyObject* c = PyObject_GetAttr(a[i], s_is_cuda);
     ok = c != nullptr;
     if (c) Py_DECREF(c);
@@ -460,7 +482,9 @@ struct Lists {
       for (Py_ssize_t i = 0; ok && i < n; ++i) {
         int dev = -1;
         ok = describe(PyTuple_GET_ITEM(held[l], i), &d[l * n + i], false, &dev);
-        if (args) args->met(dev);
+        if (!ok || !args) continue;
+        if (dev < 0) ok = device_of(PyTuple_GET_ITEM(held[l], i), &dev);
+        args->met(dev);
       }
   }
   ~Lists() {
@@ -570,7 +594,7 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     const char* name;
   } names[] = {{&s_is_cuda, "is_cuda"}, {&s_dtype, "dtype"},       {&s_shape, "shape"},
                {&s_stride, "stride"},   {&s_data_ptr, "data_ptr"}, {&s_numel, "numel"},
-               {&s_element_size, "element_size"}};
+               {&s_element_size, "element_size"}, {&s_get_device, "get_device"}};
   for (auto& e : names)
     if (!(*e.to = PyUnicode_InternFromString(e.name))) return nullptr;
   return PyModule_Create(&module);

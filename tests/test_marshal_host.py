@@ -74,3 +74,72 @@ def test_tensors_of_lists_are_held_until_the_call_returns():
 def test_generators_are_refused(call):
     with pytest.raises(TypeError):
         call(lambda: (x for x in []))
+
+
+class _On:
+    """A tensor of a device to the marshalling, read by its attributes."""
+    is_cuda, dtype, shape = True, torch.float32, (2, 4)
+
+    def __init__(self, device, dtype=torch.float32):
+        self.device_index, self.dtype = device, dtype
+
+    def get_device(self):
+        return self.device_index
+
+    def stride(self):
+        return (4, 1)
+
+    def data_ptr(self):
+        return 4096
+
+    def numel(self):
+        return 8
+
+    def element_size(self):
+        return 4
+
+
+class _Ids(_On):
+    shape = (2,)
+
+    def stride(self):
+        return (1,)
+
+
+_TWO_DEVICES = [lambda x, y, i, **k: b.layer_norm_fwd(x, None, None, y, **k), lambda x, y, i, **k: b.embedding_fwd(i, x, y, **k),
+                lambda x, y, i, **k: b.embedding_bwd(i, x, x, workspace=y, **k), lambda x, y, i, **k: b.cross_entropy(x, i, dlogits=y, **k),
+                lambda x, y, i, **k: b.layer_norm_bwd(x, None, x, y, workspace=x, **k),
+                lambda x, y, i, **k: b.clip_grad_norm([x, y], 1.0, workspace=x, **k),
+                lambda x, y, i, **k: b.clip_grad_norm([x], 1.0, out=[x], workspace=y, **k)]
+
+
+@pytest.mark.parametrize("call", _TWO_DEVICES)
+def test_tensors_read_by_their_attributes_have_a_device(call):
+    """Subclasses of a tensor on another device than the others', or than the current one, are refused as plain ones are."""
+    with pytest.raises(ValueError, match="different devices"):
+        call(_On(0), _On(1), _Ids(0, torch.int32), stream=0)
+    init = b._INIT
+    b._m.init(*init[:5], lambda: 0, *init[6:9], lambda: 1)  # the current device is 1, its stream 0
+    try:
+        with pytest.raises(ValueError, match="on device 0, the current one is 1"):
+            call(_On(0), _On(0), _Ids(0, torch.int32))
+    finally:
+        b._m.init(*init)
+
+
+def test_a_device_that_cannot_be_told():
+    """Objects that name no device are taken as before, an error in naming it is the caller's."""
+    class Broken(_On):
+        def get_device(self):
+            raise RuntimeError("no such thing")
+
+    with pytest.raises(RuntimeError, match="no such thing"):
+        b.layer_norm_fwd(Broken(0), None, None, _On(0), stream=0)
+
+    class Nowhere:
+        is_cuda, dtype, shape = True, torch.float32, (2, 4)
+        stride, data_ptr = _On.stride, _On.data_ptr
+
+    with pytest.raises(b.MtError) as e:  # one tensor twice: refused before any memory is touched
+        b.layer_norm_fwd(Nowhere(), None, None, Nowhere(), stream=0)
+    assert e.value.name == "MT_ERR_ALIAS"
