@@ -47,8 +47,9 @@ def _build_marshal() -> None:
     """The native half of binding.py: a CPython module, host code only."""
     out = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
     tmp = out + ".tmp"
-    torch_include = os.path.join(importlib.util.find_spec("torch").submodule_search_locations[0], "include")
-    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", "-I", torch_include,
+    torch = importlib.util.find_spec("torch")  # its headers, where there are any: for faster calls only
+    include = ["-I", os.path.join(torch.submodule_search_locations[0], "include")] if torch else []
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-fPIC", "-shared", "-Wall", *include,
            "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "pymarshal.cpp"), "-o", tmp, "-ldl"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

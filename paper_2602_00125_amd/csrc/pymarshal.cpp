@@ -4,7 +4,8 @@
 // a call took 11 us, more than its kernels. Nothing is kept between calls.
 //
 // Plain tensors are read through torch's DLPack exchange functions (0.08 us a
-// tensor), anything else by its Python attributes (0.5 us).
+// tensor), anything else by its Python attributes (0.5 us); all of them where torch
+// or its header has no such functions.
 //
 // init(handle, float32, bfloat16, int32, describe, current_stream, stream_of,
 // tensor, parameter, device): the library's dlopen handle, torch's dtypes, binding.desc
@@ -13,15 +14,16 @@
 // is found. Every other function returns the entry point's status.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
-#include <ATen/dlpack.h>
 #include <dlfcn.h>
+#if __has_include(<ATen/dlpack.h>)
+#include <ATen/dlpack.h>
+#endif
 
 #include "../../include/minitensor_hip.h"
 
 namespace {
 
 PyObject *g_f32, *g_bf16, *g_i32, *g_describe, *g_current, *g_stream_of, *g_tensor, *g_parameter, *g_device;
-const DLPackExchangeAPI* g_exchange;  // torch's; NULL: none
 PyObject *s_is_cuda, *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_numel, *s_element_size, *s_get_device;
 
 struct Lib {
@@ -104,31 +106,63 @@ bool device_of(PyObject* t, int* device) {
   return !PyErr_Occurred();
 }
 
-// What a plain tensor holds, without taking hold of it; false: by its attributes.
-bool view_of(PyObject* t, DLTensor* x) {
-  if (!g_exchange || ((PyObject*)Py_TYPE(t) != g_tensor && (PyObject*)Py_TYPE(t) != g_parameter)) return false;
-  if (g_exchange->dltensor_from_py_object_no_sync(t, x) == 0 && (x->strides || x->ndim == 0)) return true;
+// What a plain tensor holds.
+struct Plain {
+  void* data;
+  const int64_t *shape, *stride;
+  int ndim, device, dtype;  // the GPU, -1: the host's; MT_F32 .., -1: another type
+  size_t bytes;             // of an element
+};
+#if defined(DLPACK_MAJOR_VERSION) && defined(DLPACK_MINOR_VERSION)
+#if DLPACK_MAJOR_VERSION == 1 && DLPACK_MINOR_VERSION >= 3  // with the exchange functions
+#define MT_EXCHANGE
+#endif
+#endif
+#ifdef MT_EXCHANGE
+const DLPackExchangeAPI* g_exchange;  // torch's; NULL: none
+void find_exchange() {  // the functions live as long as torch
+  PyObject* c = PyObject_GetAttrString(g_tensor, "__dlpack_c_exchange_api__");
+  g_exchange = c && PyCapsule_IsValid(c, "dlpack_exchange_api")
+                   ? (const DLPackExchangeAPI*)PyCapsule_GetPointer(c, "dlpack_exchange_api") : nullptr;
+  if (g_exchange && (g_exchange->header.version.major != DLPACK_MAJOR_VERSION || !g_exchange->dltensor_from_py_object_no_sync))
+    g_exchange = nullptr;
+  Py_XDECREF(c);
   PyErr_Clear();
-  return false;
 }
-bool on_device(const DLTensor& x) { return x.device.device_type == kDLROCM || x.device.device_type == kDLCUDA; }
+// Without taking hold of it; false: by its attributes.
+bool view_of(PyObject* t, Plain* v) {
+  if (!g_exchange || ((PyObject*)Py_TYPE(t) != g_tensor && (PyObject*)Py_TYPE(t) != g_parameter)) return false;
+  DLTensor x;
+  if (g_exchange->dltensor_from_py_object_no_sync(t, &x) != 0 || (!x.strides && x.ndim > 0)) {
+    PyErr_Clear();
+    return false;
+  }
+  const bool gpu = x.device.device_type == kDLROCM || x.device.device_type == kDLCUDA, one = x.dtype.lanes == 1;
+  *v = Plain{(char*)x.data + x.byte_offset, x.shape, x.strides, x.ndim, gpu ? x.device.device_id : -1, -1,
+             ((size_t)x.dtype.bits * x.dtype.lanes + 7) / 8};
+  if (one && x.dtype.code == kDLInt && x.dtype.bits == 32) v->dtype = MT_I32;
+  if (one && x.dtype.code == kDLFloat && x.dtype.bits == 32) v->dtype = MT_F32;
+  if (one && x.dtype.code == kDLBfloat && x.dtype.bits == 16) v->dtype = MT_BF16;
+  return true;
+}
+#else
+void find_exchange() {}
+bool view_of(PyObject*, Plain*) { return false; }
+#endif
 
 // index: a tensor of int32 lengths, positions, tokens or classes, else one of the two dtypes.
 // device: receives a plain tensor's.
 bool describe(PyObject* t, mt_tensor* d, bool index = false, int* device = nullptr) {
-  DLTensor x;
+  Plain x;
   if (view_of(t, &x)) {
-    if (!on_device(x) || x.dtype.lanes != 1 || x.ndim > MT_MAX_DIMS) return refuse(t, index);
-    if (index && x.dtype.code == kDLInt && x.dtype.bits == 32) d->dtype = MT_I32;
-    else if (!index && x.dtype.code == kDLFloat && x.dtype.bits == 32) d->dtype = MT_F32;
-    else if (!index && x.dtype.code == kDLBfloat && x.dtype.bits == 16) d->dtype = MT_BF16;
-    else return refuse(t, index);
-    if (device) *device = x.device.device_id;
-    d->data = (char*)x.data + x.byte_offset;
+    if (x.device < 0 || x.dtype < 0 || (x.dtype == MT_I32) != index || x.ndim > MT_MAX_DIMS) return refuse(t, index);
+    if (device) *device = x.device;
+    d->dtype = x.dtype;
+    d->data = x.data;
     d->ndim = x.ndim;
     for (int i = 0; i < x.ndim; ++i) {
       d->shape[i] = x.shape[i];
-      d->stride[i] = x.strides[i];
+      d->stride[i] = x.stride[i];
     }
     return true;
   }
@@ -227,11 +261,11 @@ struct Args {
   Ws ws(int i) {
     Ws w;
     if (!ok || a[i] == Py_None) return w;
-    DLTensor x;
-    if (view_of(a[i], &x) && on_device(x)) {
-      met(x.device.device_id);
-      w.p = (char*)x.data + x.byte_offset;
-      w.n = ((size_t)x.dtype.bits * x.dtype.lanes + 7) / 8;
+    Plain x;
+    if (view_of(a[i], &x) && x.device >= 0) {
+      met(x.device);
+      w.p = x.data;
+      w.n = x.bytes;
       for (int d = 0; d < x.ndim; ++d) w.n *= (size_t)x.shape[d];
       return w;
     }
@@ -563,14 +597,7 @@ FN(init) {
     Py_INCREF(a[i + 1]);
     Py_XSETREF(*to[i], a[i + 1]);
   }
-  // the functions live as long as torch
-  PyObject* c = PyObject_GetAttrString(g_tensor, "__dlpack_c_exchange_api__");
-  g_exchange = c && PyCapsule_IsValid(c, "dlpack_exchange_api")
-                   ? (const DLPackExchangeAPI*)PyCapsule_GetPointer(c, "dlpack_exchange_api") : nullptr;
-  if (g_exchange && (g_exchange->header.version.major != DLPACK_MAJOR_VERSION || !g_exchange->dltensor_from_py_object_no_sync))
-    g_exchange = nullptr;
-  Py_XDECREF(c);
-  PyErr_Clear();
+  find_exchange();
   Py_RETURN_NONE;
 }
 
