@@ -1,8 +1,8 @@
-"""mt_cross_entropy's sums of a row's exponentials, however many of them a thread meets."""
+"""mt_cross_entropy's sums: a row's exponentials, however many of them a thread meets, and the mean over many rows."""
 import pytest
 import torch
 
-from language_reference import DEV, DT, close, cross_entropy
+from language_reference import DEV, DT, U, close, cross_entropy, draw, integers
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,16 @@ def test_rows_of_many_logits(V, x):
     got = run(z, t, "f32")
     for name, g, w in zip(("loss", "losses", "dlogits"), got, cross_entropy(z, t, torch.float32)):
         close(name, g, *w)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V", [(100000, 33), (1000, 10), (300, 40), (40000, 1025), (20000, 513), (3000, 5000)])
+def test_the_mean_is_that_of_the_losses(M, V, x):
+    """The losses are added in 64 bits and the mean is rounded once: half a step."""
+    z, t = draw((M, V), x, 1, 2.0), integers((M,), -1, V, 2)
+    n = int((t >= 0).sum())
+    for out in (None, "bf16"):
+        loss, losses, _ = run(z, t, out)
+        assert not losses[t < 0].any()
+        want = losses.double().sum() / n
+        assert abs(float(loss) - float(want)) <= (U + 1e-12) * float(want)
