@@ -12,7 +12,7 @@
 // ones have a block each, whose threads hold 16 or 32 values through the row's
 // maximum, its sum and the gradient, exponentials in the logits' registers. Of rows
 // longer than that a thread keeps a running maximum and sum and reads them again,
-// from the caches: 8192 x 50001 fp32 to bf16, a fifth of it padding, 457 us, 4.65
+// from the caches: 8192 x 50001 fp32 to bf16, a fifth of it padding, 460 us, 4.64
 // TB/s of what has to move. Holding nothing took 500 us, 16 values 488, 64 (too many
 // registers for two blocks a CU) 563, and rows held whole by 1024 threads 811: one
 // block a CU, whose loads, arithmetic and stores took turns.

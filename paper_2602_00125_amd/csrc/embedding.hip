@@ -22,9 +22,9 @@
 // 3. join_kernel. Where a run goes on past its first chunk, its pieces are added
 //    in order, in 64 bits.
 //
-// 16384 tokens of 1024 fp32 values into 50001 rows: 73 us for 272 MB, of which the
+// 16384 tokens of 1024 fp32 values into 50001 rows: 74 us for 272 MB, of which the
 // first launch takes 9 (it waits for loads, LDS and its own order), the second 55
-// (276 MB moved, 5.0 TB/s), the third 7 (a chain of loads). Clearing part of the
+// (276 MB moved, 5.0 TB/s), the third 8 (a chain of loads). Clearing part of the
 // rows in the first and the last launch too moved their time, and saved none.
 // A few tokens take one launch instead (few_kernel).
 #include <hip/hip_runtime.h>
@@ -182,7 +182,7 @@ __device__ __forceinline__ void clear(const EmbeddingGradParams& p, int block, i
 }
 
 // Sum: what a run's rows are added in, fp32 where a chunk has up to kEmbedChunk of
-// them (in 64 bits three waves a SIMD would be left for four).
+// them (64 bits take registers: three waves a SIMD, not four).
 template <bool BF, typename Sum>
 __global__ __launch_bounds__(256) void sum_kernel(const EmbeddingGradParams p, int G_shift, int tiles, int sum_blocks) {
   if ((int)blockIdx.x >= sum_blocks) {

@@ -195,8 +195,8 @@ NormForm norm_form(mt::LayerNormParams* p, int vec, int values, int threads, int
   const int most = values / vec;  // groups a lane
   for (p->L = 1; p->L < 64 && p->L * vec * most < p->C;) p->L *= 2;
   if (p->L * vec * most < p->C) {
-    // as few whole waves as hold a row (13107 x 2560 bf16 40 us by four, 28 by three; 2730 x 12288 44 by 16, 36 by
-    // 12), but eight rather than six or seven (5461 x 6144 32 us by eight, 38 by six)
+    // as few whole waves as hold a row (13107 x 2560 bf16 40 us by four, 29 by three; 2730 x 12288 46 by 16, 36 by
+    // 12), but eight rather than six or seven (5461 x 6144 34 us by eight, 35 by six)
     int waves = (int)cdiv(p->C, (int64_t)64 * vec * most);
     if (waves == 6 || waves == 7) waves = 8;
     p->L = 64 * waves;
@@ -221,8 +221,8 @@ mt_status layer_norm_fwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
   p.b = b ? (const float*)b->data : nullptr;
   p.out = y->data;
   p.ldo = row_pitch(y);
-  // 16 values a lane, or 8 where that takes a part of a wave, three, four or eight waves (524288 x 64 bf16 33 -> 26
-  // us, 21845 x 1536 35 -> 28, 8192 x 4096 32 -> 29; by five waves 13107 x 2560 28 -> 32)
+  // 16 values a lane, or 8 where that takes a part of a wave, three, four or eight waves (524288 x 64 bf16 37 -> 28
+  // us, 21845 x 1536 37 -> 31, 8192 x 4096 33 -> 29; by five waves 13107 x 2560 29 -> 32)
   const int waves = (int)cdiv(p.C, 512);
   const int values = p.C <= 512 || waves == 3 || waves == 4 || waves == 8 ? 8 : 16;
   // eight blocks a CU, or seven of the forms of 512 to 1024 columns, whose registers have room for no more: of eight the
@@ -248,9 +248,10 @@ mt_status layer_norm_bwd_impl(const mt_tensor* x, const mt_tensor* w, const mt_t
   if ((dw && (s = check_vector(dw, "dw", p.C))) || (db && (s = check_vector(db, "db", p.C))) ||
       (s = check_apart({dx, dw, db}, {x, w, dy})))
     return s;
-  // two blocks a CU up to 4096 columns (524288 x 64 fp32 93 -> 86 us, 16384 x 2048 bf16 61 -> 55); of longer rows
-  // one, whose sums of dw and db are half as many (4096 x 8192 bf16 70 us, two blocks 74)
-  // 8 values a lane for short rows (524288 x 64 bf16 55 -> 49), 16 for others (32768 x 1024 bf16 47, 8 values 62)
+  // two blocks a CU up to 4096 columns (524288 x 64 bf16 51 -> 48 us, 16384 x 2048 bf16 65 -> 57); of longer rows
+  // one, whose sums of dw and db are half as many (2048 x 16384 bf16 73 us, two blocks 88; 512 x 6075 fp32 23, 29; bf16
+  // rows of 6144 and 8192 alone take two the better, 4096 x 8192 70 us, 63)
+  // 8 values a lane for short rows (524288 x 64 bf16 53 -> 48), 16 for others (32768 x 1024 bf16 49, 8 values 61)
   const NormForm f = norm_form(&p, vector_of({x, dy}), p.C <= 512 ? 8 : 16, p.C <= 4096 ? 512 : 1024,
                                p.C <= 4096 ? 512 : 256);
   const bool weights = dw || db;

@@ -48,7 +48,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int L, int grp, float (*
       for (int i = 0; i < N; ++i) red[i][wave] = v[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {  // 16 lanes read a wave's sum each, at once (one after another 2730 x 12288 bf16 37 us, so 36)
+    // 16 lanes read a wave's sum each (one after another: 2730 x 12288 bf16 37 us, this way 36)
+    for (int i = 0; i < N; ++i) {
       const int w = threadIdx.x & 15;
       v[i] = lanes_sum(w < W ? red[i][first + w] : 0.f, 16);
     }
@@ -59,8 +60,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], int L, int grp, float (*
 // not whole, is the row's last VEC values: those before `lo` belong to the group
 // before it, take no part in sums and are written twice alike. (By element a
 // wave would go through up to seven loads and stores for it: 32768 x 1023 bf16
-// 54 us, this way 31.) hi: VEC, or C where a row has less. WHOLE: C is a multiple
-// of VEC, and a group has all its columns or none (1024: 29.5 us as any, 28 whole).
+// 54 us, this way 30.) hi: VEC, or C where a row has less. WHOLE: C is a multiple
+// of VEC, and a group has all its columns or none (1024: 27 us as any, 26 whole).
 template <int VEC, bool WHOLE>
 struct Columns {
   int c, lo, hi;
